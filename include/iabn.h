@@ -343,6 +343,93 @@ int iabn_ckpt_backward(const void *xhat, void *dz_dx, int dtype, const float *ga
                        float eps, float slope, int64_t N, int64_t C, int64_t HW,
                        void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * A transformer's feed-forward sublayer
+ * -------------------------------------
+ * The entry points below take rows instead of channels: x is [R, C], R tokens
+ * of C values, contiguous, of one storage type.  They share the conventions
+ * above (caller-owned memory, asynchronous, host validation before any launch,
+ * fixed order of every sum, any alignment of an element).  R may be 0: a
+ * forward then does nothing, and a backward writes the zeros that sums over
+ * no rows are.
+ */
+
+/* Norms.  hat = v/sqrt(mean(v^2) + eps) (RMS) or (v - mean)/sqrt(var + eps)
+ * (LAYER, the biased variance), over the C values of a row. */
+typedef enum { IABN_NORM_NONE = 0, IABN_NORM_RMS = 1, IABN_NORM_LAYER = 2 } iabn_norm_t;
+
+/*
+ * Dropout: y = x*k/(1 - p) with k in {0, 1} a function of (seed, offset,
+ * place) alone; no mask is stored, and the same call on a gradient is the
+ * backward.  y may be x.
+ *   p              in [0, 1], taken to the nearest 2^-16 (the scale uses the
+ *                  same value); 1 drops everything.  A dropped value is 0,
+ *                  whatever x holds.
+ *   seed, offset   the generator's key and the upper half of its counter:
+ *                  Philox4x32-10; element (row, col) takes 16 bits of the
+ *                  output for the counter (row*ceil(C/8) + col/8, offset):
+ *                  word col%8/2, the low half for even col.  It is kept where
+ *                  they are >= p*2^16.  Calls with another seed or offset are
+ *                  independent.
+ *   R, C           rows and width; C < 2^31, R*C <= 2^46.
+ */
+int iabn_dropout(const void *x, void *y, int dtype, float p, uint64_t seed, uint64_t offset,
+                 int64_t R, int64_t C, void *stream);
+
+/*
+ * The norms around a block, fused with its gate, residual scale and dropout:
+ *
+ *   r = alpha*x + beta*gate*D(post(h)),   u = pre(r)
+ *
+ * x is the residual stream, h the block's output; post is the norm after the
+ * block, pre the norm before the next one.  A norm is hat*weight + bias.
+ *   x              [R, C].
+ *   h              [R, C], or NULL: r = alpha*x (post, gate, p are not used).
+ *   r              [R, C] out, or NULL where only u is wanted.  May be x or h.
+ *   u              [R, C] out; NULL if and only if pre_norm is NONE.  May be x
+ *                  or h, not r.  Formed from r before it is rounded.
+ *   gate           [groups, C] of the storage type, or NULL (1): row i takes
+ *                  row i/(R/groups) of it.  groups divides R: 1 is a gate
+ *                  per channel, R a gate per element.
+ *   *_norm         an iabn_norm_t; *_weight, *_bias [C] fp32, or NULL (1, 0).
+ *   *_stats        [2, R] fp32 out, or NULL: the mean (RMS: 0) and 1/sqrt(. +
+ *                  eps) of every row, which the backward takes.
+ *   p, seed, offset  as in iabn_dropout; p = 0 for none.
+ *   C              at most 16384.
+ * No workspace.
+ *
+ * iabn_resnorm_backward: its gradients, from dr and du (the gradients of r
+ * and u), the r and h that the forward kept, and the statistics.
+ *   dr             [R, C], or NULL (0).      du  [R, C]; NULL if and only if
+ *                  pre_norm is NONE.         r   [R, C], read where du is.
+ *   h              [R, C]; NULL where post_norm is NONE and dgate is NULL.
+ *   dx, dh         [R, C] out, or NULL where not wanted.  Either may be dr,
+ *                  du, r or h (not both the same).  dx = alpha*dL/dr.
+ *   dgate          [groups, C] out, storage type, or NULL.
+ *   dpost_weight, dpost_bias, dpre_weight, dpre_bias  [C] fp32 out, or NULL;
+ *                  only where there is the norm.
+ * All outputs are overwritten.  Dropout's mask is made again from (p, seed,
+ * offset).  The workspace holds iabn_resnorm_workspace_size(R, C, groups)
+ * bytes (groups 0: no gate), 16-byte aligned.
+ */
+int iabn_resnorm_forward(const void *x, const void *h, void *r, void *u, int dtype,
+                         const void *gate, int64_t groups, int post_norm,
+                         const float *post_weight, const float *post_bias, int pre_norm,
+                         const float *pre_weight, const float *pre_bias, float *post_stats,
+                         float *pre_stats, float alpha, float beta, float eps, float p,
+                         uint64_t seed, uint64_t offset, int64_t R, int64_t C, void *stream);
+
+size_t iabn_resnorm_workspace_size(int64_t R, int64_t C, int64_t groups);
+
+int iabn_resnorm_backward(const void *dr, const void *du, const void *r, const void *h, void *dx,
+                          void *dh, int dtype, const void *gate, int64_t groups, int post_norm,
+                          const float *post_weight, const float *post_bias, int pre_norm,
+                          const float *pre_weight, const float *post_stats,
+                          const float *pre_stats, void *dgate, float *dpost_weight,
+                          float *dpost_bias, float *dpre_weight, float *dpre_bias, float alpha,
+                          float beta, float p, uint64_t seed, uint64_t offset, int64_t R,
+                          int64_t C, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -37,7 +37,8 @@ __all__ = [
     "iabn_forward_stats", "iabn_forward_apply", "iabn_backward_reduce", "iabn_backward_apply",
     "iabn_backward_ii", "iabn_std_forward_train", "iabn_std_backward", "iabn_ckpt_forward_train",
     "iabn_ckpt_recompute", "iabn_ckpt_backward", "iabn_plan", "iabn_forward_train_noalloc",
-    "DTYPE_CODES", "OPS",
+    "DTYPE_CODES", "OPS", "NORMS",
+    "iabn_dropout", "iabn_resnorm_forward", "iabn_resnorm_workspace_size", "iabn_resnorm_backward",
 ]
 
 DTYPE_CODES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
@@ -62,9 +63,10 @@ _lib_lock = threading.Lock()
 _NATIVE = ("iabn_workspace_size", "iabn_forward_train", "iabn_forward_train_noalloc",
            "iabn_forward_eval", "iabn_backward", "iabn_backward_ii", "iabn_std_forward_train",
            "iabn_std_backward", "iabn_ckpt_forward_train", "iabn_ckpt_recompute",
-           "iabn_ckpt_backward")
+           "iabn_ckpt_backward", "iabn_dropout", "iabn_resnorm_forward",
+           "iabn_resnorm_workspace_size", "iabn_resnorm_backward")
 (_WORKSPACE_SIZE, _FORWARD_TRAIN, _FORWARD_TRAIN_NOALLOC, _FORWARD_EVAL, _BACKWARD, _BACKWARD_II,
- _STD_FORWARD, _STD_BACKWARD, _CKPT_FORWARD, _CKPT_RECOMPUTE, _CKPT_BACKWARD) = range(len(_NATIVE))
+ _STD_FORWARD, _STD_BACKWARD, _CKPT_FORWARD, _CKPT_RECOMPUTE, _CKPT_BACKWARD) = range(11)
 
 
 class IabnError(RuntimeError):
@@ -95,6 +97,7 @@ def load():
 def declare(lib):
     """Attach the C signatures of include/iabn.h to a loaded libiabn handle."""
     vp, i64, f32, sz, i32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t, ctypes.c_int
+    u64 = ctypes.c_uint64
     sig = {
         "iabn_version": ([], i32),
         "iabn_status_string": ([i32], ctypes.c_char_p),
@@ -115,6 +118,12 @@ def declare(lib):
         "iabn_ckpt_recompute": ([vp, vp, i32, vp, vp, f32, i64, i64, i64, vp], i32),
         "iabn_ckpt_backward": ([vp, vp, i32, vp, vp, vp, vp, vp, f32, f32, i64, i64, i64, vp, sz, vp], i32),
         "iabn_plan": ([i32, i32, i64, i64, i64, ctypes.POINTER(_Plan)], i32),
+        "iabn_dropout": ([vp, vp, i32, f32, u64, u64, i64, i64, vp], i32),
+        "iabn_resnorm_forward": ([vp, vp, vp, vp, i32, vp, i64, i32, vp, vp, i32, vp, vp, vp, vp, f32, f32, f32, f32,
+                                  u64, u64, i64, i64, vp], i32),
+        "iabn_resnorm_workspace_size": ([i64, i64, i64], sz),
+        "iabn_resnorm_backward": ([vp, vp, vp, vp, vp, vp, i32, vp, i64, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp,
+                                   vp, f32, f32, f32, u64, u64, i64, i64, vp, sz, vp], i32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -141,6 +150,7 @@ def _first_call(*args):
                 module = importlib.util.module_from_spec(spec)
                 spec.loader.exec_module(module)
                 _call = module.call
+                _sublayer.native = module
             except Exception as e:  # noqa: BLE001
                 warnings.warn("libiabn's native fast path is not available, calls are marshalled in "
                               "Python: %s" % e, RuntimeWarning, stacklevel=4)
@@ -500,3 +510,8 @@ def iabn_backward_apply(z, dz_dx, gamma, beta, save_var, dgamma, dbeta, eps, slo
                                     N, C, HW, wp, wb, _stream(dev, stream))
     _check("iabn_backward_apply", rc)
     return dz_dx
+
+
+from . import sublayer as _sublayer  # noqa: E402
+from .sublayer import (NORMS, iabn_dropout, iabn_resnorm_backward, iabn_resnorm_forward,  # noqa: E402
+                       iabn_resnorm_workspace_size)

@@ -32,7 +32,12 @@ enum Op : long {
     kCkptForward,
     kCkptRecompute,
     kCkptBackward,
-    kOps
+    kOps,
+    // The feed-forward sublayer's, each with a function of its own below.
+    kDropout = kOps,
+    kResnormForward,
+    kResnormWorkspaceSize,
+    kResnormBackward
 };
 
 // What follows the table and the op in a call: activation tensors,
@@ -205,7 +210,223 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
     }
 }
 
+// ---------------------------------------------------------------- the sublayer
+
+// The arguments of a sublayer's call, taken one after the other; `plain` turns
+// false at the first one that is not as it should be.
+struct Args {
+    PyObject* const* at;
+    bool plain = true;
+    int64_t R = -1, C = 0;
+    int code = -1;
+    at::Device dev{at::kCPU};
+
+    const at::Tensor* tensor(bool optional) {
+        PyObject* const o = *at++;
+        if (optional && o == Py_None) return nullptr;
+        if (!plain || !THPVariable_CheckExact(o)) {
+            plain = false;
+            return nullptr;
+        }
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || !t.is_contiguous()) plain = false;
+        return plain ? &t : nullptr;
+    }
+    // A tensor of [..., C]: the first one of the call says which R and C.
+    void* rows(bool optional = false) {
+        const at::Tensor* const t = tensor(optional);
+        if (t == nullptr) return nullptr;
+        const int64_t d = t->dim();
+        if (d < 1) return plain = false, nullptr;
+        if (R < 0) {
+            C = t->size(d - 1);
+            R = 1;
+            for (int64_t i = 0; i + 1 < d; ++i) R *= t->size(i);
+            code = dtype_code(t->scalar_type());
+            dev = t->device();
+            if (code < 0) plain = false;
+        } else if (t->size(d - 1) != C || t->numel() != R * C || dtype_code(t->scalar_type()) != code ||
+                   t->device() != dev) {
+            plain = false;
+        }
+        return plain ? t->data_ptr() : nullptr;
+    }
+    // A tensor of the rows' type, of whole rows of C; their number in `n`.
+    void* gate(int64_t& n) {
+        n = 0;
+        const at::Tensor* const t = tensor(true);
+        if (t == nullptr) return nullptr;
+        if (t->dim() < 1 || t->size(t->dim() - 1) != C || C == 0 || dtype_code(t->scalar_type()) != code ||
+            t->device() != dev)
+            return plain = false, nullptr;
+        n = t->numel() / C;
+        return t->data_ptr();
+    }
+    float* floats(int64_t n) {
+        const at::Tensor* const t = tensor(true);
+        if (t == nullptr) return nullptr;
+        if (t->scalar_type() != at::kFloat || t->numel() != n || t->device() != dev)
+            return plain = false, nullptr;
+        return static_cast<float*>(t->data_ptr());
+    }
+    float number() {
+        PyObject* const o = *at++;
+        if (!plain || !(PyFloat_Check(o) || PyLong_Check(o))) return plain = false, 0.0f;
+        const double v = PyFloat_AsDouble(o);
+        if (PyErr_Occurred()) plain = false;
+        return static_cast<float>(v);
+    }
+    int choice() {
+        PyObject* const o = *at++;
+        if (!plain || !PyLong_CheckExact(o)) return plain = false, 0;
+        const long v = PyLong_AsLong(o);
+        if (PyErr_Occurred() || v < 0 || v > 1000) plain = false;
+        return static_cast<int>(v);
+    }
+    uint64_t word() {
+        PyObject* const o = *at++;
+        if (!plain || !PyLong_CheckExact(o)) return plain = false, 0;
+        const uint64_t v = PyLong_AsUnsignedLongLong(o);
+        if (PyErr_Occurred()) plain = false;
+        return v;
+    }
+    // The caller's workspace, or none (`own`).
+    at::Tensor workspace(bool& own) {
+        PyObject* const o = *at++;
+        own = o == Py_None;
+        if (own) return at::Tensor();
+        if (!plain || !THPVariable_CheckExact(o)) return plain = false, at::Tensor();
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (t.device() != dev || !t.is_contiguous()) plain = false;
+        return t;
+    }
+    void* stream() const { return c10::hip::getCurrentHIPStream(dev.index()).stream(); }
+    void take(at::Tensor& ws, bool own, size_t need) const {
+        if (own)
+            ws = at::empty({static_cast<int64_t>(need ? need : 1)},
+                           at::TensorOptions().dtype(at::kByte).device(dev));
+    }
+};
+
+size_t bytes_of(const at::Tensor& t) { return t.numel() * t.element_size(); }
+
+// Runs `fn` without the GIL (an allocation can wait for the device and a
+// launch for room in the queue).
+template <typename Fn>
+PyObject* without_gil(Fn fn) {
+    int rc = 0;
+    PyThreadState* thread = PyEval_SaveThread();
+    try {
+        rc = fn();
+    } catch (...) {
+        PyEval_RestoreThread(thread);
+        throw;
+    }
+    PyEval_RestoreThread(thread);
+    return PyLong_FromLong(rc);
+}
+
+PyObject* dropout_checked(void* const* table, Args& a) {
+    void* const x = a.rows();
+    void* const y = a.rows();
+    const float p = a.number();
+    const uint64_t seed = a.word(), offset = a.word();
+    if (!a.plain) return not_plain();
+    return without_gil([&] {
+        return entry<decltype(iabn_dropout)>(table, kDropout)(x, y, a.code, p, seed, offset, a.R, a.C,
+                                                              a.stream());
+    });
+}
+
+PyObject* resnorm_forward_checked(void* const* table, Args& a) {
+    void* const x = a.rows();
+    void* const h = a.rows(true);
+    void* const r = a.rows(true);
+    void* const u = a.rows(true);
+    int64_t groups;
+    void* const gate = a.gate(groups);
+    const int post = a.choice();
+    float* const post_w = a.floats(a.C);
+    float* const post_b = a.floats(a.C);
+    const int pre = a.choice();
+    float* const pre_w = a.floats(a.C);
+    float* const pre_b = a.floats(a.C);
+    float* const post_stats = a.floats(2 * a.R);
+    float* const pre_stats = a.floats(2 * a.R);
+    const float alpha = a.number(), beta = a.number(), eps = a.number(), p = a.number();
+    const uint64_t seed = a.word(), offset = a.word();
+    if (!a.plain) return not_plain();
+    return without_gil([&] {
+        return entry<decltype(iabn_resnorm_forward)>(table, kResnormForward)(
+            x, h, r, u, a.code, gate, groups, post, post_w, post_b, pre, pre_w, pre_b, post_stats,
+            pre_stats, alpha, beta, eps, p, seed, offset, a.R, a.C, a.stream());
+    });
+}
+
+PyObject* resnorm_backward_checked(void* const* table, Args& a) {
+    void* const dr = a.rows(true);
+    void* const du = a.rows(true);
+    void* const r = a.rows(true);
+    void* const h = a.rows(true);
+    void* const dx = a.rows(true);
+    void* const dh = a.rows(true);
+    if (a.R < 0) return not_plain();
+    int64_t groups, dgroups;
+    void* const gate = a.gate(groups);
+    const int post = a.choice();
+    float* const post_w = a.floats(a.C);
+    float* const post_b = a.floats(a.C);
+    const int pre = a.choice();
+    float* const pre_w = a.floats(a.C);
+    float* const post_stats = a.floats(2 * a.R);
+    float* const pre_stats = a.floats(2 * a.R);
+    void* const dgate = a.gate(dgroups);
+    float* const dpost_w = a.floats(a.C);
+    float* const dpost_b = a.floats(a.C);
+    float* const dpre_w = a.floats(a.C);
+    float* const dpre_b = a.floats(a.C);
+    const float alpha = a.number(), beta = a.number(), p = a.number();
+    const uint64_t seed = a.word(), offset = a.word();
+    bool own;
+    at::Tensor ws = a.workspace(own);
+    if (!a.plain || (dgate && dgroups != groups)) return not_plain();
+    return without_gil([&] {
+        a.take(ws, own, entry<decltype(iabn_resnorm_workspace_size)>(table, kResnormWorkspaceSize)(
+                            a.R, a.C, groups));
+        return entry<decltype(iabn_resnorm_backward)>(table, kResnormBackward)(
+            dr, du, r, h, dx, dh, a.code, gate, groups, post, post_w, post_b, pre, pre_w, post_stats,
+            pre_stats, dgate, dpost_w, dpost_b, dpre_w, dpre_b, alpha, beta, p, seed, offset, a.R, a.C,
+            ws.data_ptr(), bytes_of(ws), a.stream());
+    });
+}
+
+// fn(table, arguments...) -> status or NotImplemented, as `call`.
+template <PyObject* (*FN)(void* const*, Args&), Py_ssize_t N>
+PyObject* sublayer(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    try {
+        if (n != N + 1) return not_plain();
+        void* const* table = static_cast<void* const*>(PyLong_AsVoidPtr(args[0]));
+        if (table == nullptr) return not_plain();
+        Args a{args + 1};
+        return FN(table, a);
+    } catch (abi::__forced_unwind&) {
+        throw;
+    } catch (...) {
+        return not_plain();
+    }
+}
+
+template <PyObject* (*FN)(void* const*, Args&), Py_ssize_t N>
+PyCFunction method() {
+    return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(sublayer<FN, N>));
+}
+
 PyMethodDef methods[] = {
+    {"dropout", method<dropout_checked, 5>(), METH_FASTCALL, "iabn_dropout, as call"},
+    {"resnorm_forward", method<resnorm_forward_checked, 19>(), METH_FASTCALL,
+     "iabn_resnorm_forward, as call"},
+    {"resnorm_backward", method<resnorm_backward_checked, 24>(), METH_FASTCALL,
+     "iabn_resnorm_backward, as call"},
     {"call", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(call)), METH_FASTCALL,
      "call(table, op, tensors..., floats...[, workspace]) -> status or NotImplemented"},
     {nullptr, nullptr, 0, nullptr}};

@@ -13,17 +13,18 @@
 #include <cmath>
 #include <mutex>
 
+#include "errors.h"
 #include "launch.h"
 #include "tile.h"
 
 #define IABN_VERSION 10100
 
 namespace iabn_impl {
+
 namespace {
-
 thread_local char g_last_error[256] = "";
+}  // namespace
 
-int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 int fail(int code, const char* fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
@@ -36,6 +37,8 @@ int ok() {
     g_last_error[0] = '\0';
     return IABN_OK;
 }
+
+namespace {
 
 constexpr int64_t kMaxChannelElems = (int64_t(1) << 31) - 1;
 constexpr int64_t kMaxChannels = int64_t(1) << 20;
@@ -492,11 +495,15 @@ int check_params(float eps, float slope) {
     return IABN_OK;
 }
 
+}  // namespace
+
 int launched(const char* what) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(IABN_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
     return ok();
 }
+
+namespace {
 
 int validate_common(int dtype, int64_t N, int64_t C, int64_t HW, bool train) {
     if (!valid_dtype(dtype)) return fail(IABN_ERR_DTYPE, "unknown dtype %d", dtype);

@@ -1,0 +1,334 @@
+// Backward of the norms around a block (resnorm_fwd.hip).  Per row, with
+// rhat, hhat the normalised rows of r and h (from the saved statistics):
+//
+//   a  = du*w',  g = dr + rho'*(a - [mean a] - rhat*mean(a*rhat))
+//   dx = alpha*g,  e = beta*g*D,  dn = e*gate
+//   b  = dn*w,   dh = rho*(b - [mean b] - hhat*mean(b*hhat))
+//
+// ([.]: layer norms only), and over the rows dw' = sum du*rhat, db' = sum du,
+// dw = sum dn*hhat, db = sum dn, and over the rows of a gate dgate = sum e*n.
+//
+// Bound by HBM traffic: dr, du, r, h in and dx, dh out, 6 row-sized
+// transfers, all of them once: the threads of a row keep it in registers over
+// the two sums, and keep its columns' sums over the rows in registers from
+// row to row, so the vectors' gradients cost no second reading.  A block
+// therefore goes through many rows (a segment); the next row's loads are
+// issued before this row's sums.  Each block leaves its columns' sums in the
+// workspace and a second kernel adds the blocks' in double, in a fixed order.
+#include "sublayer.h"
+
+namespace iabn_impl {
+namespace {
+
+// ONE_WAVE: a block is kRows rows at a time of one wave each.
+constexpr int kRows = 4;
+
+template <int DT, int K>
+struct RowRegs {
+    typename ChunkOf<DT>::vec dr[K], du[K], r[K], h[K];
+};
+
+template <int DT, int K, bool POST, bool PRE>
+__device__ __forceinline__ void load_row(const ResnormBwdArgs& a, int64_t row, const int (&n)[K],
+                                         const int (&col)[K], RowRegs<DT, K>& x) {
+    const int64_t base = row * a.C;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (a.dr) x.dr[k] = load_chunk<DT, kStream>(a.dr, base + col[k], n[k]);
+        if constexpr (PRE) {
+            x.du[k] = load_chunk<DT, kStream>(a.du, base + col[k], n[k]);
+            x.r[k] = load_chunk<DT, kStream>(a.r, base + col[k], n[k]);
+        }
+        if constexpr (POST) {
+            if (a.h) x.h[k] = load_chunk<DT, kStream>(a.h, base + col[k], n[k]);
+        }
+    }
+}
+
+// Adds up the block's columns' sums and leaves them at `out`: the threads of
+// one row at a time hold every column once; kRows waves add theirs in LDS.
+template <int K, bool ONE_WAVE, typename Put>
+__device__ __forceinline__ void flush(float (&acc)[K][kChunk], const int (&n)[K],
+                                      const int (&col)[K], float* lds, Put put) {
+    if constexpr (ONE_WAVE) {
+        const int w = threadIdx.x / kWave;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) lds[(w * kChunk + j) * kWave + lane_id()] = acc[0][j];
+        __syncthreads();
+        if (w == 0) {
+#pragma unroll
+            for (int j = 0; j < kChunk; ++j) {
+                float s = acc[0][j];
+                for (int i = 1; i < kRows; ++i) s += lds[(i * kChunk + j) * kWave + lane_id()];
+                acc[0][j] = s;
+            }
+            put(0, n[0], col[0], acc[0]);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < K; ++k) put(k, n[k], col[k], acc[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) acc[k][j] = 0.0f;
+}
+
+template <int DT, int K, bool ONE_WAVE, bool POST, bool PRE>
+__global__ __launch_bounds__(ONE_WAVE ? kRows * kWave : kMaxRowWaves * kWave)
+void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
+    __shared__ SumSlot slots[4];
+    __shared__ float lds[ONE_WAVE ? kRows * kWave * kChunk : 1];
+    const int t = ONE_WAVE ? lane_id() : threadIdx.x, T = ONE_WAVE ? kWave : waves * kWave;
+    const int first = ONE_WAVE ? threadIdx.x / kWave : 0;
+    constexpr int kStep = ONE_WAVE ? kRows : 1;
+    int n[K], col[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int c = t + k * T;
+        n[k] = max(min(kChunk, a.C - c * kChunk), 0);
+        col[k] = c * kChunk;
+    }
+    // The columns' sums: dw, db, dgate; dw', db'.
+    float sw[POST ? K : 1][kChunk] = {}, sb[POST ? K : 1][kChunk] = {}, sg[POST ? K : 1][kChunk] = {};
+    float tw[PRE ? K : 1][kChunk] = {}, tb[PRE ? K : 1][kChunk] = {};
+    // The vectors, in registers for all rows.
+    float pre_w[PRE ? K : 1][kChunk], post_w[POST ? K : 1][kChunk];
+    if constexpr (PRE) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+#pragma unroll
+            for (int j = 0; j < kChunk; ++j) pre_w[k][j] = 1.0f;
+            if (a.pre_w) widen<IABN_F32>(load_chunk<IABN_F32, kCached>(a.pre_w, col[k], n[k]), pre_w[k]);
+        }
+    }
+    if constexpr (POST) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+#pragma unroll
+            for (int j = 0; j < kChunk; ++j) post_w[k][j] = 1.0f;
+            if (a.post_w) widen<IABN_F32>(load_chunk<IABN_F32, kCached>(a.post_w, col[k], n[k]), post_w[k]);
+        }
+    }
+    const int64_t seg_rows = (a.split.group_rows + a.split.per_group - 1) / a.split.per_group;
+    int par = 0;  // alternates the slots of consecutive rows
+
+    for (int s = 0; s < a.split.segs; ++s) {
+        const int64_t seg = int64_t(blockIdx.x) * a.split.segs + s, group = seg / a.split.per_group;
+        if (group >= a.split.groups) break;
+        const int64_t in_group = (seg - group * a.split.per_group) * seg_rows, at = group * a.split.group_rows;
+        const int64_t lo = at + min(in_group, a.split.group_rows);
+        const int64_t hi = at + min(in_group + seg_rows, a.split.group_rows);
+        RowRegs<DT, K> next;
+        if (lo + first < hi) load_row<DT, K, POST, PRE>(a, lo + first, n, col, next);
+        for (int64_t row = lo + first; row < hi; row += kStep) {
+            RowRegs<DT, K> x = next;
+            if (row + kStep < hi) load_row<DT, K, POST, PRE>(a, row + kStep, n, col, next);
+            float g[K][kChunk];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                if (a.dr) widen<DT>(x.dr[k], g[k]);
+                else
+#pragma unroll
+                    for (int j = 0; j < kChunk; ++j) g[k][j] = 0.0f;
+            }
+            if constexpr (PRE) {
+                const float mean = a.pre_stats[row], rstd = a.pre_stats[a.R + row];
+                float hat[K][kChunk], d[K][kChunk], s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    widen<DT>(x.r[k], hat[k]);
+                    widen<DT>(x.du[k], d[k]);
+#pragma unroll
+                    for (int j = 0; j < kChunk; ++j) {
+                        hat[k][j] = j < n[k] ? (hat[k][j] - mean) * rstd : 0.0f;
+                        tw[k][j] = fmaf(d[k][j], hat[k][j], tw[k][j]);
+                        tb[k][j] += d[k][j];
+                        d[k][j] *= pre_w[k][j];
+                        s1 += d[k][j];
+                        s2 = fmaf(d[k][j], hat[k][j], s2);
+                    }
+                }
+                row_sum2<ONE_WAVE>(s1, s2, slots[par], waves);
+                s1 = a.pre == IABN_NORM_LAYER ? s1 * a.inv_c : 0.0f;
+                s2 *= a.inv_c;
+#pragma unroll
+                for (int k = 0; k < K; ++k)
+#pragma unroll
+                    for (int j = 0; j < kChunk; ++j)
+                        g[k][j] = fmaf(rstd, d[k][j] - s1 - hat[k][j] * s2, g[k][j]);
+            }
+            const int64_t base = row * a.C;
+            if (a.dx) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    float o[kChunk];
+#pragma unroll
+                    for (int j = 0; j < kChunk; ++j) o[j] = a.alpha * g[k][j];
+                    store_chunk<DT, kStream>(a.dx, base + col[k], n[k], o);
+                }
+            }
+            if constexpr (POST) {
+                float hat[K][kChunk], s1 = 0.0f, s2 = 0.0f, mean = 0.0f, rstd = 1.0f;
+                if (a.post != IABN_NORM_NONE) {
+                    mean = a.post_stats[row];
+                    rstd = a.post_stats[a.R + row];
+                }
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    if (a.h) widen<DT>(x.h[k], hat[k]);
+                    // From here g is e = beta*g*D, then dn, then dn*w.
+#pragma unroll
+                    for (int j = 0; j < kChunk; ++j) {
+                        hat[k][j] = a.h && j < n[k] ? (hat[k][j] - mean) * rstd : 0.0f;
+                        g[k][j] = j < n[k] ? a.beta * g[k][j] : 0.0f;
+                    }
+                    if (a.drop.threshold)
+                        drop_group(a.drop, static_cast<uint64_t>(row * a.chunks + col[k] / kChunk), g[k]);
+                    if (a.gate) {
+                        float gv[kChunk], o[kChunk], bv[kChunk] = {};
+                        widen<DT>(load_chunk<DT, kCached>(a.gate, row / a.gate_rows * a.C + col[k], n[k]), gv);
+                        if (a.post_b)
+                            widen<IABN_F32>(load_chunk<IABN_F32, kCached>(a.post_b, col[k], n[k]), bv);
+#pragma unroll
+                        for (int j = 0; j < kChunk; ++j) {
+                            o[j] = g[k][j] * fmaf(hat[k][j], post_w[k][j], bv[j]);
+                            sg[k][j] += o[j];
+                            g[k][j] *= gv[j];
+                        }
+                        if (a.dgate && a.gate_each_row)
+                            store_chunk<DT, kStream>(a.dgate, base + col[k], n[k], o);
+                    }
+                    if (a.post != IABN_NORM_NONE) {
+#pragma unroll
+                        for (int j = 0; j < kChunk; ++j) {
+                            sw[k][j] = fmaf(g[k][j], hat[k][j], sw[k][j]);
+                            sb[k][j] += g[k][j];
+                            g[k][j] *= post_w[k][j];
+                            s1 += g[k][j];
+                            s2 = fmaf(g[k][j], hat[k][j], s2);
+                        }
+                    }
+                }
+                if (a.post != IABN_NORM_NONE) {
+                    row_sum2<ONE_WAVE>(s1, s2, slots[2 + par], waves);
+                    s1 = a.post == IABN_NORM_LAYER ? s1 * a.inv_c : 0.0f;
+                    s2 *= a.inv_c;
+#pragma unroll
+                    for (int k = 0; k < K; ++k)
+#pragma unroll
+                        for (int j = 0; j < kChunk; ++j)
+                            g[k][j] = rstd * (g[k][j] - s1 - hat[k][j] * s2);
+                }
+                if (a.dh)
+#pragma unroll
+                    for (int k = 0; k < K; ++k) store_chunk<DT, kStream>(a.dh, base + col[k], n[k], g[k]);
+            }
+            par ^= 1;
+        }
+        if constexpr (POST) {
+            if (a.dgate && !a.gate_each_row) {
+                const int64_t out = (a.split.per_group == 1 ? group : int64_t(blockIdx.x)) * a.C;
+                flush<K, ONE_WAVE>(sg, n, col, lds, [&](int, int m, int c, float (&v)[kChunk]) {
+                    if (a.split.per_group == 1) store_chunk<DT, kStream>(a.dgate, out + c, m, v);
+                    else store_chunk<IABN_F32, kCached>(a.gpart, out + c, m, v);
+                });
+            }
+        }
+    }
+    const auto put = [&](int which) {
+        return [=](int, int m, int c, float (&v)[kChunk]) {
+            store_chunk<IABN_F32, kCached>(a.part, (int64_t(which) * a.split.blocks + blockIdx.x) * a.C + c, m, v);
+        };
+    };
+    if constexpr (POST) {
+        if (a.dpost_w) flush<K, ONE_WAVE>(sw, n, col, lds, put(0));
+        if (a.dpost_b) flush<K, ONE_WAVE>(sb, n, col, lds, put(1));
+    }
+    if constexpr (PRE) {
+        if (a.dpre_w) flush<K, ONE_WAVE>(tw, n, col, lds, put(2));
+        if (a.dpre_b) flush<K, ONE_WAVE>(tb, n, col, lds, put(3));
+    }
+}
+
+// out[c] = sum over `count` rows of part[., c], in double.  A block takes 32
+// columns; 8 of its threads share a column.
+constexpr int kSumCols = 32;
+
+template <int DT>
+__device__ __forceinline__ void column_sum(const float* __restrict__ part, int count, int C,
+                                           void* __restrict__ out) {
+    __shared__ double lds[kThreads];
+    const int c = blockIdx.x * kSumCols + threadIdx.x % kSumCols, y = threadIdx.x / kSumCols;
+    constexpr int kY = kThreads / kSumCols;
+    double s = 0.0;
+    if (c < C) {
+#pragma unroll 8
+        for (int i = y; i < count; i += kY) s += part[int64_t(i) * C + c];
+    }
+    lds[threadIdx.x] = s;
+    __syncthreads();
+    if (y == 0 && c < C) {
+        for (int i = 1; i < kY; ++i) s += lds[i * kSumCols + threadIdx.x];
+        static_cast<typename Elem<DT>::T*>(out)[c] =
+            static_cast<typename Elem<DT>::T>(static_cast<float>(s));
+    }
+}
+
+// Grid: (columns, the 4 vectors and then the gate's groups).
+template <int DT>
+__global__ __launch_bounds__(kThreads) void resnorm_bwd_sum_kernel(ResnormBwdArgs a) {
+    if (blockIdx.y < 4) {
+        float* const out = blockIdx.y == 0   ? a.dpost_w
+                           : blockIdx.y == 1 ? a.dpost_b
+                           : blockIdx.y == 2 ? a.dpre_w
+                                             : a.dpre_b;
+        if (out)
+            column_sum<IABN_F32>(a.part + int64_t(blockIdx.y) * a.split.blocks * a.C, a.split.blocks, a.C, out);
+    } else {
+        const int64_t g = blockIdx.y - 4;
+        column_sum<DT>(a.gpart + g * a.split.per_group * a.C, a.split.per_group, a.C,
+                       static_cast<typename Elem<DT>::T*>(a.dgate) + g * a.C);
+    }
+}
+
+template <int DT, bool POST, bool PRE>
+void launch_rows(const ResnormBwdArgs& a, hipStream_t st) {
+    const RowShape s = row_shape(a.chunks);
+    const dim3 grid(static_cast<uint32_t>(a.split.blocks));
+    if (s.waves == 1)
+        resnorm_bwd_kernel<DT, 1, true, POST, PRE><<<grid, kRows * kWave, 0, st>>>(a, 1);
+    else if (s.k == 1)
+        resnorm_bwd_kernel<DT, 1, false, POST, PRE><<<grid, s.waves * kWave, 0, st>>>(a, s.waves);
+    else
+        resnorm_bwd_kernel<DT, 2, false, POST, PRE><<<grid, s.waves * kWave, 0, st>>>(a, s.waves);
+}
+
+template <int DT>
+void launch(const ResnormBwdArgs& a, hipStream_t st) {
+    const bool post = a.dh || a.dgate || a.dpost_w || a.dpost_b, pre = a.du != nullptr;
+    if (post && pre) launch_rows<DT, true, true>(a, st);
+    else if (post) launch_rows<DT, true, false>(a, st);
+    else if (pre) launch_rows<DT, false, true>(a, st);
+    else launch_rows<DT, false, false>(a, st);
+    const bool gate = a.dgate && a.split.per_group > 1 && !a.gate_each_row;
+    if (a.dpost_w || a.dpost_b || a.dpre_w || a.dpre_b || gate) {
+        const dim3 grid((a.C + kSumCols - 1) / kSumCols,
+                        4 + (gate ? static_cast<uint32_t>(a.split.groups) : 0u));
+        resnorm_bwd_sum_kernel<DT><<<grid, kThreads, 0, st>>>(a);
+    }
+}
+
+}  // namespace
+
+bool launch_resnorm_bwd(int dtype, const ResnormBwdArgs& a, hipStream_t st) {
+    switch (dtype) {
+        case IABN_F32: launch<IABN_F32>(a, st); return true;
+        case IABN_F16: launch<IABN_F16>(a, st); return true;
+        case IABN_BF16: launch<IABN_BF16>(a, st); return true;
+        default: return false;
+    }
+}
+
+}  // namespace iabn_impl

@@ -1,0 +1,209 @@
+"""Python binding of libiabn's feed-forward sublayer: dropout, and the norms
+around a block.  Marshalling only, as the rest of the package (``__init__``).
+
+Tensors: rows are contiguous [..., C] in float32, float16 or bfloat16 on a HIP
+device; norms' weights, biases and statistics are contiguous float32 on the
+same device.  Calls are asynchronous on ``stream`` (default: torch's current
+stream for the tensors' device).
+"""
+
+from __future__ import annotations
+
+import ctypes
+import math
+
+import torch
+
+import paper_1712_02616_amd as _iabn
+
+# iabn_norm_t.
+NORMS = {None: 0, "none": 0, "rms": 1, "layer": 2}
+
+# The native fast path (binding.cpp): set by the package when it loads it;
+# None before the first call, and where it does not load.
+native = None
+
+
+def _fast(name, *args):
+    """Whether the native call did it (and succeeded)."""
+    if native is None:
+        if _iabn._call is not _iabn._first_call:
+            return False
+        _iabn._first_call()  # loads it
+        if native is None:
+            return False
+    rc = getattr(native, name)((_iabn._lib or _iabn.load()).table, *args)
+    if rc is NotImplemented:
+        return False
+    if rc:
+        _iabn._check("iabn_" + name, rc)
+    return True
+
+
+def _code(table, key, what):
+    try:
+        return table[key]
+    except (KeyError, TypeError):
+        raise ValueError("%s must be one of %s" % (what, [k for k in table if k])) from None
+
+
+class _Rows:
+    """Checks tensors against the first one given."""
+
+    def __init__(self):
+        self.R = None
+
+    def __call__(self, t, what, optional=False):
+        if t is None and optional:
+            return None
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("%s must be a torch.Tensor" % what)
+        if t.dim() < 1:
+            raise ValueError("%s must have at least one dim" % what)
+        if t.dtype not in _iabn.DTYPE_CODES:
+            raise ValueError("%s has unsupported dtype %s" % (what, t.dtype))
+        if not t.is_contiguous():
+            raise ValueError("%s must be contiguous" % what)
+        if t.device.type != "cuda":
+            raise ValueError("%s must be on a HIP device" % what)
+        if self.R is None:
+            self.C, self.R = t.shape[-1], math.prod(t.shape[:-1])
+            self.dtype, self.device, self.first = t.dtype, t.device, what
+            self.code = _iabn.DTYPE_CODES[t.dtype]
+        elif t.shape[-1] != self.C or t.numel() != self.R * self.C or t.dtype != self.dtype or \
+                t.device != self.device:
+            raise ValueError("%s must match %s in rows, width, dtype and device" % (what, self.first))
+        return _iabn._ptr(t)
+
+    def gate(self, t, what, groups=None):
+        if t is None:
+            return None, 0
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("%s must be a torch.Tensor" % what)
+        if t.dim() < 1 or t.shape[-1] != self.C or t.dtype != self.dtype or not t.is_contiguous() or \
+                t.device != self.device:
+            raise ValueError("%s must be contiguous [groups, %d] of %s on %s"
+                             % (what, self.C, self.dtype, self.device))
+        n = math.prod(t.shape[:-1])
+        if groups is not None and n != groups:
+            raise ValueError("%s must have the gate's %d rows" % (what, groups))
+        return _iabn._ptr(t), n
+
+    def floats(self, t, n, what):
+        if t is None:
+            return None
+        if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or not t.is_contiguous():
+            raise ValueError("%s must be a contiguous float32 tensor" % what)
+        if t.numel() != n or t.device != self.device:
+            raise ValueError("%s must hold %d values on %s" % (what, n, self.device))
+        return _iabn._ptr(t)
+
+
+def _word(v, what):
+    v = int(v)
+    if not 0 <= v < 1 << 64:
+        raise ValueError("%s must be in [0, 2^64)" % what)
+    return v
+
+
+def _workspace(need, device, workspace, stream):
+    """The caller's workspace, or a new one (see _workspace of the package)."""
+    if workspace is None:
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
+        if stream is not None:
+            if not isinstance(stream, torch.cuda.Stream):
+                stream = torch.cuda.ExternalStream(int(stream), device=device)
+            workspace.record_stream(stream)
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on %s" % device)
+    return workspace, _iabn._ptr(workspace), workspace.numel() * workspace.element_size()
+
+
+def iabn_dropout(x, y, p, seed, offset=0, stream=None):
+    """y = D(x): the dropout of (p, seed, offset), whose mask is not stored (the
+    same call on a gradient is the backward); ``y`` may be ``x``.  Returns ``y``."""
+    if stream is None and _fast("dropout", x, y, p, seed, offset):
+        return y
+    rows = _Rows()
+    xp, yp = rows(x, "x"), rows(y, "y")
+    rc = _iabn.load().iabn_dropout(xp, yp, rows.code, float(p), _word(seed, "seed"),
+                                   _word(offset, "offset"), rows.R, rows.C,
+                                   _iabn._stream(rows.device, stream))
+    _iabn._check("iabn_dropout", rc)
+    return y
+
+
+def iabn_resnorm_forward(x, h, r, u, gate=None, post_norm=None, post_weight=None, post_bias=None,
+                         pre_norm=None, pre_weight=None, pre_bias=None, post_stats=None,
+                         pre_stats=None, alpha=1.0, beta=1.0, eps=1e-5, p=0.0, seed=0, offset=0,
+                         stream=None):
+    """r = alpha*x + beta*gate*D(post(h)), u = pre(r); returns ``(r, u)``.
+
+    ``post_norm``, ``pre_norm``: None, "rms" or "layer".  ``h`` may be None (r =
+    alpha*x), ``r`` where only ``u`` is wanted, and ``u`` is None without a pre
+    norm.  ``gate``: [groups, C] of x's dtype.  ``post_stats``, ``pre_stats``:
+    [2, rows] float32, written for the backward where given."""
+    post, pre = _code(NORMS, post_norm, "post_norm"), _code(NORMS, pre_norm, "pre_norm")
+    if stream is None and _fast("resnorm_forward", x, h, r, u, gate, post, post_weight, post_bias, pre,
+                                pre_weight, pre_bias, post_stats, pre_stats, alpha, beta, eps, p,
+                                seed, offset):
+        return r, u
+    rows = _Rows()
+    tensors = [rows(x, "x")] + [rows(t, n, True) for t, n in ((h, "h"), (r, "r"), (u, "u"))]
+    C, R = rows.C, rows.R
+    gp, groups = rows.gate(gate, "gate")
+    vectors = {n: rows.floats(t, C, n) for t, n in (
+        (post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"),
+        (pre_bias, "pre_bias"))}
+    stats = [rows.floats(t, 2 * R, n) for t, n in ((post_stats, "post_stats"),
+                                                    (pre_stats, "pre_stats"))]
+    rc = _iabn.load().iabn_resnorm_forward(
+        *tensors, rows.code, gp, groups, post, vectors["post_weight"], vectors["post_bias"], pre,
+        vectors["pre_weight"], vectors["pre_bias"], *stats, float(alpha), float(beta), float(eps),
+        float(p), _word(seed, "seed"), _word(offset, "offset"), R, C,
+        _iabn._stream(rows.device, stream))
+    _iabn._check("iabn_resnorm_forward", rc)
+    return r, u
+
+
+def iabn_resnorm_workspace_size(R: int, C: int, groups: int = 0) -> int:
+    """Workspace bytes of iabn_resnorm_backward (``groups`` 0: no gate)."""
+    return int(_iabn.load().iabn_resnorm_workspace_size(int(R), int(C), int(groups)))
+
+
+def iabn_resnorm_backward(dr, du, r, h, dx, dh, gate=None, post_norm=None, post_weight=None,
+                          post_bias=None, pre_norm=None, pre_weight=None, post_stats=None,
+                          pre_stats=None, dgate=None, dpost_weight=None, dpost_bias=None,
+                          dpre_weight=None, dpre_bias=None, alpha=1.0, beta=1.0, p=0.0, seed=0,
+                          offset=0, workspace=None, stream=None):
+    """The gradients of iabn_resnorm_forward from ``dr`` and ``du``, with the
+    r, h and statistics that the forward gave; writes the outputs that are not
+    None and returns ``(dx, dh)``."""
+    post, pre = _code(NORMS, post_norm, "post_norm"), _code(NORMS, pre_norm, "pre_norm")
+    if stream is None and _fast("resnorm_backward", dr, du, r, h, dx, dh, gate, post, post_weight,
+                                post_bias, pre, pre_weight, post_stats, pre_stats, dgate,
+                                dpost_weight, dpost_bias, dpre_weight, dpre_bias, alpha, beta, p,
+                                seed, offset, workspace):
+        return dx, dh
+    rows = _Rows()
+    tensors = [rows(t, n, True) for t, n in ((dr, "dr"), (du, "du"), (r, "r"), (h, "h"), (dx, "dx"),
+                                             (dh, "dh"))]
+    if rows.R is None:
+        raise ValueError("dr and du are both None")
+    C, R = rows.C, rows.R
+    gp, groups = rows.gate(gate, "gate")
+    dgp, _ = rows.gate(dgate, "dgate", groups)
+    v = {n: rows.floats(t, C, n) for t, n in (
+        (post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"),
+        (dpost_weight, "dpost_weight"), (dpost_bias, "dpost_bias"), (dpre_weight, "dpre_weight"),
+        (dpre_bias, "dpre_bias"))}
+    stats = [rows.floats(t, 2 * R, n) for t, n in ((post_stats, "post_stats"),
+                                                    (pre_stats, "pre_stats"))]
+    ws, wp, wb = _workspace(iabn_resnorm_workspace_size(R, C, groups), rows.device, workspace, stream)
+    rc = _iabn.load().iabn_resnorm_backward(
+        *tensors, rows.code, gp, groups, post, v["post_weight"], v["post_bias"], pre, v["pre_weight"],
+        *stats, dgp, v["dpost_weight"], v["dpost_bias"], v["dpre_weight"], v["dpre_bias"],
+        float(alpha), float(beta), float(p), _word(seed, "seed"), _word(offset, "offset"), R, C, wp,
+        wb, _iabn._stream(rows.device, stream))
+    _iabn._check("iabn_resnorm_backward", rc)
+    return dx, dh
