@@ -430,6 +430,48 @@ int iabn_resnorm_backward(const void *dr, const void *du, const void *r, const v
                           float beta, float p, uint64_t seed, uint64_t offset, int64_t R,
                           int64_t C, void *workspace, size_t workspace_bytes, void *stream);
 
+/* Activations of the gated feed-forward block.  LEAKY takes slope (0: a
+ * rectifier); its derivative at 0 is 1.  GELU is the exact one, v*Phi(v). */
+typedef enum { IABN_ACT_SILU = 0, IABN_ACT_GELU = 1, IABN_ACT_LEAKY = 2 } iabn_act_t;
+
+/*
+ * A gated feed-forward block:
+ *
+ *   g = x Wg^T,  u = x Wu^T,  h = act(g)*u,  y = h Wd^T
+ *
+ * Both projections, the activation and the product are one kernel; h goes
+ * through the workspace.  Products are summed in fp32 (matrix cores); h, and
+ * the backward's dg and du, are rounded to the storage type between the
+ * products.
+ *   x, y           [M, C]; y is out and must not overlap the inputs.
+ *   w_gate, w_up   [F, C].    w_down  [C, F].
+ *   g, u           [M, F] out: the projections, which the backward takes, or
+ *                  both NULL (inference).
+ *   act, slope     an iabn_act_t; slope >= 0 and finite (LEAKY only).
+ *   M, C, F        tokens, width, hidden width; C, F <= 2^24, M < 2^31.
+ *                  C or F = 0: y is 0.
+ * The workspace holds iabn_ffn_workspace_size(M, C, F, dtype) bytes, 16-byte
+ * aligned: enough for either direction.
+ *
+ * iabn_ffn_backward: its gradients from dy, and the g, u that the forward kept.
+ *   dx             [M, C] out.   dw_gate, dw_up [F, C], dw_down [C, F] out.
+ *   dg, du         [M, F] out: the gradients of the projections.  dg may be g
+ *                  and du may be u (in place: the backward then keeps nothing
+ *                  but h besides).
+ * All outputs are overwritten; M = 0 writes zeros to the weights' gradients.
+ */
+int iabn_ffn_forward(const void *x, const void *w_gate, const void *w_up, const void *w_down,
+                     void *y, void *g, void *u, int dtype, int act, float slope, int64_t M,
+                     int64_t C, int64_t F, void *workspace, size_t workspace_bytes, void *stream);
+
+size_t iabn_ffn_workspace_size(int64_t M, int64_t C, int64_t F, int dtype);
+
+int iabn_ffn_backward(const void *dy, const void *x, const void *g, const void *u,
+                      const void *w_gate, const void *w_up, const void *w_down, void *dx, void *dg,
+                      void *du, void *dw_gate, void *dw_up, void *dw_down, int dtype, int act,
+                      float slope, int64_t M, int64_t C, int64_t F, void *workspace,
+                      size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -39,6 +39,7 @@ __all__ = [
     "iabn_ckpt_recompute", "iabn_ckpt_backward", "iabn_plan", "iabn_forward_train_noalloc",
     "DTYPE_CODES", "OPS", "NORMS",
     "iabn_dropout", "iabn_resnorm_forward", "iabn_resnorm_workspace_size", "iabn_resnorm_backward",
+    "ACTIVATIONS", "iabn_ffn_forward", "iabn_ffn_workspace_size", "iabn_ffn_backward",
 ]
 
 DTYPE_CODES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
@@ -64,7 +65,8 @@ _NATIVE = ("iabn_workspace_size", "iabn_forward_train", "iabn_forward_train_noal
            "iabn_forward_eval", "iabn_backward", "iabn_backward_ii", "iabn_std_forward_train",
            "iabn_std_backward", "iabn_ckpt_forward_train", "iabn_ckpt_recompute",
            "iabn_ckpt_backward", "iabn_dropout", "iabn_resnorm_forward",
-           "iabn_resnorm_workspace_size", "iabn_resnorm_backward")
+           "iabn_resnorm_workspace_size", "iabn_resnorm_backward", "iabn_ffn_workspace_size",
+           "iabn_ffn_forward", "iabn_ffn_backward")
 (_WORKSPACE_SIZE, _FORWARD_TRAIN, _FORWARD_TRAIN_NOALLOC, _FORWARD_EVAL, _BACKWARD, _BACKWARD_II,
  _STD_FORWARD, _STD_BACKWARD, _CKPT_FORWARD, _CKPT_RECOMPUTE, _CKPT_BACKWARD) = range(11)
 
@@ -124,6 +126,9 @@ def declare(lib):
         "iabn_resnorm_workspace_size": ([i64, i64, i64], sz),
         "iabn_resnorm_backward": ([vp, vp, vp, vp, vp, vp, i32, vp, i64, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp,
                                    vp, f32, f32, f32, u64, u64, i64, i64, vp, sz, vp], i32),
+        "iabn_ffn_workspace_size": ([i64, i64, i64, i32], sz),
+        "iabn_ffn_forward": ([vp] * 7 + [i32, i32, f32, i64, i64, i64, vp, sz, vp], i32),
+        "iabn_ffn_backward": ([vp] * 13 + [i32, i32, f32, i64, i64, i64, vp, sz, vp], i32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -513,5 +518,6 @@ def iabn_backward_apply(z, dz_dx, gamma, beta, save_var, dgamma, dbeta, eps, slo
 
 
 from . import sublayer as _sublayer  # noqa: E402
-from .sublayer import (NORMS, iabn_dropout, iabn_resnorm_backward, iabn_resnorm_forward,  # noqa: E402
-                       iabn_resnorm_workspace_size)
+from .sublayer import (ACTIVATIONS, NORMS, iabn_dropout, iabn_ffn_backward,  # noqa: E402
+                       iabn_ffn_forward, iabn_ffn_workspace_size, iabn_resnorm_backward,
+                       iabn_resnorm_forward, iabn_resnorm_workspace_size)

@@ -37,7 +37,10 @@ enum Op : long {
     kDropout = kOps,
     kResnormForward,
     kResnormWorkspaceSize,
-    kResnormBackward
+    kResnormBackward,
+    kFfnWorkspaceSize,
+    kFfnForward,
+    kFfnBackward
 };
 
 // What follows the table and the op in a call: activation tensors,
@@ -262,6 +265,25 @@ struct Args {
         n = t->numel() / C;
         return t->data_ptr();
     }
+    // A tensor of the rows' type and `n` values whose last dim is `last`.
+    void* matrix(int64_t n, int64_t last, bool optional = false) {
+        const at::Tensor* const t = tensor(optional);
+        if (t == nullptr) return nullptr;
+        if (t->dim() < 1 || t->size(t->dim() - 1) != last || t->numel() != n ||
+            dtype_code(t->scalar_type()) != code || t->device() != dev)
+            return plain = false, nullptr;
+        return t->data_ptr();
+    }
+    // A weight, [F, C]; the first one of the call says which F.
+    int64_t F = 0;
+    void* first_weight() {
+        const at::Tensor* const t = tensor(false);
+        if (t == nullptr) return nullptr;
+        if (t->dim() != 2 || t->size(1) != C || dtype_code(t->scalar_type()) != code || t->device() != dev)
+            return plain = false, nullptr;
+        F = t->size(0);
+        return t->data_ptr();
+    }
     float* floats(int64_t n) {
         const at::Tensor* const t = tensor(true);
         if (t == nullptr) return nullptr;
@@ -400,6 +422,62 @@ PyObject* resnorm_backward_checked(void* const* table, Args& a) {
     });
 }
 
+PyObject* ffn_forward_checked(void* const* table, Args& a) {
+    void* const x = a.rows();
+    void* const wg = a.first_weight();
+    void* const wu = a.matrix(a.F * a.C, a.C);
+    void* const wd = a.matrix(a.C * a.F, a.F);
+    void* const y = a.rows();
+    void* const g = a.matrix(a.R * a.F, a.F, true);
+    void* const u = a.matrix(a.R * a.F, a.F, true);
+    const int act = a.choice();
+    const float slope = a.number();
+    bool own;
+    at::Tensor ws = a.workspace(own);
+    if (!a.plain) return not_plain();
+    return without_gil([&] {
+        a.take(ws, own, entry<decltype(iabn_ffn_workspace_size)>(table, kFfnWorkspaceSize)(
+                            a.R, a.C, a.F, a.code));
+        return entry<decltype(iabn_ffn_forward)>(table, kFfnForward)(
+            x, wg, wu, wd, y, g, u, a.code, act, slope, a.R, a.C, a.F, ws.data_ptr(), bytes_of(ws),
+            a.stream());
+    });
+}
+
+PyObject* ffn_backward_checked(void* const* table, Args& a) {
+    void* const dy = a.rows();
+    void* const x = a.rows();
+    // F stands in the weights, which come after g and u.
+    PyObject* const* const at_g = a.at;
+    a.at += 2;
+    void* const wg = a.first_weight();
+    void* const wu = a.matrix(a.F * a.C, a.C);
+    void* const wd = a.matrix(a.C * a.F, a.F);
+    PyObject* const* const at_dx = a.at;
+    a.at = at_g;
+    void* const g = a.matrix(a.R * a.F, a.F);
+    void* const u = a.matrix(a.R * a.F, a.F);
+    a.at = at_dx;
+    void* const dx = a.rows();
+    void* const dg = a.matrix(a.R * a.F, a.F);
+    void* const du = a.matrix(a.R * a.F, a.F);
+    void* const dwg = a.matrix(a.F * a.C, a.C);
+    void* const dwu = a.matrix(a.F * a.C, a.C);
+    void* const dwd = a.matrix(a.C * a.F, a.F);
+    const int act = a.choice();
+    const float slope = a.number();
+    bool own;
+    at::Tensor ws = a.workspace(own);
+    if (!a.plain) return not_plain();
+    return without_gil([&] {
+        a.take(ws, own, entry<decltype(iabn_ffn_workspace_size)>(table, kFfnWorkspaceSize)(
+                            a.R, a.C, a.F, a.code));
+        return entry<decltype(iabn_ffn_backward)>(table, kFfnBackward)(
+            dy, x, g, u, wg, wu, wd, dx, dg, du, dwg, dwu, dwd, a.code, act, slope, a.R, a.C, a.F,
+            ws.data_ptr(), bytes_of(ws), a.stream());
+    });
+}
+
 // fn(table, arguments...) -> status or NotImplemented, as `call`.
 template <PyObject* (*FN)(void* const*, Args&), Py_ssize_t N>
 PyObject* sublayer(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -427,6 +505,8 @@ PyMethodDef methods[] = {
      "iabn_resnorm_forward, as call"},
     {"resnorm_backward", method<resnorm_backward_checked, 24>(), METH_FASTCALL,
      "iabn_resnorm_backward, as call"},
+    {"ffn_forward", method<ffn_forward_checked, 10>(), METH_FASTCALL, "iabn_ffn_forward, as call"},
+    {"ffn_backward", method<ffn_backward_checked, 16>(), METH_FASTCALL, "iabn_ffn_backward, as call"},
     {"call", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(call)), METH_FASTCALL,
      "call(table, op, tensors..., floats...[, workspace]) -> status or NotImplemented"},
     {nullptr, nullptr, 0, nullptr}};

@@ -5,7 +5,7 @@
 #include <cmath>
 
 #include "errors.h"
-#include "sublayer.h"
+#include "ffn.h"
 
 namespace iabn_impl {
 namespace {
@@ -82,6 +82,52 @@ ResnormSplit split_rows(int64_t R, int64_t C, int64_t groups) {
 
 size_t resnorm_workspace(const ResnormSplit& s, int64_t C) {
     return static_cast<size_t>(5) * s.blocks * C * sizeof(float);
+}
+
+// ---------------------------------------------------------------- gated feed-forward block
+
+constexpr int64_t kMaxFfnWidth = int64_t(1) << 24;
+constexpr int64_t kMaxFfnRows = (int64_t(1) << 31) - 1;
+
+int elem_bytes(int dtype) { return dtype == IABN_F32 ? 4 : 2; }
+
+int check_ffn(int dtype, int act, float slope, int64_t M, int64_t C, int64_t F) {
+    if (!valid_dtype(dtype)) return fail(IABN_ERR_DTYPE, "unknown dtype %d", dtype);
+    if (M < 0 || C < 0 || F < 0)
+        return fail(IABN_ERR_SHAPE, "negative size M=%lld C=%lld F=%lld", (long long)M, (long long)C,
+                    (long long)F);
+    if (M > kMaxFfnRows || C > kMaxFfnWidth || F > kMaxFfnWidth)
+        return fail(IABN_ERR_SHAPE, "M=%lld, C=%lld or F=%lld is too large", (long long)M,
+                    (long long)C, (long long)F);
+    if (act != IABN_ACT_SILU && act != IABN_ACT_GELU && act != IABN_ACT_LEAKY)
+        return fail(IABN_ERR_PARAM, "unknown activation %d", act);
+    if (act == IABN_ACT_LEAKY && !(slope >= 0.0f && std::isfinite(slope)))
+        return fail(IABN_ERR_PARAM, "slope=%g must be >= 0 and finite", slope);
+    return IABN_OK;
+}
+
+// h, [M, F].
+size_t ffn_workspace(int64_t M, int64_t F, int dtype) {
+    const size_t h = static_cast<size_t>(M) * F * elem_bytes(dtype);
+    return (h + 255) / 256 * 256;
+}
+
+int check_workspace(void* workspace, size_t bytes, size_t need) {
+    if (need == 0) return IABN_OK;
+    if (!workspace) return fail(IABN_ERR_NULL, "workspace is NULL");
+    if (bytes < need)
+        return fail(IABN_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", bytes, need);
+    if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0)
+        return fail(IABN_ERR_WORKSPACE, "workspace is not 16-byte aligned");
+    return IABN_OK;
+}
+
+void gemm(int dtype, GemmKind kind, const GemmArgs& a, int products, hipStream_t st) {
+    switch (dtype) {
+        case IABN_F32: launch_gemm<IABN_F32>(kind, a, products, st); break;
+        case IABN_F16: launch_gemm<IABN_F16>(kind, a, products, st); break;
+        default: launch_gemm<IABN_BF16>(kind, a, products, st); break;
+    }
 }
 
 bool finite(float v) { return std::isfinite(v); }
@@ -180,20 +226,12 @@ int iabn_resnorm_backward(const void* dr, const void* du, const void* r, const v
         if (dh && dh == dx) return fail(IABN_ERR_PARAM, "dx and dh are one buffer");
     }
     a.split = split_rows(R, C, gate ? groups : 0);
-    const size_t need = resnorm_workspace(a.split, C);
-    if (need > 0) {
-        if (!workspace) return fail(IABN_ERR_NULL, "workspace is NULL");
-        if (workspace_bytes < need)
-            return fail(IABN_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
-        if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0)
-            return fail(IABN_ERR_WORKSPACE, "workspace is not 16-byte aligned");
-    }
-    const int eb = dtype == IABN_F32 ? 4 : 2;
+    if ((rc = check_workspace(workspace, workspace_bytes, resnorm_workspace(a.split, C)))) return rc;
     if (R == 0) {
         float* const vectors[] = {dpost_weight, dpost_bias, dpre_weight, dpre_bias};
         for (float* v : vectors)
             if (v) launch_zero(v, C * 4, st);
-        if (dgate) launch_zero(dgate, groups * C * eb, st);
+        if (dgate) launch_zero(dgate, groups * C * elem_bytes(dtype), st);
         return launched("resnorm_backward");
     }
     a.dr = dr, a.du = du, a.r = r, a.h = h, a.dx = dx, a.dh = dh, a.gate = gate, a.dgate = dgate;
@@ -212,6 +250,93 @@ int iabn_resnorm_backward(const void* dr, const void* du, const void* r, const v
     a.gpart = a.part + static_cast<size_t>(4) * a.split.blocks * C;
     launch_resnorm_bwd(dtype, a, st);
     return launched("resnorm_backward");
+}
+
+size_t iabn_ffn_workspace_size(int64_t M, int64_t C, int64_t F, int dtype) {
+    if (check_ffn(dtype, IABN_ACT_SILU, 0.0f, M, C, F) != IABN_OK) return 0;
+    return ffn_workspace(M, F, dtype);
+}
+
+int iabn_ffn_forward(const void* x, const void* w_gate, const void* w_up, const void* w_down,
+                     void* y, void* g, void* u, int dtype, int act, float slope, int64_t M,
+                     int64_t C, int64_t F, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_ffn(dtype, act, slope, M, C, F);
+    if (rc) return rc;
+    if ((g == nullptr) != (u == nullptr)) return fail(IABN_ERR_NULL, "one of g and u is NULL");
+    if (M == 0) return ok();
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const int eb = elem_bytes(dtype);
+    if (C == 0 || F == 0) {
+        if (C > 0 && !y) return fail(IABN_ERR_NULL, "y is NULL");
+        launch_zero(y, M * C * eb, st);
+        if (g) launch_zero(g, M * F * eb, st);
+        if (u) launch_zero(u, M * F * eb, st);
+        return launched("ffn_forward");
+    }
+    if (!x || !w_gate || !w_up || !w_down || !y)
+        return fail(IABN_ERR_NULL, "x, y or a weight is NULL");
+    if ((rc = check_workspace(workspace, workspace_bytes, ffn_workspace(M, F, dtype)))) return rc;
+    GemmArgs up = {};
+    up.x = {{x, x}, C}, up.y = {{w_gate, w_up}, C};
+    up.M = M, up.N = F, up.K = C;
+    up.out[0] = workspace, up.dg = g, up.du = u;
+    up.act = act, up.slope = slope;
+    gemm(dtype, kGemmUp, up, 1, st);
+    GemmArgs down = {};
+    down.x = {{workspace, workspace}, F}, down.y = {{w_down, w_down}, F};
+    down.M = M, down.N = C, down.K = F;
+    down.out[0] = y;
+    gemm(dtype, kGemmDown, down, 1, st);
+    return launched("ffn_forward");
+}
+
+int iabn_ffn_backward(const void* dy, const void* x, const void* g, const void* u,
+                      const void* w_gate, const void* w_up, const void* w_down, void* dx, void* dg,
+                      void* du, void* dw_gate, void* dw_up, void* dw_down, int dtype, int act,
+                      float slope, int64_t M, int64_t C, int64_t F, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+    int rc = check_ffn(dtype, act, slope, M, C, F);
+    if (rc) return rc;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const int eb = elem_bytes(dtype);
+    if (M == 0 || C == 0 || F == 0) {
+        // Sums over nothing: no tokens, or no width on one side.
+        if ((M * C > 0 && !dx) || (M * F > 0 && (!dg || !du)) ||
+            (C * F > 0 && (!dw_gate || !dw_up || !dw_down)))
+            return fail(IABN_ERR_NULL, "an output is NULL");
+        launch_zero(dx, M * C * eb, st);
+        launch_zero(dg, M * F * eb, st);
+        launch_zero(du, M * F * eb, st);
+        for (void* w : {dw_gate, dw_up, dw_down}) launch_zero(w, C * F * eb, st);
+        return launched("ffn_backward");
+    }
+    if (!dy || !x || !g || !u || !w_gate || !w_up || !w_down)
+        return fail(IABN_ERR_NULL, "dy, x, g, u or a weight is NULL");
+    if (!dx || !dg || !du || !dw_gate || !dw_up || !dw_down)
+        return fail(IABN_ERR_NULL, "an output is NULL");
+    if ((rc = check_workspace(workspace, workspace_bytes, ffn_workspace(M, F, dtype)))) return rc;
+    GemmArgs dh = {};
+    dh.x = {{dy, dy}, C}, dh.y = {{w_down, w_down}, F};
+    dh.M = M, dh.N = F, dh.K = C;
+    dh.out[0] = workspace, dh.g = g, dh.u = u, dh.dg = dg, dh.du = du;
+    dh.act = act, dh.slope = slope;
+    gemm(dtype, kGemmDh, dh, 1, st);
+    GemmArgs dwd = {};
+    dwd.x = {{dy, dy}, C}, dwd.y = {{workspace, workspace}, F};
+    dwd.M = C, dwd.N = F, dwd.K = M;
+    dwd.out[0] = dw_down;
+    gemm(dtype, kGemmDw, dwd, 1, st);
+    GemmArgs dwp = {};
+    dwp.x = {{dg, du}, F}, dwp.y = {{x, x}, C};
+    dwp.M = F, dwp.N = C, dwp.K = M;
+    dwp.out[0] = dw_gate, dwp.out[1] = dw_up;
+    gemm(dtype, kGemmDw, dwp, 2, st);
+    GemmArgs dxp = {};
+    dxp.x = {{dg, du}, F}, dxp.y = {{w_gate, w_up}, C};
+    dxp.M = M, dxp.N = C, dxp.K = F;
+    dxp.out[0] = dx;
+    gemm(dtype, kGemmDx, dxp, 1, st);
+    return launched("ffn_backward");
 }
 
 }  // extern "C"

@@ -1,0 +1,64 @@
+// The gated feed-forward block's kernels: what the host side hands to them.
+//
+//   g = x Wg^T, u = x Wu^T, h = act(g)*u, y = h Wd^T       (x [M, C], W* as stored:
+//   dh = dy Wd, dg = dh*u*act'(g), du = dh*act(g)           Wg, Wu [F, C], Wd [C, F])
+//   dWd = dy^T h, dWg = dg^T x, dWu = du^T x, dx = dg Wg + du Wu
+#pragma once
+
+#include "sublayer.h"
+
+namespace iabn_impl {
+
+// out[m][n] = sum over k of X[m][k]*Y[n][k], an operand stored with k
+// contiguous (rows m or n of ld elements) or strided (rows k of ld elements).
+struct Operand {
+    // Two matrices of one shape: the gate's and the up projection's.  See GemmKind.
+    const void* p[2];
+    int64_t ld;
+};
+
+// The products of the block.
+enum GemmKind {
+    kGemmUp,       // y: Wg and Wu side by side, k contiguous; out h, and g, u where kept
+    kGemmDown,     // out y: both k contiguous
+    kGemmDh,       // Wd k-strided; out dg, du, h from g, u
+    kGemmDx,       // Wg, Wu k-strided; the sum of two products
+    kGemmDw,       // both k-strided; two products (blockIdx.z) of x[z] and y[z] or one
+};
+
+struct GemmArgs {
+    Operand x, y;
+    int64_t M, N, K;
+    void* out[2];
+    // kGemmUp: h -> out[0], g, u (may be null).  kGemmDh: g, u -> dg, du, out[0] = h.
+    const void *g, *u;
+    void *dg, *du;
+    int act;
+    float slope;
+};
+
+// act(v) and its derivative.
+__device__ __forceinline__ void activate(int act, float slope, float v, float& a, float& da) {
+    if (act == IABN_ACT_SILU) {
+        const float s = 1.0f / (1.0f + expf(-v));
+        a = v * s;
+        da = s * (1.0f + v * (1.0f - s));
+    } else if (act == IABN_ACT_GELU) {
+        const float c = 0.5f * (1.0f + erff(v * 0.70710678118654752f));
+        a = v * c;
+        da = c + v * expf(-0.5f * v * v) * 0.39894228040143268f;
+    } else {
+        a = v >= 0.0f ? v : slope * v;
+        da = v >= 0.0f ? 1.0f : slope;
+    }
+}
+
+// products: 2 for kGemmDw of both projections, else 1.
+template <int DT>
+bool launch_gemm(GemmKind kind, const GemmArgs& a, int products, hipStream_t st);
+
+extern template bool launch_gemm<IABN_F32>(GemmKind, const GemmArgs&, int, hipStream_t);
+extern template bool launch_gemm<IABN_F16>(GemmKind, const GemmArgs&, int, hipStream_t);
+extern template bool launch_gemm<IABN_BF16>(GemmKind, const GemmArgs&, int, hipStream_t);
+
+}  // namespace iabn_impl

@@ -1,8 +1,8 @@
-"""Python binding of libiabn's feed-forward sublayer: dropout, and the norms
-around a block.  Marshalling only, as the rest of the package (``__init__``).
+"""Python binding of libiabn's feed-forward sublayer: dropout, the norms
+around a block, and the gated feed-forward block.  Marshalling only, as the rest of the package (``__init__``).
 
 Tensors: rows are contiguous [..., C] in float32, float16 or bfloat16 on a HIP
-device; norms' weights, biases and statistics are contiguous float32 on the
+device, weights contiguous matrices of the same type; norms' weights, biases and statistics are contiguous float32 on the
 same device.  Calls are asynchronous on ``stream`` (default: torch's current
 stream for the tensors' device).
 """
@@ -18,6 +18,9 @@ import paper_1712_02616_amd as _iabn
 
 # iabn_norm_t.
 NORMS = {None: 0, "none": 0, "rms": 1, "layer": 2}
+
+# iabn_act_t.
+ACTIVATIONS = {"silu": 0, "gelu": 1, "leaky": 2}
 
 # The native fast path (binding.cpp): set by the package when it loads it;
 # None before the first call, and where it does not load.
@@ -88,6 +91,26 @@ class _Rows:
         if groups is not None and n != groups:
             raise ValueError("%s must have the gate's %d rows" % (what, groups))
         return _iabn._ptr(t), n
+
+    def matrix(self, t, rows, cols, what, optional=False):
+        if t is None and optional:
+            return None
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("%s must be a torch.Tensor" % what)
+        if t.dim() < 1 or t.shape[-1] != cols or t.numel() != rows * cols or t.dtype != self.dtype or \
+                not t.is_contiguous() or t.device != self.device:
+            raise ValueError("%s must be contiguous [%d, %d] of %s on %s"
+                             % (what, rows, cols, self.dtype, self.device))
+        return _iabn._ptr(t)
+
+    def weights(self, w_gate, w_up, w_down):
+        if not isinstance(w_gate, torch.Tensor):
+            raise TypeError("w_gate must be a torch.Tensor")
+        if w_gate.dim() != 2:
+            raise ValueError("w_gate must be [F, C]")
+        self.F = w_gate.shape[0]
+        return [self.matrix(w_gate, self.F, self.C, "w_gate"), self.matrix(w_up, self.F, self.C, "w_up"),
+                self.matrix(w_down, self.C, self.F, "w_down")]
 
     def floats(self, t, n, what):
         if t is None:
@@ -207,3 +230,56 @@ def iabn_resnorm_backward(dr, du, r, h, dx, dh, gate=None, post_norm=None, post_
         wb, _iabn._stream(rows.device, stream))
     _iabn._check("iabn_resnorm_backward", rc)
     return dx, dh
+
+
+def iabn_ffn_workspace_size(M: int, C: int, F: int, dtype) -> int:
+    """Workspace bytes of iabn_ffn_forward and iabn_ffn_backward; ``dtype`` is a
+    torch dtype or a dtype code."""
+    code = _iabn.DTYPE_CODES[dtype] if isinstance(dtype, torch.dtype) else int(dtype)
+    return int(_iabn.load().iabn_ffn_workspace_size(int(M), int(C), int(F), code))
+
+
+def iabn_ffn_forward(x, w_gate, w_up, w_down, y, g=None, u=None, act="silu", slope=0.01,
+                     workspace=None, stream=None):
+    """y = (act(x w_gate^T) * (x w_up^T)) w_down^T; returns ``y``.
+
+    ``w_gate``, ``w_up``: [F, C], ``w_down``: [C, F].  ``g``, ``u``: [..., F], the
+    two projections, written for the backward where given.  ``act``: "silu",
+    "gelu" or "leaky" (``slope``)."""
+    code = _code(ACTIVATIONS, act, "act")
+    if stream is None and _fast("ffn_forward", x, w_gate, w_up, w_down, y, g, u, code, slope, workspace):
+        return y
+    rows = _Rows()
+    xp = rows(x, "x")
+    weights = rows.weights(w_gate, w_up, w_down)
+    R, C, F = rows.R, rows.C, rows.F
+    yp = rows(y, "y")
+    gp, up = rows.matrix(g, R, F, "g", True), rows.matrix(u, R, F, "u", True)
+    ws, wp, wb = _workspace(iabn_ffn_workspace_size(R, C, F, rows.code), rows.device, workspace, stream)
+    rc = _iabn.load().iabn_ffn_forward(xp, *weights, yp, gp, up, rows.code, code, float(slope), R, C, F,
+                                       wp, wb, _iabn._stream(rows.device, stream))
+    _iabn._check("iabn_ffn_forward", rc)
+    return y
+
+
+def iabn_ffn_backward(dy, x, g, u, w_gate, w_up, w_down, dx, dg, du, dw_gate, dw_up, dw_down,
+                      act="silu", slope=0.01, workspace=None, stream=None):
+    """The gradients of iabn_ffn_forward from ``dy`` and the ``g``, ``u`` that it
+    gave; ``dg`` may be ``g`` and ``du`` may be ``u``.  Returns ``dx``."""
+    code = _code(ACTIVATIONS, act, "act")
+    if stream is None and _fast("ffn_backward", dy, x, g, u, w_gate, w_up, w_down, dx, dg, du, dw_gate,
+                                dw_up, dw_down, code, slope, workspace):
+        return dx
+    rows = _Rows()
+    dyp, xp = rows(dy, "dy"), rows(x, "x")
+    weights = rows.weights(w_gate, w_up, w_down)
+    R, C, F = rows.R, rows.C, rows.F
+    kept = [rows.matrix(t, R, F, n) for t, n in ((g, "g"), (u, "u"))]
+    outs = [rows(dx, "dx")] + [rows.matrix(t, a, b, n) for t, a, b, n in (
+        (dg, R, F, "dg"), (du, R, F, "du"), (dw_gate, F, C, "dw_gate"), (dw_up, F, C, "dw_up"),
+        (dw_down, C, F, "dw_down"))]
+    ws, wp, wb = _workspace(iabn_ffn_workspace_size(R, C, F, rows.code), rows.device, workspace, stream)
+    rc = _iabn.load().iabn_ffn_backward(dyp, xp, *kept, *weights, *outs, rows.code, code, float(slope),
+                                        R, C, F, wp, wb, _iabn._stream(rows.device, stream))
+    _iabn._check("iabn_ffn_backward", rc)
+    return dx

@@ -115,3 +115,40 @@ def test_python_refuses():
         iabn.iabn_resnorm_forward(x, x, x, x, post_norm="batch")
     with pytest.raises(ValueError, match="both None"):
         iabn.iabn_resnorm_backward(None, None, None, None, None, None)
+
+
+def ffn_forward(lib, **kw):
+    a = dict(x=P, wg=P, wu=P, wd=P, y=P, g=P, u=P, dtype=F16, act=0, slope=0.0, M=4, C=16, F=24, ws=P,
+             ws_bytes=1 << 30)
+    a.update(kw)
+    return lib.iabn_ffn_forward(*a.values(), None)
+
+
+def ffn_backward(lib, **kw):
+    a = dict(dy=P, x=P, g=P, u=P, wg=P, wu=P, wd=P, dx=P, dg=P, du=P, dwg=P, dwu=P, dwd=P, dtype=F16, act=0,
+             slope=0.0, M=4, C=16, F=24, ws=P, ws_bytes=1 << 30)
+    a.update(kw)
+    return lib.iabn_ffn_backward(*a.values(), None)
+
+
+@no_gpu
+def test_ffn_refuses(lib):
+    need = lib.iabn_ffn_workspace_size(4, 16, 24, F16)
+    assert need >= 4 * 24 * 2
+    both = ((ERR_DTYPE, dict(dtype=3)), (ERR_SHAPE, dict(M=-1)), (ERR_SHAPE, dict(C=(1 << 24) + 1)),
+            (ERR_SHAPE, dict(F=-8)), (ERR_SHAPE, dict(M=1 << 31)), (ERR_PARAM, dict(act=3)),
+            (ERR_PARAM, dict(act=2, slope=-0.1)), (ERR_PARAM, dict(act=2, slope=NAN)),
+            (ERR_NULL, dict(ws=None)), (ERR_WORKSPACE, dict(ws_bytes=need - 1)),
+            (ERR_WORKSPACE, dict(ws=ctypes.c_void_p(4096 + 8))))
+    for status, kw in both:
+        refused(lib, status, ffn_forward(lib, **kw))
+        refused(lib, status, ffn_backward(lib, **kw))
+    for k in ("x", "wg", "wu", "wd", "y"):
+        refused(lib, ERR_NULL, ffn_forward(lib, **{k: None}))
+    refused(lib, ERR_NULL, ffn_forward(lib, g=None))
+    refused(lib, ERR_NULL, ffn_forward(lib, u=None))
+    for k in ("dy", "x", "g", "u", "wg", "wu", "wd", "dx", "dg", "du", "dwg", "dwu", "dwd"):
+        refused(lib, ERR_NULL, ffn_backward(lib, **{k: None}))
+    refused(lib, ERR_NULL, ffn_backward(lib, M=0, dwg=None))
+    assert ffn_forward(lib, M=0, x=None, y=None, ws=None) == OK
+    assert lib.iabn_ffn_workspace_size(-1, 16, 24, F16) == 0 and lib.iabn_ffn_workspace_size(4, 16, 24, 9) == 0
