@@ -38,12 +38,13 @@ struct GemmArgs {
 };
 
 // act(v) and its derivative.
-__device__ __forceinline__ void activate(int act, float slope, float v, float& a, float& da) {
-    if (act == IABN_ACT_SILU) {
+template <int ACT>
+__device__ __forceinline__ void activate(float slope, float v, float& a, float& da) {
+    if constexpr (ACT == IABN_ACT_SILU) {
         const float s = 1.0f / (1.0f + expf(-v));
         a = v * s;
         da = s * (1.0f + v * (1.0f - s));
-    } else if (act == IABN_ACT_GELU) {
+    } else if constexpr (ACT == IABN_ACT_GELU) {
         const float c = 0.5f * (1.0f + erff(v * 0.70710678118654752f));
         a = v * c;
         da = c + v * expf(-0.5f * v * v) * 0.39894228040143268f;
@@ -51,6 +52,48 @@ __device__ __forceinline__ void activate(int act, float slope, float v, float& a
         a = v >= 0.0f ? v : slope * v;
         da = v >= 0.0f ? 1.0f : slope;
     }
+}
+
+template <int ACT, int N>
+__device__ __forceinline__ void gate_forward_as(float slope, const float (&g)[N], const float (&u)[N],
+                                                float (&h)[N]) {
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        float v, d;
+        activate<ACT>(slope, g[q], v, d);
+        h[q] = v * u[q];
+    }
+}
+
+template <int N>
+__device__ __forceinline__ void gate_forward(int act, float slope, const float (&g)[N],
+                                             const float (&u)[N], float (&h)[N]) {
+    if (act == IABN_ACT_SILU) gate_forward_as<IABN_ACT_SILU>(slope, g, u, h);
+    else if (act == IABN_ACT_GELU) gate_forward_as<IABN_ACT_GELU>(slope, g, u, h);
+    else gate_forward_as<IABN_ACT_LEAKY>(slope, g, u, h);
+}
+
+template <int ACT, int N>
+__device__ __forceinline__ void gate_backward_as(float slope, const float (&dh)[N], const float (&g)[N],
+                                                 const float (&u)[N], float (&dg)[N], float (&du)[N],
+                                                 float (&h)[N]) {
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        float v, d;
+        activate<ACT>(slope, g[q], v, d);
+        dg[q] = dh[q] * u[q] * d;
+        du[q] = dh[q] * v;
+        h[q] = v * u[q];
+    }
+}
+
+template <int N>
+__device__ __forceinline__ void gate_backward(int act, float slope, const float (&dh)[N],
+                                              const float (&g)[N], const float (&u)[N], float (&dg)[N],
+                                              float (&du)[N], float (&h)[N]) {
+    if (act == IABN_ACT_SILU) gate_backward_as<IABN_ACT_SILU>(slope, dh, g, u, dg, du, h);
+    else if (act == IABN_ACT_GELU) gate_backward_as<IABN_ACT_GELU>(slope, dh, g, u, dg, du, h);
+    else gate_backward_as<IABN_ACT_LEAKY>(slope, dh, g, u, dg, du, h);
 }
 
 // products: 2 for kGemmDw of both projections, else 1.

@@ -1,5 +1,9 @@
 // The block's matrix products on the matrix cores: tiles of TM x TN outputs,
-// K in steps of 128 bytes per row, both operands staged through LDS.
+// K in steps of 128 bytes per row, both operands staged through two LDS
+// buffers: while the waves multiply out of one, the next step's tiles arrive
+// in the other.  Operands whose rows are whole 16-byte accesses go straight
+// from memory to LDS (DMA); others, and a last step that K does not fill, go
+// through registers, which hold zeros for what is not there.
 //
 // A block's waves each own WM x WN outputs in 16x16 accumulators (fp32).  The
 // operand with the n index (the weights, mostly) takes the first place of the
@@ -70,14 +74,16 @@ __device__ __forceinline__ u32x4 load16(const typename Elem<DT>::T* p, int64_t n
     return __builtin_bit_cast(u32x4, v);
 }
 
-// One operand's tile of ROWS x 128 bytes of K: from memory to registers, to
-// LDS, and fragments from there.  KS: k strided in memory (and in LDS, where
-// the transposing read turns it).
+// One operand's tile of ROWS x 128 bytes of K: from memory to LDS, and
+// fragments from there.  KS: k strided in memory (and in LDS, where the
+// transposing read turns it).
 //
-// LDS, k contiguous: a row's eight 16-byte chunks are permuted by the row, so
-// that the 16 rows that one read takes fall on all 64 banks.  k strided: a
-// row is one k; 32-byte chunks (fp32: 64) are permuted so that the k that one
-// read takes fall on different banks.
+// The tile's 16-byte chunks lie in LDS in the order of the threads that bring
+// them, THREADS chunks at a time; which chunk of the line a thread brings is
+// permuted.  k contiguous: a line is a row, its eight chunks are permuted by
+// the row, so that the 16 rows that one read takes fall on all 64 banks.  k
+// strided: a line is one k; 32-byte pairs of chunks (fp32: 64-byte fours) are
+// permuted so that the k that one read takes fall on different banks.
 template <int DT, bool KS, int ROWS, int THREADS, bool DUAL>
 struct Stage {
     using T = typename Elem<DT>::T;
@@ -85,49 +91,87 @@ struct Stage {
     static constexpr int BK = kRowBytes / sizeof(T);
     static constexpr int kBytes = ROWS * kRowBytes;
     static constexpr int kLoads = kBytes / 16 / THREADS;
-    static constexpr int kPerRow = KS ? ROWS / E : 8;  // 16-byte chunks of a row of memory
+    static constexpr int kPerLine = KS ? ROWS / E : 8;  // chunks
     static_assert(kLoads * 16 * THREADS == kBytes, "a tile is whole accesses");
+    // A thread's chunks stand at one place of lines that are this far apart.
+    static constexpr int kLineStep = THREADS / kPerLine;
+    static_assert(THREADS % kPerLine == 0, "");
 
-    u32x4 r[kLoads];
-
-    static __device__ __forceinline__ uint32_t swizzle(int k) {
-        return DT == IABN_F32 ? (k >> 2) & 3 : ((k >> 1) & 4) | (k & 3);
+    static __device__ __forceinline__ uint32_t swizzle(int line) {
+        if constexpr (!KS) return (line >> 1) & 7;
+        else return DT == IABN_F32 ? (line >> 2) & 3 : ((line >> 1) & 4) | (line & 3);
+    }
+    static __device__ __forceinline__ int first_line() { return threadIdx.x / kPerLine; }
+    // The chunk of its i-th line that this thread brings (the same one of each
+    // where the permutation does not tell lines that are a step apart).
+    static __device__ __forceinline__ int chunk(int i) {
+        constexpr int kGroup = !KS ? 1 : DT == IABN_F32 ? 4 : 2;
+        const int line = first_line() + (kLineStep % 16 == 0 ? 0 : i * kLineStep);
+        return static_cast<int>((threadIdx.x % kPerLine) ^ (swizzle(line) * kGroup));
+    }
+    // The matrix and the row in it of a line (k contiguous).
+    static __device__ __forceinline__ int row_of(int line) {
+        return DUAL ? line / kSpan * (kSpan / 2) + line % (kSpan / 2) : line;
+    }
+    static __device__ __forceinline__ int matrix_of(int line, int seg) {
+        return DUAL ? line % kSpan / (kSpan / 2) : seg;
     }
 
-    // rows: how many of the operand's rows there are from row0 on.
+    // Through registers.  rows: how many of the operand's rows there are from
+    // row0 on.
+    u32x4 r[kLoads];
     __device__ __forceinline__ void load(const Operand& o, int seg, int64_t row0, int64_t rows,
                                          int64_t k0, int64_t K) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int idx = threadIdx.x + i * THREADS, line = idx / kPerRow, c = idx % kPerRow;
+            const int line = first_line() + i * kLineStep, c = chunk(i) * E;
+            const T* p = static_cast<const T*>(o.p[KS ? seg : matrix_of(line, seg)]);
+            if constexpr (KS)
+                r[i] = load16<DT>(p + (k0 + line) * o.ld + row0 + c, k0 + line < K ? rows - c : 0);
+            else
+                r[i] = load16<DT>(p + (row0 + row_of(line)) * o.ld + k0 + c,
+                                  row_of(line) < rows ? K - k0 - c : 0);
+        }
+    }
+    __device__ __forceinline__ void store(char* lds) const {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            *reinterpret_cast<u32x4*>(lds + (threadIdx.x + i * THREADS) * 16) = r[i];
+    }
+
+    // Straight to LDS, a whole step of K.  Rows past the operand's read its
+    // last ones (the results that they go into are not stored).
+    uint32_t off[kLoads];  // bytes from the step's first element
+    __device__ __forceinline__ void prepare(const Operand& o, int64_t rows) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int line = first_line() + i * kLineStep, c = chunk(i) * E;
             if constexpr (KS) {
-                const T* p = static_cast<const T*>(o.p[seg]) + (k0 + line) * o.ld + row0 + c * E;
-                r[i] = load16<DT>(p, k0 + line < K ? rows - c * E : 0);
+                off[i] = static_cast<uint32_t>((line * o.ld + (c < rows ? c : 0)) * sizeof(T));
             } else {
-                int row = line;
-                if constexpr (DUAL) {
-                    seg = line % kSpan / (kSpan / 2);
-                    row = line / kSpan * (kSpan / 2) + line % (kSpan / 2);
-                }
-                const T* p = static_cast<const T*>(o.p[seg]) + (row0 + row) * o.ld + k0 + c * E;
-                r[i] = load16<DT>(p, row < rows ? K - k0 - c * E : 0);
+                const int64_t row = min(static_cast<int64_t>(row_of(line)), rows - 1);
+                off[i] = static_cast<uint32_t>((row * o.ld + c) * sizeof(T));
             }
         }
     }
-
-    __device__ __forceinline__ void store(char* lds) const {
+    __device__ __forceinline__ void fetch(const Operand& o, int seg, int64_t row0, int64_t k0,
+                                          char* lds) const {
+#if defined(__HIP_DEVICE_COMPILE__)  // (the host's pass does not know the buffer types)
+        typedef __attribute__((address_space(3))) void lds_t;
+        const int64_t at = KS ? k0 * o.ld + row0 : row0 * o.ld + k0;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int idx = threadIdx.x + i * THREADS, line = idx / kPerRow, c = idx % kPerRow;
-            uint32_t at;
-            if constexpr (!KS)
-                at = line * kRowBytes + ((c ^ ((line >> 1) & 7)) << 4);
-            else if constexpr (DT == IABN_F32)
-                at = line * ROWS * 4 + (((c >> 2) ^ swizzle(line)) << 6) + ((c & 3) << 4);
-            else
-                at = line * ROWS * 2 + (((c >> 1) ^ swizzle(line)) << 5) + ((c & 1) << 4);
-            *reinterpret_cast<u32x4*>(lds + at) = r[i];
+            // (A wave's lines are of one matrix: a wave covers 8 lines or fewer.)
+            const int which =
+                DUAL ? __builtin_amdgcn_readfirstlane(matrix_of(first_line() + i * kLineStep, seg)) : seg;
+            const T* base = static_cast<const T*>(which ? o.p[1] : o.p[0]) + at;
+            const __amdgpu_buffer_rsrc_t rsrc =
+                __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, 0xffffffff, 0x00027000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                rsrc, (lds_t*)(lds + (wave * kWave + i * THREADS) * 16), 16, off[i], 0, 0, 0);
         }
+#endif
     }
 
     // The fragment of rows row..row+15 for step s.
@@ -136,7 +180,7 @@ struct Stage {
         if constexpr (!KS) {
             const int line = row + i;
             return *reinterpret_cast<const u32x4*>(
-                lds + line * kRowBytes + (((s * 4 + g) ^ ((line >> 1) & 7)) << 4));
+                lds + line * kRowBytes + (((s * 4 + g) ^ swizzle(line)) << 4));
         } else if constexpr (DT == IABN_F32) {
             f32x4 v;
 #pragma unroll
@@ -164,40 +208,6 @@ struct Stage {
     }
 };
 
-// 4 consecutive elements, of which n are inside.
-template <int DT>
-__device__ __forceinline__ void store4(void* base, int64_t at, int64_t n, const f32x4& v) {
-    using T = typename Elem<DT>::T;
-    typedef T vec __attribute__((ext_vector_type(4)));
-    typedef T mem __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-    T* p = static_cast<T*>(base) + at;
-    const vec w = __builtin_convertvector(v, vec);
-    if (n >= 4) {
-        *reinterpret_cast<mem*>(p) = w;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j < n) p[j] = w[j];
-    }
-}
-
-template <int DT>
-__device__ __forceinline__ f32x4 load4(const void* base, int64_t at, int64_t n) {
-    using T = typename Elem<DT>::T;
-    typedef T vec __attribute__((ext_vector_type(4)));
-    typedef T mem __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-    const T* p = static_cast<const T*>(base) + at;
-    vec v = {};
-    if (n >= 4) {
-        v = *reinterpret_cast<const mem*>(p);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j < n) v[j] = p[j];
-    }
-    return __builtin_convertvector(v, f32x4);
-}
-
 template <int KIND>
 struct KindOf {
     static constexpr bool kDual = KIND == kGemmUp;
@@ -206,7 +216,21 @@ struct KindOf {
     static constexpr int kSegs = KIND == kGemmDx ? 2 : 1;  // products that add up
 };
 
-template <int DT, int KIND, int TM, int TN, int WAVES_M, int WAVES_N>
+// The tile of a block.  The hardware hands consecutive blocks to the XCDs in
+// turn; each XCD takes a contiguous range of tiles, in strips of kStrip tiles
+// of m, so that the tiles that run on it at one time share rows of both
+// operands in its L2.
+constexpr int kStrip = 8;
+__device__ __forceinline__ void tile_of(int tiles_m, int tiles_n, int& tm, int& tn) {
+    const uint32_t n = gridDim.x, x = blockIdx.x % kXcds, j = blockIdx.x / kXcds;
+    const uint32_t t = x * (n / kXcds) + min(x, n % kXcds) + j;
+    const uint32_t strip = t / (kStrip * tiles_n), in = t - strip * (kStrip * tiles_n);
+    const uint32_t height = min(static_cast<uint32_t>(kStrip), tiles_m - strip * kStrip);
+    tn = static_cast<int>(in / height);
+    tm = static_cast<int>(strip * kStrip + in % height);
+}
+
+template <int DT, int KIND, int TM, int TN, int WAVES_M, int WAVES_N, bool DMA>
 __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs a, int tiles_m,
                                                                         int tiles_n) {
     using Kind = KindOf<KIND>;
@@ -216,34 +240,21 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
     using SX = Stage<DT, Kind::kXStrided, TM, kT, false>;
     using SY = Stage<DT, Kind::kYStrided, TN, kT, Kind::kDual>;
     constexpr int BK = SX::BK;
-    __shared__ __align__(16) char lds[2][SX::kBytes + SY::kBytes];
+    __shared__ __align__(16) char lds0[SX::kBytes + SY::kBytes];
+    __shared__ __align__(16) char lds1[SX::kBytes + SY::kBytes];
 
-    const int tile = blockIdx.x;
-    const int64_t m0 = int64_t(tile % tiles_m) * TM;
+    int tm, tn;
+    tile_of(tiles_m, tiles_n, tm, tn);
+    const int64_t m0 = int64_t(tm) * TM;
     constexpr int kCols = Kind::kDual ? TN / 2 : TN;  // columns of the output
-    const int64_t n0 = int64_t(tile / tiles_m) * kCols;
+    const int64_t n0 = int64_t(tn) * kCols;
     const int z = blockIdx.z;
     const int wave = threadIdx.x / kWave, wm = wave / WAVES_N * WM, wn = wave % WAVES_N * WN;
 
     f32x4 acc[NM][NN] = {};
     SX sx;
     SY sy;
-    const int64_t per_seg = (a.K + BK - 1) / BK, tiles_k = per_seg * Kind::kSegs;
-    const auto load = [&](int64_t kt) {
-        const int seg = Kind::kSegs > 1 ? (kt >= per_seg ? 1 : 0) : z;
-        const int64_t k0 = (Kind::kSegs > 1 && seg ? kt - per_seg : kt) * BK;
-        sx.load(a.x, seg, m0, a.M - m0, k0, a.K);
-        sy.load(a.y, seg, n0, a.N - n0, k0, a.K);
-    };
-    if (tiles_k > 0) {
-        load(0);
-        sx.store(lds[0]);
-        sy.store(lds[0] + SX::kBytes);
-    }
-    __syncthreads();
-    for (int64_t kt = 0; kt < tiles_k; ++kt) {
-        const char* const cur = lds[kt & 1];
-        if (kt + 1 < tiles_k) load(kt + 1);
+    const auto multiply = [&](const char* __restrict__ cur) {
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             u32x4 fy[NN];
@@ -256,82 +267,168 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
                 for (int j = 0; j < NN; ++j) acc[i][j] = Mma<DT>::run(fy[j], fx, acc[i][j]);
             }
         }
-        if (kt + 1 < tiles_k) {
-            char* const next = lds[(kt + 1) & 1];
-            sx.store(next);
-            sy.store(next + SX::kBytes);
+    };
+    // Steps of K that go straight to LDS: whole ones, those of the first
+    // product and then those of the second.
+    const int whole = DMA ? static_cast<int>(a.K / BK) : 0, steps = whole * Kind::kSegs;
+    if constexpr (DMA) {
+        const auto fetch = [&](int kt, char* buf) {
+            const int seg = Kind::kSegs > 1 ? (kt >= whole ? 1 : 0) : z;
+            const int64_t k0 = int64_t(Kind::kSegs > 1 && seg ? kt - whole : kt) * BK;
+            sx.fetch(a.x, seg, m0, k0, buf);
+            sy.fetch(a.y, seg, n0, k0, buf + SX::kBytes);
+        };
+        sx.prepare(a.x, a.M - m0);
+        sy.prepare(a.y, a.N - n0);
+        // What a wave has fetched is in LDS when its own loads are done: each
+        // waits for its own before the barrier that all meet at.
+        const auto arrive = [&] {
+            __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+            __syncthreads();
+        };
+        if (steps > 0) fetch(0, lds0);
+        arrive();
+        // The buffers are told apart (restrict), so that reading one does not
+        // wait for what arrives in the other.
+        const auto both = [&](int kt, const char* __restrict__ cur, char* __restrict__ next) {
+            if (kt + 1 < steps) fetch(kt + 1, next);
+            multiply(cur);
+        };
+        for (int kt = 0; kt < steps; kt += 2) {
+            both(kt, lds0, lds1);
+            arrive();
+            if (kt + 1 >= steps) break;
+            both(kt + 1, lds1, lds0);
+            arrive();
         }
-        __syncthreads();
+    }
+    // The others through registers.
+    const int64_t per_seg = (a.K + BK - 1) / BK - whole, rest = per_seg * Kind::kSegs;
+    if (rest > 0) {
+        const auto load = [&](int64_t kt) {
+            const int seg = Kind::kSegs > 1 ? (kt >= per_seg ? 1 : 0) : z;
+            const int64_t k0 = (whole + (Kind::kSegs > 1 && seg ? kt - per_seg : kt)) * BK;
+            sx.load(a.x, seg, m0, a.M - m0, k0, a.K);
+            sy.load(a.y, seg, n0, a.N - n0, k0, a.K);
+        };
+        const auto store = [&](char* buf) {
+            sx.store(buf);
+            sy.store(buf + SX::kBytes);
+            __syncthreads();
+        };
+        load(0);
+        store(lds0);
+        for (int64_t kt = 0; kt < rest; kt += 2) {
+            if (kt + 1 < rest) load(kt + 1);
+            multiply(lds0);
+            if (kt + 1 >= rest) break;
+            store(lds1);
+            if (kt + 2 < rest) load(kt + 2);
+            multiply(lds1);
+            if (kt + 2 < rest) store(lds0);
+        }
     }
 
-    // A lane holds row m and 4 consecutive n of every accumulator.
-    const int lm = lane_id() & 15, ln = (lane_id() >> 4) * 4;
+    // The results, through LDS: a lane holds a row and 4 consecutive columns of
+    // each accumulator; it gets chunks of 8 columns, which it finishes and
+    // stores as one access, 128 bytes of a row by 8 lanes.  Each wave has
+    // kPass rows of 16 accumulators at a time in its own part.
+    __syncthreads();
+    constexpr int kPass = NM < 4 ? NM : 4, kPart = kPass * 16 * WN;
+    static_assert(WAVES_M * WAVES_N * kPart * 4 <= 2 * (SX::kBytes + SY::kBytes) && NM % kPass == 0 && WN == 64, "");
+    constexpr int kHalf = WAVES_M * WAVES_N / 2;
+    float* const part = reinterpret_cast<float*>(wave < kHalf ? lds0 : lds1) + (wave % kHalf) * kPart;
+    const auto at = [](int row, int col) {  // 16-byte units permuted by the row
+        return row * WN + (((col >> 2) ^ (row & 15)) << 2);
+    };
 #pragma unroll
-    for (int i = 0; i < NM; ++i) {
-        const int64_t m = m0 + wm + i * 16 + lm;
-        if (m >= a.M) continue;
-        if constexpr (KIND == kGemmUp) {
+    for (int p = 0; p < NM; p += kPass) {
+        const int lm = lane_id() & 15, ln = (lane_id() >> 4) * 4;
 #pragma unroll
-            for (int j = 0; j < NN / 2; ++j) {
-                const int64_t n = n0 + wn / 2 + j * 16 + ln, left = a.N - n, at = m * a.N + n;
-                if (left <= 0) continue;
-                const f32x4 g = acc[i][j], u = acc[i][j + NN / 2];
-                f32x4 h;
+        for (int i = 0; i < kPass; ++i)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float v, d;
-                    activate(a.act, a.slope, g[q], v, d);
-                    h[q] = v * u[q];
-                }
-                store4<DT>(a.out[0], at, left, h);
+            for (int j = 0; j < NN; ++j)
+                *reinterpret_cast<f32x4*>(part + at(i * 16 + lm, j * 16 + ln)) = acc[p + i][j];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const auto read = [&](int row, int col, float (&v)[kChunk]) {
+            const f32x4 lo = *reinterpret_cast<const f32x4*>(part + at(row, col));
+            const f32x4 hi = *reinterpret_cast<const f32x4*>(part + at(row, col + 4));
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = lo[q], v[q + 4] = hi[q];
+        };
+        constexpr int kCh = (Kind::kDual ? WN / 2 : WN) / kChunk;  // chunks of a row
+#pragma unroll 1
+        for (int c = lane_id(); c < kPass * 16 * kCh; c += kWave) {
+            const int row = c / kCh, col = c % kCh * kChunk;
+            const int64_t m = m0 + wm + p * 16 + row;
+            const int64_t n = n0 + (Kind::kDual ? wn / 2 : wn) + col, left = a.N - n, to = m * a.N + n;
+            if (m >= a.M || left <= 0) continue;
+            const int inside = static_cast<int>(min(left, int64_t(kChunk)));
+            float v[kChunk];
+            read(row, col, v);
+            if constexpr (KIND == kGemmUp) {
+                float u[kChunk], h[kChunk];
+                read(row, col + WN / 2, u);
+                gate_forward(a.act, a.slope, v, u, h);
+                store_chunk<DT, kCached>(a.out[0], to, inside, h);
                 if (a.dg) {
-                    store4<DT>(a.dg, at, left, g);
-                    store4<DT>(a.du, at, left, u);
+                    store_chunk<DT, kStream>(a.dg, to, inside, v);
+                    store_chunk<DT, kStream>(a.du, to, inside, u);
                 }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < NN; ++j) {
-                const int64_t n = n0 + wn + j * 16 + ln, left = a.N - n, at = m * a.N + n;
-                if (left <= 0) continue;
-                if constexpr (KIND == kGemmDh) {
-                    const f32x4 g = load4<DT>(a.g, at, left), u = load4<DT>(a.u, at, left);
-                    f32x4 dg, du, h;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        float v, d;
-                        activate(a.act, a.slope, g[q], v, d);
-                        dg[q] = acc[i][j][q] * u[q] * d;
-                        du[q] = acc[i][j][q] * v;
-                        h[q] = v * u[q];
-                    }
-                    store4<DT>(a.dg, at, left, dg);
-                    store4<DT>(a.du, at, left, du);
-                    store4<DT>(a.out[0], at, left, h);
-                } else {
-                    store4<DT>(a.out[z], at, left, acc[i][j]);
-                }
+            } else if constexpr (KIND == kGemmDh) {
+                float g[kChunk], u[kChunk], dg[kChunk], du[kChunk], h[kChunk];
+                widen<DT>(load_chunk<DT, kStream>(a.g, to, inside), g);
+                widen<DT>(load_chunk<DT, kStream>(a.u, to, inside), u);
+                gate_backward(a.act, a.slope, v, g, u, dg, du, h);
+                store_chunk<DT, kCached>(a.dg, to, inside, dg);
+                store_chunk<DT, kCached>(a.du, to, inside, du);
+                store_chunk<DT, kCached>(a.out[0], to, inside, h);
+            } else {
+                store_chunk<DT, kCached>(z ? a.out[1] : a.out[0], to, inside, v);
             }
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
-template <int DT, int KIND, int TM, int TN, int WAVES_M, int WAVES_N>
+template <int DT, int KIND, int TM, int TN, int WAVES_M, int WAVES_N, bool DMA>
 void launch_tiles(const GemmArgs& a, int products, hipStream_t st) {
     constexpr int kCols = KindOf<KIND>::kDual ? TN / 2 : TN;
     const int64_t tm = (a.M + TM - 1) / TM, tn = (a.N + kCols - 1) / kCols;
-    gemm_kernel<DT, KIND, TM, TN, WAVES_M, WAVES_N>
+    gemm_kernel<DT, KIND, TM, TN, WAVES_M, WAVES_N, DMA>
         <<<dim3(static_cast<uint32_t>(tm * tn), 1, products), WAVES_M * WAVES_N * kWave, 0, st>>>(
             a, static_cast<int>(tm), static_cast<int>(tn));
 }
 
+// Whether an operand's tiles can go straight to LDS: every chunk of 16 bytes
+// is whole and aligned, and a tile's offsets fit 31 bits.
+template <int DT>
+bool whole_chunks(const Operand& o, bool strided, int64_t rows, int64_t K) {
+    constexpr int64_t es = sizeof(typename Elem<DT>::T), E = 16 / es;
+    if ((strided ? rows : K) % E != 0 || o.ld % E != 0 || o.ld * es * 256 >= int64_t(1) << 31) return false;
+    for (const void* p : o.p)
+        if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return false;
+    return true;
+}
+
 // Tiles of 256x256 where there are enough of them for every CU, else of 128x128.
-template <int DT, int KIND>
+template <int DT, int KIND, bool DMA>
 void launch_kind(const GemmArgs& a, int products, hipStream_t st) {
     constexpr int kCols = KindOf<KIND>::kDual ? 128 : 256;
     const int64_t big = (a.M + 255) / 256 * ((a.N + kCols - 1) / kCols) * products;
-    if (big >= 192) launch_tiles<DT, KIND, 256, 256, 2, 4>(a, products, st);
-    else launch_tiles<DT, KIND, 128, 128, 2, 2>(a, products, st);
+    if (big >= 192) launch_tiles<DT, KIND, 256, 256, 2, 4, DMA>(a, products, st);
+    else launch_tiles<DT, KIND, 128, 128, 2, 2, DMA>(a, products, st);
+}
+
+template <int DT, int KIND>
+void launch_kind(const GemmArgs& a, int products, hipStream_t st) {
+    if (whole_chunks<DT>(a.x, KindOf<KIND>::kXStrided, a.M, a.K) &&
+        whole_chunks<DT>(a.y, KindOf<KIND>::kYStrided, a.N, a.K))
+        launch_kind<DT, KIND, true>(a, products, st);
+    else
+        launch_kind<DT, KIND, false>(a, products, st);
 }
 
 template <int DT>
