@@ -106,10 +106,24 @@ int check_ffn(int dtype, int act, float slope, int64_t M, int64_t C, int64_t F) 
     return IABN_OK;
 }
 
-// h, [M, F].
-size_t ffn_workspace(int64_t M, int64_t F, int dtype) {
-    const size_t h = static_cast<size_t>(M) * F * elem_bytes(dtype);
-    return (h + 255) / 256 * 256;
+// A product of the block as the entry points ask for it, and what it needs
+// of the workspace: its sums, where the sum over k is split.
+size_t part_bytes(int dtype, GemmKind kind, int64_t M, int64_t N, int64_t K, int products) {
+    const int splits = gemm_splits(dtype, kind, M, N, K, products);
+    return splits > 1 ? static_cast<size_t>(splits) * products * M * N * sizeof(float) : 0;
+}
+
+// h, [M, F], and then the largest of the products' sums.
+size_t h_bytes(int64_t M, int64_t F, int dtype) {
+    return (static_cast<size_t>(M) * F * elem_bytes(dtype) + 255) / 256 * 256;
+}
+
+size_t ffn_workspace(int64_t M, int64_t C, int64_t F, int dtype) {
+    size_t part = 0;
+    for (size_t p : {part_bytes(dtype, kGemmDown, M, C, F, 1), part_bytes(dtype, kGemmDx, M, C, 2 * F, 1),
+                     part_bytes(dtype, kGemmDw, C, F, M, 1), part_bytes(dtype, kGemmDw, F, C, M, 2)})
+        part = part < p ? p : part;
+    return h_bytes(M, F, dtype) + part;
 }
 
 int check_workspace(void* workspace, size_t bytes, size_t need) {
@@ -122,12 +136,25 @@ int check_workspace(void* workspace, size_t bytes, size_t need) {
     return IABN_OK;
 }
 
-void gemm(int dtype, GemmKind kind, const GemmArgs& a, int products, hipStream_t st) {
-    switch (dtype) {
-        case IABN_F32: launch_gemm<IABN_F32>(kind, a, products, st); break;
-        case IABN_F16: launch_gemm<IABN_F16>(kind, a, products, st); break;
-        default: launch_gemm<IABN_BF16>(kind, a, products, st); break;
+void gemm(int dtype, GemmKind kind, GemmArgs a, int products, void* workspace, int64_t M, int64_t F,
+          hipStream_t st) {
+    const int64_t terms = kind == kGemmDx ? 2 * a.K : a.K;
+    a.splits = gemm_splits(dtype, kind, a.M, a.N, terms, products);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + h_bytes(M, F, dtype));
+    if (few_rows(kind, a.M)) {
+        switch (dtype) {
+            case IABN_F32: launch_few<IABN_F32>(kind, a, st); break;
+            case IABN_F16: launch_few<IABN_F16>(kind, a, st); break;
+            default: launch_few<IABN_BF16>(kind, a, st); break;
+        }
+    } else {
+        switch (dtype) {
+            case IABN_F32: launch_gemm<IABN_F32>(kind, a, products, st); break;
+            case IABN_F16: launch_gemm<IABN_F16>(kind, a, products, st); break;
+            default: launch_gemm<IABN_BF16>(kind, a, products, st); break;
+        }
     }
+    if (a.splits > 1) launch_join(dtype, a, products, st);
 }
 
 bool finite(float v) { return std::isfinite(v); }
@@ -254,7 +281,7 @@ int iabn_resnorm_backward(const void* dr, const void* du, const void* r, const v
 
 size_t iabn_ffn_workspace_size(int64_t M, int64_t C, int64_t F, int dtype) {
     if (check_ffn(dtype, IABN_ACT_SILU, 0.0f, M, C, F) != IABN_OK) return 0;
-    return ffn_workspace(M, F, dtype);
+    return ffn_workspace(M, C, F, dtype);
 }
 
 int iabn_ffn_forward(const void* x, const void* w_gate, const void* w_up, const void* w_down,
@@ -275,18 +302,18 @@ int iabn_ffn_forward(const void* x, const void* w_gate, const void* w_up, const 
     }
     if (!x || !w_gate || !w_up || !w_down || !y)
         return fail(IABN_ERR_NULL, "x, y or a weight is NULL");
-    if ((rc = check_workspace(workspace, workspace_bytes, ffn_workspace(M, F, dtype)))) return rc;
+    if ((rc = check_workspace(workspace, workspace_bytes, ffn_workspace(M, C, F, dtype)))) return rc;
     GemmArgs up = {};
     up.x = {{x, x}, C}, up.y = {{w_gate, w_up}, C};
     up.M = M, up.N = F, up.K = C;
     up.out[0] = workspace, up.dg = g, up.du = u;
     up.act = act, up.slope = slope;
-    gemm(dtype, kGemmUp, up, 1, st);
+    gemm(dtype, kGemmUp, up, 1, workspace, M, F, st);
     GemmArgs down = {};
     down.x = {{workspace, workspace}, F}, down.y = {{w_down, w_down}, F};
     down.M = M, down.N = C, down.K = F;
     down.out[0] = y;
-    gemm(dtype, kGemmDown, down, 1, st);
+    gemm(dtype, kGemmDown, down, 1, workspace, M, F, st);
     return launched("ffn_forward");
 }
 
@@ -314,28 +341,28 @@ int iabn_ffn_backward(const void* dy, const void* x, const void* g, const void* 
         return fail(IABN_ERR_NULL, "dy, x, g, u or a weight is NULL");
     if (!dx || !dg || !du || !dw_gate || !dw_up || !dw_down)
         return fail(IABN_ERR_NULL, "an output is NULL");
-    if ((rc = check_workspace(workspace, workspace_bytes, ffn_workspace(M, F, dtype)))) return rc;
+    if ((rc = check_workspace(workspace, workspace_bytes, ffn_workspace(M, C, F, dtype)))) return rc;
     GemmArgs dh = {};
     dh.x = {{dy, dy}, C}, dh.y = {{w_down, w_down}, F};
     dh.M = M, dh.N = F, dh.K = C;
     dh.out[0] = workspace, dh.g = g, dh.u = u, dh.dg = dg, dh.du = du;
     dh.act = act, dh.slope = slope;
-    gemm(dtype, kGemmDh, dh, 1, st);
+    gemm(dtype, kGemmDh, dh, 1, workspace, M, F, st);
     GemmArgs dwd = {};
     dwd.x = {{dy, dy}, C}, dwd.y = {{workspace, workspace}, F};
     dwd.M = C, dwd.N = F, dwd.K = M;
     dwd.out[0] = dw_down;
-    gemm(dtype, kGemmDw, dwd, 1, st);
+    gemm(dtype, kGemmDw, dwd, 1, workspace, M, F, st);
     GemmArgs dwp = {};
     dwp.x = {{dg, du}, F}, dwp.y = {{x, x}, C};
     dwp.M = F, dwp.N = C, dwp.K = M;
     dwp.out[0] = dw_gate, dwp.out[1] = dw_up;
-    gemm(dtype, kGemmDw, dwp, 2, st);
+    gemm(dtype, kGemmDw, dwp, 2, workspace, M, F, st);
     GemmArgs dxp = {};
     dxp.x = {{dg, du}, F}, dxp.y = {{w_gate, w_up}, C};
     dxp.M = M, dxp.N = C, dxp.K = F;
     dxp.out[0] = dx;
-    gemm(dtype, kGemmDx, dxp, 1, st);
+    gemm(dtype, kGemmDx, dxp, 1, workspace, M, F, st);
     return launched("ffn_backward");
 }
 

@@ -35,7 +35,21 @@ struct GemmArgs {
     void *dg, *du;
     int act;
     float slope;
+    // Where the sum over k is split over blocks: their fp32 sums, [splits]
+    // [products][M][N], which launch_join adds up in this order.
+    int splits;
+    float* part;
 };
+
+// The split of a product's sum over k; 1 where it has enough tiles by itself.
+// `kind` as launch_gemm and launch_few take it.
+int gemm_splits(int dtype, GemmKind kind, int64_t M, int64_t N, int64_t K, int products);
+
+// Largest sum of fp32 values that a product of the block leaves in `part`.
+constexpr int kMaxSplits = 16;
+
+// out[z][m][n] = sum over the splits, rounded once.
+void launch_join(int dtype, const GemmArgs& a, int products, hipStream_t st);
 
 // act(v) and its derivative.
 template <int ACT>
@@ -96,9 +110,26 @@ __device__ __forceinline__ void gate_backward(int act, float slope, const float 
     else gate_backward_as<IABN_ACT_LEAKY>(slope, dh, g, u, dg, du, h);
 }
 
+// The products kGemmUp and kGemmDown of at most kFewRows tokens (ffn_few.h).
+constexpr int kFewRows = 64;
+inline bool few_rows(GemmKind kind, int64_t M) {
+    return M <= kFewRows && (kind == kGemmUp || kind == kGemmDown);
+}
+template <int DT>
+bool launch_few(GemmKind kind, const GemmArgs& a, hipStream_t st);
+
+extern template bool launch_few<IABN_F32>(GemmKind, const GemmArgs&, hipStream_t);
+extern template bool launch_few<IABN_F16>(GemmKind, const GemmArgs&, hipStream_t);
+extern template bool launch_few<IABN_BF16>(GemmKind, const GemmArgs&, hipStream_t);
+
 // products: 2 for kGemmDw of both projections, else 1.
 template <int DT>
 bool launch_gemm(GemmKind kind, const GemmArgs& a, int products, hipStream_t st);
+
+// A product's tiles: of 256x256 (kGemmUp: of 128 columns of each projection),
+// 128x128 or 64x128 outputs.
+enum TileSize { kTile256, kTile128, kTile64 };
+TileSize gemm_tile(int dtype, GemmKind kind, int64_t M, int64_t N, int products);
 
 extern template bool launch_gemm<IABN_F32>(GemmKind, const GemmArgs&, int, hipStream_t);
 extern template bool launch_gemm<IABN_F16>(GemmKind, const GemmArgs&, int, hipStream_t);

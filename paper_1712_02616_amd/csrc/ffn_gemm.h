@@ -9,70 +9,18 @@
 // operand with the n index (the weights, mostly) takes the first place of the
 // matrix instruction, so that a lane's 4 results are consecutive in n, which
 // is how every output is stored.
-//
-// The fragment of an instruction is 16 bytes per lane whatever the type: 8
-// 16-bit elements, one 16x16x32 instruction; or 4 fp32, four 16x16x4
-// instructions, whose k indices are those that the lanes hold (any order of
-// the sum over k will do, the same for both operands).
 #pragma once
 
 #include "ffn.h"
+#include "mma.h"
 
 namespace iabn_impl {
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-template <int DT>
-struct Mma;
-template <>
-struct Mma<IABN_BF16> {
-    typedef __bf16 frag __attribute__((ext_vector_type(8)));
-    static __device__ __forceinline__ f32x4 run(u32x4 a, u32x4 b, f32x4 c) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(frag, a),
-                                                       __builtin_bit_cast(frag, b), c, 0, 0, 0);
-    }
-};
-template <>
-struct Mma<IABN_F16> {
-    typedef _Float16 frag __attribute__((ext_vector_type(8)));
-    static __device__ __forceinline__ f32x4 run(u32x4 a, u32x4 b, f32x4 c) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(frag, a),
-                                                      __builtin_bit_cast(frag, b), c, 0, 0, 0);
-    }
-};
-template <>
-struct Mma<IABN_F32> {
-    static __device__ __forceinline__ f32x4 run(u32x4 a, u32x4 b, f32x4 c) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(f32x4, a)[j],
-                                                     __builtin_bit_cast(f32x4, b)[j], c, 0, 0, 0);
-        return c;
-    }
-};
 
 constexpr int kRowBytes = 128;  // of K per LDS row (k contiguous)
 constexpr int kSteps = 2;       // fragments of 64 bytes of K in it
 // kGemmUp's tile: a wave's span of n holds the gate's columns in its first
 // half and the same columns of the up projection in its second.
 constexpr int kSpan = 64;
-
-// 16 bytes of consecutive elements at element alignment; those past the
-// first n are zero and not read.
-template <int DT>
-__device__ __forceinline__ u32x4 load16(const typename Elem<DT>::T* p, int64_t n) {
-    using T = typename Elem<DT>::T;
-    constexpr int E = 16 / sizeof(T);
-    typedef T vec __attribute__((ext_vector_type(E)));
-    typedef T mem __attribute__((ext_vector_type(E), aligned(sizeof(T))));
-    if (n >= E) return __builtin_bit_cast(u32x4, static_cast<vec>(*reinterpret_cast<const mem*>(p)));
-    vec v = {};
-#pragma unroll
-    for (int j = 0; j < E; ++j)
-        if (j < n) v[j] = p[j];
-    return __builtin_bit_cast(u32x4, v);
-}
 
 // One operand's tile of ROWS x 128 bytes of K: from memory to LDS, and
 // fragments from there.  KS: k strided in memory (and in LDS, where the
@@ -99,7 +47,10 @@ struct Stage {
 
     static __device__ __forceinline__ uint32_t swizzle(int line) {
         if constexpr (!KS) return (line >> 1) & 7;
-        else return DT == IABN_F32 ? (line >> 2) & 3 : ((line >> 1) & 4) | (line & 3);
+        else if constexpr (DT == IABN_F32) return (line >> 2) & 3;
+        // (Lines of 64 elements are half a round of the banks.)
+        else if constexpr (ROWS == 64) return ((line >> 2) & 2) | ((line >> 1) & 1);
+        else return ((line >> 1) & 4) | (line & 3);
     }
     static __device__ __forceinline__ int first_line() { return threadIdx.x / kPerLine; }
     // The chunk of its i-th line that this thread brings (the same one of each
@@ -127,9 +78,9 @@ struct Stage {
             const int line = first_line() + i * kLineStep, c = chunk(i) * E;
             const T* p = static_cast<const T*>(o.p[KS ? seg : matrix_of(line, seg)]);
             if constexpr (KS)
-                r[i] = load16<DT>(p + (k0 + line) * o.ld + row0 + c, k0 + line < K ? rows - c : 0);
+                r[i] = load16_first<DT>(p + (k0 + line) * o.ld + row0 + c, k0 + line < K ? rows - c : 0);
             else
-                r[i] = load16<DT>(p + (row0 + row_of(line)) * o.ld + k0 + c,
+                r[i] = load16_first<DT>(p + (row0 + row_of(line)) * o.ld + k0 + c,
                                   row_of(line) < rows ? K - k0 - c : 0);
         }
     }
@@ -268,9 +219,16 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
             }
         }
     };
-    // Steps of K that go straight to LDS: whole ones, those of the first
-    // product and then those of the second.
+    // Steps of K: whole ones that go straight to LDS, those of the first
+    // product and then those of the second, and the others, through
+    // registers.  This block's share of them all: [lo, hi) and [from, to).
     const int whole = DMA ? static_cast<int>(a.K / BK) : 0, steps = whole * Kind::kSegs;
+    const int per_seg = static_cast<int>((a.K + BK - 1) / BK) - whole, rest = per_seg * Kind::kSegs;
+    const int64_t all = steps + rest;
+    const int begin = static_cast<int>(all * blockIdx.y / gridDim.y);
+    const int end = static_cast<int>(all * (blockIdx.y + 1) / gridDim.y);
+    const int lo = min(begin, steps), hi = min(end, steps);
+    const int from = max(begin - steps, 0), to = max(end - steps, 0);
     if constexpr (DMA) {
         const auto fetch = [&](int kt, char* buf) {
             const int seg = Kind::kSegs > 1 ? (kt >= whole ? 1 : 0) : z;
@@ -286,28 +244,26 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
             __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
             __syncthreads();
         };
-        if (steps > 0) fetch(0, lds0);
+        if (lo < hi) fetch(lo, lds0);
         arrive();
         // The buffers are told apart (restrict), so that reading one does not
         // wait for what arrives in the other.
         const auto both = [&](int kt, const char* __restrict__ cur, char* __restrict__ next) {
-            if (kt + 1 < steps) fetch(kt + 1, next);
+            if (kt + 1 < hi) fetch(kt + 1, next);
             multiply(cur);
         };
-        for (int kt = 0; kt < steps; kt += 2) {
+        for (int kt = lo; kt < hi; kt += 2) {
             both(kt, lds0, lds1);
             arrive();
-            if (kt + 1 >= steps) break;
+            if (kt + 1 >= hi) break;
             both(kt + 1, lds1, lds0);
             arrive();
         }
     }
-    // The others through registers.
-    const int64_t per_seg = (a.K + BK - 1) / BK - whole, rest = per_seg * Kind::kSegs;
-    if (rest > 0) {
-        const auto load = [&](int64_t kt) {
+    if (from < to) {
+        const auto load = [&](int kt) {
             const int seg = Kind::kSegs > 1 ? (kt >= per_seg ? 1 : 0) : z;
-            const int64_t k0 = (whole + (Kind::kSegs > 1 && seg ? kt - per_seg : kt)) * BK;
+            const int64_t k0 = int64_t(whole + (Kind::kSegs > 1 && seg ? kt - per_seg : kt)) * BK;
             sx.load(a.x, seg, m0, a.M - m0, k0, a.K);
             sy.load(a.y, seg, n0, a.N - n0, k0, a.K);
         };
@@ -316,16 +272,16 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
             sy.store(buf + SX::kBytes);
             __syncthreads();
         };
-        load(0);
+        load(from);
         store(lds0);
-        for (int64_t kt = 0; kt < rest; kt += 2) {
-            if (kt + 1 < rest) load(kt + 1);
+        for (int kt = from; kt < to; kt += 2) {
+            if (kt + 1 < to) load(kt + 1);
             multiply(lds0);
-            if (kt + 1 >= rest) break;
+            if (kt + 1 >= to) break;
             store(lds1);
-            if (kt + 2 < rest) load(kt + 2);
+            if (kt + 2 < to) load(kt + 2);
             multiply(lds1);
-            if (kt + 2 < rest) store(lds0);
+            if (kt + 2 < to) store(lds0);
         }
     }
 
@@ -362,7 +318,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
         for (int c = lane_id(); c < kPass * 16 * kCh; c += kWave) {
             const int row = c / kCh, col = c % kCh * kChunk;
             const int64_t m = m0 + wm + p * 16 + row;
-            const int64_t n = n0 + (Kind::kDual ? wn / 2 : wn) + col, left = a.N - n, to = m * a.N + n;
+            const int64_t n = n0 + (Kind::kDual ? wn / 2 : wn) + col, left = a.N - n, at_out = m * a.N + n;
             if (m >= a.M || left <= 0) continue;
             const int inside = static_cast<int>(min(left, int64_t(kChunk)));
             float v[kChunk];
@@ -371,21 +327,25 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
                 float u[kChunk], h[kChunk];
                 read(row, col + WN / 2, u);
                 gate_forward(a.act, a.slope, v, u, h);
-                store_chunk<DT, kCached>(a.out[0], to, inside, h);
+                store_chunk<DT, kCached>(a.out[0], at_out, inside, h);
                 if (a.dg) {
-                    store_chunk<DT, kStream>(a.dg, to, inside, v);
-                    store_chunk<DT, kStream>(a.du, to, inside, u);
+                    store_chunk<DT, kStream>(a.dg, at_out, inside, v);
+                    store_chunk<DT, kStream>(a.du, at_out, inside, u);
                 }
             } else if constexpr (KIND == kGemmDh) {
                 float g[kChunk], u[kChunk], dg[kChunk], du[kChunk], h[kChunk];
-                widen<DT>(load_chunk<DT, kStream>(a.g, to, inside), g);
-                widen<DT>(load_chunk<DT, kStream>(a.u, to, inside), u);
+                widen<DT>(load_chunk<DT, kStream>(a.g, at_out, inside), g);
+                widen<DT>(load_chunk<DT, kStream>(a.u, at_out, inside), u);
                 gate_backward(a.act, a.slope, v, g, u, dg, du, h);
-                store_chunk<DT, kCached>(a.dg, to, inside, dg);
-                store_chunk<DT, kCached>(a.du, to, inside, du);
-                store_chunk<DT, kCached>(a.out[0], to, inside, h);
+                store_chunk<DT, kCached>(a.dg, at_out, inside, dg);
+                store_chunk<DT, kCached>(a.du, at_out, inside, du);
+                store_chunk<DT, kCached>(a.out[0], at_out, inside, h);
             } else {
-                store_chunk<DT, kCached>(z ? a.out[1] : a.out[0], to, inside, v);
+                if (gridDim.y > 1)
+                    store_chunk<IABN_F32, kCached>(
+                        a.part, (int64_t(blockIdx.y) * gridDim.z + z) * a.M * a.N + at_out, inside, v);
+                else
+                    store_chunk<DT, kCached>(z ? a.out[1] : a.out[0], at_out, inside, v);
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -398,7 +358,7 @@ void launch_tiles(const GemmArgs& a, int products, hipStream_t st) {
     constexpr int kCols = KindOf<KIND>::kDual ? TN / 2 : TN;
     const int64_t tm = (a.M + TM - 1) / TM, tn = (a.N + kCols - 1) / kCols;
     gemm_kernel<DT, KIND, TM, TN, WAVES_M, WAVES_N, DMA>
-        <<<dim3(static_cast<uint32_t>(tm * tn), 1, products), WAVES_M * WAVES_N * kWave, 0, st>>>(
+        <<<dim3(static_cast<uint32_t>(tm * tn), a.splits, products), WAVES_M * WAVES_N * kWave, 0, st>>>(
             a, static_cast<int>(tm), static_cast<int>(tn));
 }
 
@@ -413,22 +373,27 @@ bool whole_chunks(const Operand& o, bool strided, int64_t rows, int64_t K) {
     return true;
 }
 
-// Tiles of 256x256 where there are enough of them for every CU, else of 128x128.
 template <int DT, int KIND, bool DMA>
-void launch_kind(const GemmArgs& a, int products, hipStream_t st) {
-    constexpr int kCols = KindOf<KIND>::kDual ? 128 : 256;
-    const int64_t big = (a.M + 255) / 256 * ((a.N + kCols - 1) / kCols) * products;
-    if (big >= 192) launch_tiles<DT, KIND, 256, 256, 2, 4, DMA>(a, products, st);
-    else launch_tiles<DT, KIND, 128, 128, 2, 2, DMA>(a, products, st);
+void launch_size(const GemmArgs& a, int products, hipStream_t st) {
+    switch (gemm_tile(DT, static_cast<GemmKind>(KIND), a.M, a.N, products)) {
+        case kTile256:
+            // (Through registers the larger tile would spill them.)
+            if constexpr (DMA) {
+                launch_tiles<DT, KIND, 256, 256, 2, 4, DMA>(a, products, st);
+                break;
+            }
+        case kTile128: launch_tiles<DT, KIND, 128, 128, 2, 2, DMA>(a, products, st); break;
+        case kTile64: launch_tiles<DT, KIND, 64, 128, 2, 2, DMA>(a, products, st); break;
+    }
 }
 
 template <int DT, int KIND>
 void launch_kind(const GemmArgs& a, int products, hipStream_t st) {
     if (whole_chunks<DT>(a.x, KindOf<KIND>::kXStrided, a.M, a.K) &&
         whole_chunks<DT>(a.y, KindOf<KIND>::kYStrided, a.N, a.K))
-        launch_kind<DT, KIND, true>(a, products, st);
+        launch_size<DT, KIND, true>(a, products, st);
     else
-        launch_kind<DT, KIND, false>(a, products, st);
+        launch_size<DT, KIND, false>(a, products, st);
 }
 
 template <int DT>

@@ -146,6 +146,14 @@ def test_large_tiles(M, C, F):
     run_case(M, C, F, "f16")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,C,F", [(1, 40, 4096), (20, 96, 4104), (50, 33, 3001), (100, 64, 4096), (70, 2056, 136),
+                                   (3000, 40, 48), (3001, 41, 47)])
+def test_long_sums(M, C, F, dtype):
+    """Few tiles and a long sum, which is split over blocks."""
+    run_case(M, C, F, dtype)
+
+
 def test_another_stream():
     st = torch.cuda.Stream()
     run_case(100, 96, 128, "bf16", stream=st)
