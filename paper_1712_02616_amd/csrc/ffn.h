@@ -51,63 +51,80 @@ constexpr int kMaxSplits = 16;
 // out[z][m][n] = sum over the splits, rounded once.
 void launch_join(int dtype, const GemmArgs& a, int products, hipStream_t st);
 
-// act(v) and its derivative.
-template <int ACT>
+// act(v) and its derivative, for values stored as DT.  The hardware's
+// exponential and reciprocal (within 1e-7 of the largest value of each
+// function, as an fp32 evaluation is).  Phi of the GELU: for fp32 values the
+// library's erf; for 16-bit ones erfc(x) = t (a1 + t (a2 + ...)) exp(-x^2), t =
+// 1/(1 + p x), to 1.5e-7 (Abramowitz and Stegun, 7.1.26), which shares its
+// exponential with the derivative and is a quarter of the work.
+template <int ACT, int DT>
 __device__ __forceinline__ void activate(float slope, float v, float& a, float& da) {
     if constexpr (ACT == IABN_ACT_SILU) {
-        const float s = 1.0f / (1.0f + expf(-v));
+        const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-v));
         a = v * s;
         da = s * (1.0f + v * (1.0f - s));
     } else if constexpr (ACT == IABN_ACT_GELU) {
-        const float c = 0.5f * (1.0f + erff(v * 0.70710678118654752f));
+        const float e = __expf(-0.5f * v * v);
+        float c;
+        if constexpr (DT == IABN_F32) {
+            c = 0.5f * (1.0f + erff(v * 0.70710678118654752f));
+        } else {
+            const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(v), 1.0f));
+            float q = fmaf(1.061405429f, t, -1.453152027f);
+            q = fmaf(q, t, 1.421413741f);
+            q = fmaf(q, t, -0.284496736f);
+            q = fmaf(q, t, 0.254829592f);
+            q *= 0.5f * t * e;  // Phi(-|v|)
+            c = v < 0.0f ? q : 1.0f - q;
+        }
         a = v * c;
-        da = c + v * expf(-0.5f * v * v) * 0.39894228040143268f;
+        da = c + v * e * 0.39894228040143268f;
     } else {
         a = v >= 0.0f ? v : slope * v;
         da = v >= 0.0f ? 1.0f : slope;
     }
 }
 
-template <int ACT, int N>
+template <int ACT, int DT, int N>
 __device__ __forceinline__ void gate_forward_as(float slope, const float (&g)[N], const float (&u)[N],
                                                 float (&h)[N]) {
 #pragma unroll
     for (int q = 0; q < N; ++q) {
         float v, d;
-        activate<ACT>(slope, g[q], v, d);
+        activate<ACT, DT>(slope, g[q], v, d);
         h[q] = v * u[q];
     }
 }
 
-template <int N>
+template <int DT, int N>
 __device__ __forceinline__ void gate_forward(int act, float slope, const float (&g)[N],
                                              const float (&u)[N], float (&h)[N]) {
-    if (act == IABN_ACT_SILU) gate_forward_as<IABN_ACT_SILU>(slope, g, u, h);
-    else if (act == IABN_ACT_GELU) gate_forward_as<IABN_ACT_GELU>(slope, g, u, h);
-    else gate_forward_as<IABN_ACT_LEAKY>(slope, g, u, h);
+    if (act == IABN_ACT_SILU) gate_forward_as<IABN_ACT_SILU, DT>(slope, g, u, h);
+    else if (act == IABN_ACT_GELU) gate_forward_as<IABN_ACT_GELU, DT>(slope, g, u, h);
+    else gate_forward_as<IABN_ACT_LEAKY, DT>(slope, g, u, h);
 }
 
-template <int ACT, int N>
+template <int ACT, int DT, int N>
 __device__ __forceinline__ void gate_backward_as(float slope, const float (&dh)[N], const float (&g)[N],
                                                  const float (&u)[N], float (&dg)[N], float (&du)[N],
                                                  float (&h)[N]) {
 #pragma unroll
     for (int q = 0; q < N; ++q) {
         float v, d;
-        activate<ACT>(slope, g[q], v, d);
+        activate<ACT, DT>(slope, g[q], v, d);
         dg[q] = dh[q] * u[q] * d;
         du[q] = dh[q] * v;
         h[q] = v * u[q];
     }
 }
 
-template <int N>
+template <int DT, int N>
 __device__ __forceinline__ void gate_backward(int act, float slope, const float (&dh)[N],
                                               const float (&g)[N], const float (&u)[N], float (&dg)[N],
                                               float (&du)[N], float (&h)[N]) {
-    if (act == IABN_ACT_SILU) gate_backward_as<IABN_ACT_SILU>(slope, dh, g, u, dg, du, h);
-    else if (act == IABN_ACT_GELU) gate_backward_as<IABN_ACT_GELU>(slope, dh, g, u, dg, du, h);
-    else gate_backward_as<IABN_ACT_LEAKY>(slope, dh, g, u, dg, du, h);
+    if (act == IABN_ACT_SILU) gate_backward_as<IABN_ACT_SILU, DT>(slope, dh, g, u, dg, du, h);
+    else if (act == IABN_ACT_GELU) gate_backward_as<IABN_ACT_GELU, DT>(slope, dh, g, u, dg, du, h);
+    else gate_backward_as<IABN_ACT_LEAKY, DT>(slope, dh, g, u, dg, du, h);
 }
 
 // The products kGemmUp and kGemmDown of at most kFewRows tokens (ffn_few.h).

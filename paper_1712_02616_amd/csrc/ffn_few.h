@@ -129,7 +129,7 @@ __global__ __launch_bounds__(512) void few_kernel(GemmArgs a) {
         float u[4], h[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) u[j] = sum[NW - 1][j];
-        gate_forward(a.act, a.slope, v, u, h);
+        gate_forward<DT>(a.act, a.slope, v, u, h);
         put(a.out[0], h);
         if (a.dg) {
             put(a.dg, v);

@@ -92,8 +92,16 @@ struct Stage {
 
     // Straight to LDS, a whole step of K.  Rows past the operand's read its
     // last ones (the results that they go into are not stored).
+    uint64_t base[2];      // the tile's first element of each matrix
     uint32_t off[kLoads];  // bytes from the step's first element
-    __device__ __forceinline__ void prepare(const Operand& o, int64_t rows) {
+    __device__ __forceinline__ void prepare(const Operand& o, int64_t row0, int64_t rows) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            // (Kept in scalar registers, not loaded from the arguments at each step.)
+            const uint64_t p = reinterpret_cast<uint64_t>(static_cast<const T*>(o.p[q]) + row0 * (KS ? 1 : o.ld));
+            base[q] = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(p))) |
+                      uint64_t(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(p >> 32)))) << 32;
+        }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int line = first_line() + i * kLineStep, c = chunk(i) * E;
@@ -105,20 +113,18 @@ struct Stage {
             }
         }
     }
-    __device__ __forceinline__ void fetch(const Operand& o, int seg, int64_t row0, int64_t k0,
-                                          char* lds) const {
+    __device__ __forceinline__ void fetch(const Operand& o, int seg, int64_t k0, char* lds) const {
 #if defined(__HIP_DEVICE_COMPILE__)  // (the host's pass does not know the buffer types)
         typedef __attribute__((address_space(3))) void lds_t;
-        const int64_t at = KS ? k0 * o.ld + row0 : row0 * o.ld + k0;
+        const uint64_t at = (KS ? k0 * o.ld : k0) * sizeof(T);
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             // (A wave's lines are of one matrix: a wave covers 8 lines or fewer.)
             const int which =
                 DUAL ? __builtin_amdgcn_readfirstlane(matrix_of(first_line() + i * kLineStep, seg)) : seg;
-            const T* base = static_cast<const T*>(which ? o.p[1] : o.p[0]) + at;
-            const __amdgpu_buffer_rsrc_t rsrc =
-                __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, 0xffffffff, 0x00027000);
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+                reinterpret_cast<void*>((which ? base[1] : base[0]) + at), 0, 0xffffffff, 0x00027000);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 rsrc, (lds_t*)(lds + (wave * kWave + i * THREADS) * 16), 16, off[i], 0, 0, 0);
         }
@@ -181,7 +187,7 @@ __device__ __forceinline__ void tile_of(int tiles_m, int tiles_n, int& tm, int& 
     tm = static_cast<int>(strip * kStrip + in % height);
 }
 
-template <int DT, int KIND, int TM, int TN, int WAVES_M, int WAVES_N, bool DMA>
+template <int DT, int KIND, int TM, int TN, int WAVES_M, int WAVES_N, bool DMA, int STAGES>
 __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs a, int tiles_m,
                                                                         int tiles_n) {
     using Kind = KindOf<KIND>;
@@ -191,8 +197,11 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
     using SX = Stage<DT, Kind::kXStrided, TM, kT, false>;
     using SY = Stage<DT, Kind::kYStrided, TN, kT, Kind::kDual>;
     constexpr int BK = SX::BK;
-    __shared__ __align__(16) char lds0[SX::kBytes + SY::kBytes];
-    __shared__ __align__(16) char lds1[SX::kBytes + SY::kBytes];
+    // Buffers, of which one is multiplied while the others fill.
+    constexpr int kStages = DMA ? STAGES : 2, kBuffer = SX::kBytes + SY::kBytes;
+    __shared__ __align__(16) char lds[kStages * kBuffer];
+    char *const lds0 = lds, *const lds1 = lds + kBuffer;
+    char *const lds2 = lds + (kStages > 2 ? 2 : 0) * kBuffer, *const lds3 = lds + (kStages > 2 ? 3 : 0) * kBuffer;
 
     int tm, tn;
     tile_of(tiles_m, tiles_n, tm, tn);
@@ -206,6 +215,26 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
     SX sx;
     SY sy;
     const auto multiply = [&](const char* __restrict__ cur) {
+        if constexpr (NM * NN <= 16) {
+            // One or two waves of a SIMD have to keep it busy: every read of
+            // the step is under way before its first product.
+            u32x4 fy[kSteps][NN], fx[kSteps][NM];
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+#pragma unroll
+                for (int j = 0; j < NN; ++j) fy[s][j] = SY::frag(cur + SX::kBytes, wn + j * 16, s);
+#pragma unroll
+                for (int i = 0; i < NM; ++i) fx[s][i] = SX::frag(cur, wm + i * 16, s);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                for (int i = 0; i < NM; ++i)
+#pragma unroll
+                    for (int j = 0; j < NN; ++j) acc[i][j] = Mma<DT>::run(fy[s][j], fx[s][i], acc[i][j]);
+            return;
+        }
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             u32x4 fy[NN];
@@ -233,32 +262,48 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
         const auto fetch = [&](int kt, char* buf) {
             const int seg = Kind::kSegs > 1 ? (kt >= whole ? 1 : 0) : z;
             const int64_t k0 = int64_t(Kind::kSegs > 1 && seg ? kt - whole : kt) * BK;
-            sx.fetch(a.x, seg, m0, k0, buf);
-            sy.fetch(a.y, seg, n0, k0, buf + SX::kBytes);
+            sx.fetch(a.x, seg, k0, buf);
+            sy.fetch(a.y, seg, k0, buf + SX::kBytes);
         };
-        sx.prepare(a.x, a.M - m0);
-        sy.prepare(a.y, a.N - n0);
-        // What a wave has fetched is in LDS when its own loads are done: each
-        // waits for its own before the barrier that all meet at.
-        const auto arrive = [&] {
-            __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
-            __syncthreads();
-        };
-        if (lo < hi) fetch(lo, lds0);
-        arrive();
-        // The buffers are told apart (restrict), so that reading one does not
-        // wait for what arrives in the other.
-        const auto both = [&](int kt, const char* __restrict__ cur, char* __restrict__ next) {
-            if (kt + 1 < hi) fetch(kt + 1, next);
+        constexpr int kInFlight = (kStages - 2) * (SX::kLoads + SY::kLoads);
+        static_assert(kInFlight < 64, "what a wave can count");
+        // Step kt + j from buffer j: its fetches are in LDS when each wave has
+        // waited for its own (those of later steps may be on their way) and
+        // all have met; then the buffer of the step before is free.
+        const auto turn = [&](int kt, int j, const char* __restrict__ cur, char* __restrict__ free) {
+            // (This wave's reads of the buffer to be filled are done too.)
+            if (kt + j + kStages - 2 < hi)
+                __builtin_amdgcn_s_waitcnt((kInFlight & 15) | (kInFlight >> 4 << 14) | 0x0070);
+            else
+                __builtin_amdgcn_s_waitcnt(0x0070);  // the last ones
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (kt + j + kStages - 1 < hi) fetch(kt + j + kStages - 1, free);
             multiply(cur);
         };
-        for (int kt = lo; kt < hi; kt += 2) {
-            both(kt, lds0, lds1);
-            arrive();
-            if (kt + 1 >= hi) break;
-            both(kt + 1, lds1, lds0);
-            arrive();
-        }
+        // (The buffers are told apart, restrict, so that the compiler does not
+        // make the reads of one wait for what arrives in another.)
+        const auto round = [&](int kt, char* __restrict__ b0, char* __restrict__ b1,
+                               char* __restrict__ b2, char* __restrict__ b3) {
+            if constexpr (kStages == 2) {
+                turn(kt, 0, b0, b1);
+                if (kt + 1 < hi) turn(kt, 1, b1, b0);
+            } else {
+                turn(kt, 0, b0, b3);
+                if (kt + 1 < hi) turn(kt, 1, b1, b0);
+                if (kt + 2 < hi) turn(kt, 2, b2, b1);
+                if (kt + 3 < hi) turn(kt, 3, b3, b2);
+            }
+        };
+        sx.prepare(a.x, m0, a.M - m0);
+        sy.prepare(a.y, n0, a.N - n0);
+        char* const b[4] = {lds0, lds1, lds2, lds3};
+#pragma unroll
+        for (int j = 0; j < kStages - 1; ++j)
+            if (lo + j < hi) fetch(lo + j, b[j]);
+        for (int kt = lo; kt < hi; kt += kStages) round(kt, lds0, lds1, lds2, lds3);
+        __syncthreads();
     }
     if (from < to) {
         const auto load = [&](int kt) {
@@ -291,14 +336,42 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
     // kPass rows of 16 accumulators at a time in its own part.
     __syncthreads();
     constexpr int kPass = NM < 4 ? NM : 4, kPart = kPass * 16 * WN;
-    static_assert(WAVES_M * WAVES_N * kPart * 4 <= 2 * (SX::kBytes + SY::kBytes) && NM % kPass == 0 && WN == 64, "");
-    constexpr int kHalf = WAVES_M * WAVES_N / 2;
-    float* const part = reinterpret_cast<float*>(wave < kHalf ? lds0 : lds1) + (wave % kHalf) * kPart;
+    static_assert(WAVES_M * WAVES_N * kPart * 4 <= kStages * kBuffer && NM % kPass == 0 && WN == 64, "");
+    float* const part = reinterpret_cast<float*>(lds) + wave * kPart;
     const auto at = [](int row, int col) {  // 16-byte units permuted by the row
         return row * WN + (((col >> 2) ^ (row & 15)) << 2);
     };
+    // A lane's c-th chunk of the rows of pass p.
+    constexpr int kCh = (Kind::kDual ? WN / 2 : WN) / kChunk;  // chunks of a row
+    constexpr int kTurns = kPass * 16 * kCh / kWave;
+    static_assert(kTurns * kWave == kPass * 16 * kCh && kTurns % 2 == 0, "");
+    struct Place {
+        int row, col, inside;
+        int64_t out;
+    };
+    const auto place = [&](int p, int c) {
+        const int at_c = c * kWave + static_cast<int>(lane_id());
+        Place r;
+        r.row = at_c / kCh, r.col = at_c % kCh * kChunk;
+        const int64_t m = m0 + wm + p * 16 + r.row, n = n0 + (Kind::kDual ? wn / 2 : wn) + r.col;
+        r.inside = m < a.M ? static_cast<int>(max(min(a.N - n, int64_t(kChunk)), int64_t(0))) : 0;
+        r.out = m * a.N + n;
+        return r;
+    };
+    // kGemmDh: g and u of the next chunks are on their way while one is finished.
+    typedef typename ChunkOf<DT>::vec chunk_t;
+    const auto load_gu = [&](int p, int c, chunk_t (&v)[2]) {
+        const Place at_c = place(p, c);
+        v[0] = load_chunk<DT, kStream>(a.g, at_c.out, at_c.inside);
+        v[1] = load_chunk<DT, kStream>(a.u, at_c.out, at_c.inside);
+    };
 #pragma unroll
     for (int p = 0; p < NM; p += kPass) {
+        chunk_t gu[2][2];
+        if constexpr (KIND == kGemmDh) {
+            load_gu(p, 0, gu[0]);
+            load_gu(p, 1, gu[1]);
+        }
         const int lm = lane_id() & 15, ln = (lane_id() >> 4) * 4;
 #pragma unroll
         for (int i = 0; i < kPass; ++i)
@@ -313,39 +386,46 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] = lo[q], v[q + 4] = hi[q];
         };
-        constexpr int kCh = (Kind::kDual ? WN / 2 : WN) / kChunk;  // chunks of a row
+        if constexpr (KIND == kGemmDh) {
 #pragma unroll 1
-        for (int c = lane_id(); c < kPass * 16 * kCh; c += kWave) {
-            const int row = c / kCh, col = c % kCh * kChunk;
-            const int64_t m = m0 + wm + p * 16 + row;
-            const int64_t n = n0 + (Kind::kDual ? wn / 2 : wn) + col, left = a.N - n, at_out = m * a.N + n;
-            if (m >= a.M || left <= 0) continue;
-            const int inside = static_cast<int>(min(left, int64_t(kChunk)));
-            float v[kChunk];
-            read(row, col, v);
-            if constexpr (KIND == kGemmUp) {
-                float u[kChunk], h[kChunk];
-                read(row, col + WN / 2, u);
-                gate_forward(a.act, a.slope, v, u, h);
-                store_chunk<DT, kCached>(a.out[0], at_out, inside, h);
-                if (a.dg) {
-                    store_chunk<DT, kStream>(a.dg, at_out, inside, v);
-                    store_chunk<DT, kStream>(a.du, at_out, inside, u);
+            for (int c = 0; c < kTurns; c += 2)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const auto raw_g = gu[q][0], raw_u = gu[q][1];
+                    const Place at_c = place(p, c + q);
+                    if (c + q + 2 < kTurns) load_gu(p, c + q + 2, gu[q]);
+                    if (at_c.inside <= 0) continue;
+                    float v[kChunk], g[kChunk], u[kChunk], dg[kChunk], du[kChunk], h[kChunk];
+                    read(at_c.row, at_c.col, v);
+                    widen<DT>(raw_g, g);
+                    widen<DT>(raw_u, u);
+                    gate_backward<DT>(a.act, a.slope, v, g, u, dg, du, h);
+                    store_chunk<DT, kCached>(a.dg, at_c.out, at_c.inside, dg);
+                    store_chunk<DT, kCached>(a.du, at_c.out, at_c.inside, du);
+                    store_chunk<DT, kCached>(a.out[0], at_c.out, at_c.inside, h);
                 }
-            } else if constexpr (KIND == kGemmDh) {
-                float g[kChunk], u[kChunk], dg[kChunk], du[kChunk], h[kChunk];
-                widen<DT>(load_chunk<DT, kStream>(a.g, at_out, inside), g);
-                widen<DT>(load_chunk<DT, kStream>(a.u, at_out, inside), u);
-                gate_backward(a.act, a.slope, v, g, u, dg, du, h);
-                store_chunk<DT, kCached>(a.dg, at_out, inside, dg);
-                store_chunk<DT, kCached>(a.du, at_out, inside, du);
-                store_chunk<DT, kCached>(a.out[0], at_out, inside, h);
-            } else {
-                if (gridDim.y > 1)
+        } else {
+#pragma unroll 1
+            for (int c = 0; c < kTurns; ++c) {
+                const Place at_c = place(p, c);
+                if (at_c.inside <= 0) continue;
+                float v[kChunk];
+                read(at_c.row, at_c.col, v);
+                if constexpr (KIND == kGemmUp) {
+                    float u[kChunk], h[kChunk];
+                    read(at_c.row, at_c.col + WN / 2, u);
+                    gate_forward<DT>(a.act, a.slope, v, u, h);
+                    store_chunk<DT, kCached>(a.out[0], at_c.out, at_c.inside, h);
+                    if (a.dg) {
+                        store_chunk<DT, kStream>(a.dg, at_c.out, at_c.inside, v);
+                        store_chunk<DT, kStream>(a.du, at_c.out, at_c.inside, u);
+                    }
+                } else if (gridDim.y > 1) {
                     store_chunk<IABN_F32, kCached>(
-                        a.part, (int64_t(blockIdx.y) * gridDim.z + z) * a.M * a.N + at_out, inside, v);
-                else
-                    store_chunk<DT, kCached>(z ? a.out[1] : a.out[0], at_out, inside, v);
+                        a.part, (int64_t(blockIdx.y) * gridDim.z + z) * a.M * a.N + at_c.out, at_c.inside, v);
+                } else {
+                    store_chunk<DT, kCached>(z ? a.out[1] : a.out[0], at_c.out, at_c.inside, v);
+                }
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -353,11 +433,11 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
     }
 }
 
-template <int DT, int KIND, int TM, int TN, int WAVES_M, int WAVES_N, bool DMA>
+template <int DT, int KIND, int TM, int TN, int WAVES_M, int WAVES_N, bool DMA, int STAGES>
 void launch_tiles(const GemmArgs& a, int products, hipStream_t st) {
     constexpr int kCols = KindOf<KIND>::kDual ? TN / 2 : TN;
     const int64_t tm = (a.M + TM - 1) / TM, tn = (a.N + kCols - 1) / kCols;
-    gemm_kernel<DT, KIND, TM, TN, WAVES_M, WAVES_N, DMA>
+    gemm_kernel<DT, KIND, TM, TN, WAVES_M, WAVES_N, DMA, STAGES>
         <<<dim3(static_cast<uint32_t>(tm * tn), a.splits, products), WAVES_M * WAVES_N * kWave, 0, st>>>(
             a, static_cast<int>(tm), static_cast<int>(tn));
 }
@@ -379,11 +459,11 @@ void launch_size(const GemmArgs& a, int products, hipStream_t st) {
         case kTile256:
             // (Through registers the larger tile would spill them.)
             if constexpr (DMA) {
-                launch_tiles<DT, KIND, 256, 256, 2, 4, DMA>(a, products, st);
+                launch_tiles<DT, KIND, 256, 256, 2, 4, DMA, 2>(a, products, st);
                 break;
             }
-        case kTile128: launch_tiles<DT, KIND, 128, 128, 2, 2, DMA>(a, products, st); break;
-        case kTile64: launch_tiles<DT, KIND, 64, 128, 2, 2, DMA>(a, products, st); break;
+        case kTile128: launch_tiles<DT, KIND, 128, 128, 2, 2, DMA, 2>(a, products, st); break;
+        case kTile64: launch_tiles<DT, KIND, 64, 128, 2, 2, DMA, 2>(a, products, st); break;
     }
 }
 
