@@ -106,13 +106,6 @@ int check_ffn(int dtype, int act, float slope, int64_t M, int64_t C, int64_t F) 
     return IABN_OK;
 }
 
-// A product of the block as the entry points ask for it, and what it needs
-// of the workspace: its sums, where the sum over k is split.
-size_t part_bytes(int dtype, GemmKind kind, int64_t M, int64_t N, int64_t K, int products) {
-    const int splits = gemm_splits(dtype, kind, M, N, K, products);
-    return splits > 1 ? static_cast<size_t>(splits) * products * M * N * sizeof(float) : 0;
-}
-
 // h, [M, F], and then the largest of the products' sums.
 size_t h_bytes(int64_t M, int64_t F, int dtype) {
     return (static_cast<size_t>(M) * F * elem_bytes(dtype) + 255) / 256 * 256;
@@ -120,7 +113,7 @@ size_t h_bytes(int64_t M, int64_t F, int dtype) {
 
 size_t ffn_workspace(int64_t M, int64_t C, int64_t F, int dtype) {
     size_t part = 0;
-    for (size_t p : {part_bytes(dtype, kGemmDown, M, C, F, 1), part_bytes(dtype, kGemmDx, M, C, 2 * F, 1),
+    for (size_t p : {part_bytes(dtype, kGemmDown, M, C, F, 1), part_bytes(dtype, kGemmDx, M, C, F, 1),
                      part_bytes(dtype, kGemmDw, C, F, M, 1), part_bytes(dtype, kGemmDw, F, C, M, 2)})
         part = part < p ? p : part;
     return h_bytes(M, F, dtype) + part;
@@ -136,25 +129,22 @@ int check_workspace(void* workspace, size_t bytes, size_t need) {
     return IABN_OK;
 }
 
+// A product of the block, whose split sums go behind h in the workspace.
 void gemm(int dtype, GemmKind kind, GemmArgs a, int products, void* workspace, int64_t M, int64_t F,
           hipStream_t st) {
-    const int64_t terms = kind == kGemmDx ? 2 * a.K : a.K;
-    a.splits = gemm_splits(dtype, kind, a.M, a.N, terms, products);
     a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + h_bytes(M, F, dtype));
-    if (few_rows(kind, a.M)) {
-        switch (dtype) {
-            case IABN_F32: launch_few<IABN_F32>(kind, a, st); break;
-            case IABN_F16: launch_few<IABN_F16>(kind, a, st); break;
-            default: launch_few<IABN_BF16>(kind, a, st); break;
-        }
-    } else {
-        switch (dtype) {
-            case IABN_F32: launch_gemm<IABN_F32>(kind, a, products, st); break;
-            case IABN_F16: launch_gemm<IABN_F16>(kind, a, products, st); break;
-            default: launch_gemm<IABN_BF16>(kind, a, products, st); break;
-        }
+    const bool few = few_rows(kind, a.M);
+    switch (dtype) {
+        case IABN_F32:
+            few ? launch_few<IABN_F32>(kind, a, st) : launch_gemm<IABN_F32>(kind, a, products, st);
+            break;
+        case IABN_F16:
+            few ? launch_few<IABN_F16>(kind, a, st) : launch_gemm<IABN_F16>(kind, a, products, st);
+            break;
+        default:
+            few ? launch_few<IABN_BF16>(kind, a, st) : launch_gemm<IABN_BF16>(kind, a, products, st);
+            break;
     }
-    if (a.splits > 1) launch_join(dtype, a, products, st);
 }
 
 bool finite(float v) { return std::isfinite(v); }

@@ -37,16 +37,10 @@ struct GemmArgs {
     float slope;
     // Where the sum over k is split over blocks: their fp32 sums, [splits]
     // [products][M][N], which launch_join adds up in this order.
-    int splits;
+    // (Set by the launch.)
     float* part;
+    int splits;
 };
-
-// The split of a product's sum over k; 1 where it has enough tiles by itself.
-// `kind` as launch_gemm and launch_few take it.
-int gemm_splits(int dtype, GemmKind kind, int64_t M, int64_t N, int64_t K, int products);
-
-// Largest sum of fp32 values that a product of the block leaves in `part`.
-constexpr int kMaxSplits = 16;
 
 // out[z][m][n] = sum over the splits, rounded once.
 void launch_join(int dtype, const GemmArgs& a, int products, hipStream_t st);
@@ -143,13 +137,18 @@ extern template bool launch_few<IABN_BF16>(GemmKind, const GemmArgs&, hipStream_
 template <int DT>
 bool launch_gemm(GemmKind kind, const GemmArgs& a, int products, hipStream_t st);
 
-// A product's tiles: of 256x256 (kGemmUp: of 128 columns of each projection),
-// 128x128 or 64x128 outputs.
-enum TileSize { kTile256, kTile128, kTile64 };
-TileSize gemm_tile(int dtype, GemmKind kind, int64_t M, int64_t N, int products);
+// How a product runs: tiles of 256x256 (kGemmUp: of 128 columns of each
+// projection), 128x128, 64x128 or 32x128 outputs, and over how many blocks the
+// sum over k is split.  direct: its tiles go straight to LDS.
+enum TileSize { kTile256, kTile128, kTile64, kTile32 };
+struct GemmPlan {
+    TileSize tile;
+    int splits;
+};
+GemmPlan plan_gemm(int dtype, GemmKind kind, bool direct, int64_t M, int64_t N, int64_t K, int products);
+int plan_few(int64_t N, int64_t K, int dtype);
 
-extern template bool launch_gemm<IABN_F32>(GemmKind, const GemmArgs&, int, hipStream_t);
-extern template bool launch_gemm<IABN_F16>(GemmKind, const GemmArgs&, int, hipStream_t);
-extern template bool launch_gemm<IABN_BF16>(GemmKind, const GemmArgs&, int, hipStream_t);
+// What a product of these sizes can ask of `part`, in bytes.
+size_t part_bytes(int dtype, GemmKind kind, int64_t M, int64_t N, int64_t K, int products);
 
 }  // namespace iabn_impl

@@ -146,7 +146,8 @@ __global__ __launch_bounds__(512) void few_kernel(GemmArgs a) {
 }
 
 template <int DT, int KIND, int MT>
-void launch_few_tiles(const GemmArgs& a, hipStream_t st) {
+void launch_few_tiles(GemmArgs a, hipStream_t st) {
+    a.splits = KIND == kGemmDown ? plan_few(a.N, a.K, DT) : 1;
     constexpr int kLine = 128 / sizeof(typename Elem<DT>::T), NW = KIND == kGemmUp ? 2 : 1;
     const int64_t blocks = (a.N + 15) / 16, lines = (a.K + kLine - 1) / kLine;
     // Waves of a block: enough for about 2048 in all, each with a batch of
@@ -156,6 +157,7 @@ void launch_few_tiles(const GemmArgs& a, hipStream_t st) {
     const size_t lds = static_cast<size_t>(waves) * NW * MT * kWave * sizeof(f32x4);
     few_kernel<DT, KIND, MT>
         <<<dim3(static_cast<uint32_t>(blocks), a.splits), waves * kWave, lds, st>>>(a);
+    if (a.splits > 1) launch_join(DT, a, 1, st);
 }
 
 template <int DT, int KIND>

@@ -47,8 +47,9 @@ struct Stage {
 
     static __device__ __forceinline__ uint32_t swizzle(int line) {
         if constexpr (!KS) return (line >> 1) & 7;
-        else if constexpr (DT == IABN_F32) return (line >> 2) & 3;
-        // (Lines of 64 elements are half a round of the banks.)
+        else if constexpr (DT == IABN_F32) return (line >> 2) & (ROWS == 32 ? 1 : 3);
+        // (Lines of 64 elements are half a round of the banks, of 32 a quarter.)
+        else if constexpr (ROWS == 32) return (line >> 3) & 1;
         else if constexpr (ROWS == 64) return ((line >> 2) & 2) | ((line >> 1) & 1);
         else return ((line >> 1) & 4) | (line & 3);
     }
@@ -187,7 +188,7 @@ __device__ __forceinline__ void tile_of(int tiles_m, int tiles_n, int& tm, int& 
     tm = static_cast<int>(strip * kStrip + in % height);
 }
 
-template <int DT, int KIND, int TM, int TN, int WAVES_M, int WAVES_N, bool DMA, int STAGES>
+template <int DT, int KIND, int TM, int TN, int WAVES_M, int WAVES_N, bool DMA>
 __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs a, int tiles_m,
                                                                         int tiles_n) {
     using Kind = KindOf<KIND>;
@@ -197,11 +198,10 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
     using SX = Stage<DT, Kind::kXStrided, TM, kT, false>;
     using SY = Stage<DT, Kind::kYStrided, TN, kT, Kind::kDual>;
     constexpr int BK = SX::BK;
-    // Buffers, of which one is multiplied while the others fill.
-    constexpr int kStages = DMA ? STAGES : 2, kBuffer = SX::kBytes + SY::kBytes;
-    __shared__ __align__(16) char lds[kStages * kBuffer];
+    // Two buffers, of which one is multiplied while the other fills.
+    constexpr int kBuffer = SX::kBytes + SY::kBytes;
+    __shared__ __align__(16) char lds[2 * kBuffer];
     char *const lds0 = lds, *const lds1 = lds + kBuffer;
-    char *const lds2 = lds + (kStages > 2 ? 2 : 0) * kBuffer, *const lds3 = lds + (kStages > 2 ? 3 : 0) * kBuffer;
 
     int tm, tn;
     tile_of(tiles_m, tiles_n, tm, tn);
@@ -265,44 +265,27 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
             sx.fetch(a.x, seg, k0, buf);
             sy.fetch(a.y, seg, k0, buf + SX::kBytes);
         };
-        constexpr int kInFlight = (kStages - 2) * (SX::kLoads + SY::kLoads);
-        static_assert(kInFlight < 64, "what a wave can count");
-        // Step kt + j from buffer j: its fetches are in LDS when each wave has
-        // waited for its own (those of later steps may be on their way) and
-        // all have met; then the buffer of the step before is free.
-        const auto turn = [&](int kt, int j, const char* __restrict__ cur, char* __restrict__ free) {
-            // (This wave's reads of the buffer to be filled are done too.)
-            if (kt + j + kStages - 2 < hi)
-                __builtin_amdgcn_s_waitcnt((kInFlight & 15) | (kInFlight >> 4 << 14) | 0x0070);
-            else
-                __builtin_amdgcn_s_waitcnt(0x0070);  // the last ones
+        // Step kt from `cur`: what is fetched there has arrived when each wave
+        // has waited for its own fetches and all have met; then `free` may be
+        // filled, whose reads have ended (each wave has waited for its own).
+        const auto turn = [&](int kt, const char* __restrict__ cur, char* __restrict__ free) {
+            __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            if (kt + j + kStages - 1 < hi) fetch(kt + j + kStages - 1, free);
+            if (kt + 1 < hi) fetch(kt + 1, free);
             multiply(cur);
         };
         // (The buffers are told apart, restrict, so that the compiler does not
-        // make the reads of one wait for what arrives in another.)
-        const auto round = [&](int kt, char* __restrict__ b0, char* __restrict__ b1,
-                               char* __restrict__ b2, char* __restrict__ b3) {
-            if constexpr (kStages == 2) {
-                turn(kt, 0, b0, b1);
-                if (kt + 1 < hi) turn(kt, 1, b1, b0);
-            } else {
-                turn(kt, 0, b0, b3);
-                if (kt + 1 < hi) turn(kt, 1, b1, b0);
-                if (kt + 2 < hi) turn(kt, 2, b2, b1);
-                if (kt + 3 < hi) turn(kt, 3, b3, b2);
-            }
+        // make the reads of one wait for what arrives in the other.)
+        const auto round = [&](int kt, char* __restrict__ b0, char* __restrict__ b1) {
+            turn(kt, b0, b1);
+            if (kt + 1 < hi) turn(kt + 1, b1, b0);
         };
         sx.prepare(a.x, m0, a.M - m0);
         sy.prepare(a.y, n0, a.N - n0);
-        char* const b[4] = {lds0, lds1, lds2, lds3};
-#pragma unroll
-        for (int j = 0; j < kStages - 1; ++j)
-            if (lo + j < hi) fetch(lo + j, b[j]);
-        for (int kt = lo; kt < hi; kt += kStages) round(kt, lds0, lds1, lds2, lds3);
+        if (lo < hi) fetch(lo, lds0);
+        for (int kt = lo; kt < hi; kt += 2) round(kt, lds0, lds1);
         __syncthreads();
     }
     if (from < to) {
@@ -336,7 +319,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
     // kPass rows of 16 accumulators at a time in its own part.
     __syncthreads();
     constexpr int kPass = NM < 4 ? NM : 4, kPart = kPass * 16 * WN;
-    static_assert(WAVES_M * WAVES_N * kPart * 4 <= kStages * kBuffer && NM % kPass == 0 && WN == 64, "");
+    static_assert(WAVES_M * WAVES_N * kPart * 4 <= 2 * kBuffer && NM % kPass == 0 && WN == 64, "");
     float* const part = reinterpret_cast<float*>(lds) + wave * kPart;
     const auto at = [](int row, int col) {  // 16-byte units permuted by the row
         return row * WN + (((col >> 2) ^ (row & 15)) << 2);
@@ -344,7 +327,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
     // A lane's c-th chunk of the rows of pass p.
     constexpr int kCh = (Kind::kDual ? WN / 2 : WN) / kChunk;  // chunks of a row
     constexpr int kTurns = kPass * 16 * kCh / kWave;
-    static_assert(kTurns * kWave == kPass * 16 * kCh && kTurns % 2 == 0, "");
+    static_assert(kTurns * kWave == kPass * 16 * kCh && (KIND != kGemmDh || kTurns % 2 == 0), "");
     struct Place {
         int row, col, inside;
         int64_t out;
@@ -433,11 +416,11 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
     }
 }
 
-template <int DT, int KIND, int TM, int TN, int WAVES_M, int WAVES_N, bool DMA, int STAGES>
+template <int DT, int KIND, int TM, int TN, int WAVES_M, int WAVES_N, bool DMA>
 void launch_tiles(const GemmArgs& a, int products, hipStream_t st) {
     constexpr int kCols = KindOf<KIND>::kDual ? TN / 2 : TN;
     const int64_t tm = (a.M + TM - 1) / TM, tn = (a.N + kCols - 1) / kCols;
-    gemm_kernel<DT, KIND, TM, TN, WAVES_M, WAVES_N, DMA, STAGES>
+    gemm_kernel<DT, KIND, TM, TN, WAVES_M, WAVES_N, DMA>
         <<<dim3(static_cast<uint32_t>(tm * tn), a.splits, products), WAVES_M * WAVES_N * kWave, 0, st>>>(
             a, static_cast<int>(tm), static_cast<int>(tn));
 }
@@ -454,26 +437,28 @@ bool whole_chunks(const Operand& o, bool strided, int64_t rows, int64_t K) {
 }
 
 template <int DT, int KIND, bool DMA>
-void launch_size(const GemmArgs& a, int products, hipStream_t st) {
-    switch (gemm_tile(DT, static_cast<GemmKind>(KIND), a.M, a.N, products)) {
+void launch_planned(GemmArgs a, int products, hipStream_t st) {
+    const GemmPlan plan = plan_gemm(DT, static_cast<GemmKind>(KIND), DMA, a.M, a.N, a.K, products);
+    a.splits = plan.splits;
+    switch (plan.tile) {
         case kTile256:
-            // (Through registers the larger tile would spill them.)
-            if constexpr (DMA) {
-                launch_tiles<DT, KIND, 256, 256, 2, 4, DMA, 2>(a, products, st);
-                break;
-            }
-        case kTile128: launch_tiles<DT, KIND, 128, 128, 2, 2, DMA, 2>(a, products, st); break;
-        case kTile64: launch_tiles<DT, KIND, 64, 128, 2, 2, DMA, 2>(a, products, st); break;
+            // (Through registers, and in fp32, it would spill them.)
+            if constexpr (DMA && DT != IABN_F32) launch_tiles<DT, KIND, 256, 256, 2, 4, DMA>(a, products, st);
+            break;
+        case kTile128: launch_tiles<DT, KIND, 128, 128, 2, 2, DMA>(a, products, st); break;
+        case kTile64: launch_tiles<DT, KIND, 64, 128, 2, 2, DMA>(a, products, st); break;
+        case kTile32: launch_tiles<DT, KIND, 32, 128, 2, 2, DMA>(a, products, st); break;
     }
+    if (a.splits > 1) launch_join(DT, a, products, st);
 }
 
 template <int DT, int KIND>
 void launch_kind(const GemmArgs& a, int products, hipStream_t st) {
     if (whole_chunks<DT>(a.x, KindOf<KIND>::kXStrided, a.M, a.K) &&
         whole_chunks<DT>(a.y, KindOf<KIND>::kYStrided, a.N, a.K))
-        launch_size<DT, KIND, true>(a, products, st);
+        launch_planned<DT, KIND, true>(a, products, st);
     else
-        launch_size<DT, KIND, false>(a, products, st);
+        launch_planned<DT, KIND, false>(a, products, st);
 }
 
 template <int DT>

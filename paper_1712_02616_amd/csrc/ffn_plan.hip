@@ -6,14 +6,28 @@ namespace iabn_impl {
 namespace {
 
 constexpr int64_t kCUs = 256;
+constexpr int kMaxSplits = 16;
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-int64_t tiles(TileSize t, GemmKind kind, int64_t M, int64_t N, int products) {
-    const int64_t tm = t == kTile256 ? 256 : t == kTile128 ? 128 : 64;
-    const int64_t tn = (t == kTile256 ? 256 : 128) / (kind == kGemmUp ? 2 : 1);
-    return div_up(M, tm) * div_up(N, tn) * products;
-}
+// The time of a step of 128 bytes of K with 1, 2, 3 and 4 blocks on a CU, and
+// of each block's ends (us, measured at full grids of each).  16-bit: the
+// larger tile reads half of LDS per product but holds a CU alone; two blocks
+// of 128x128 hide each other's waits (0.68 us for both, 0.67 for one).  fp32
+// is bound by the matrix cores at every size: the tiles matter where they do
+// not fill the last round.
+struct TileCost {
+    float step[4], ends;
+};
+// [fp32][direct][tile]
+constexpr TileCost kCost[2][2][4] = {
+    {{{{0, 0, 0, 0}, 0}, {{1.05f, 2.1f, 3.1f, 4.2f}, 2}, {{0.76f, 0.97f, 1.65f, 1.85f}, 1}, {{0.58f, 0.8f, 0.93f, 1.5f}, 0.5f}},
+     {{{1.27f, 2.54f, 3.81f, 5.08f}, 8}, {{0.67f, 0.68f, 1.36f, 1.4f}, 1.6f}, {{0.32f, 0.55f, 0.75f, 1.16f}, 0.8f}, {{0.26f, 0.45f, 0.68f, 0.87f}, 0.4f}}},
+    {{{{0, 0, 0, 0}, 0}, {{2.65f, 5.2f, 7.8f, 10.4f}, 4}, {{1.6f, 2.6f, 4.8f, 5.0f}, 2}, {{1.0f, 1.6f, 2.25f, 3.2f}, 1}},
+     {{{0, 0, 0, 0}, 0}, {{2.05f, 3.7f, 7.2f, 7.4f}, 4}, {{1.1f, 1.93f, 2.8f, 3.9f}, 2}, {{0.63f, 1.02f, 1.5f, 1.95f}, 1}}}};
+constexpr float kGatingEnds = 3.0f;  // kGemmDh's end is so much longer
+// Joining split sums: a launch, and the sums written and read.
+constexpr float kJoinUs = 3.0f, kJoinBytesPerUs = 4e6f;
 
 template <int DT>
 __global__ __launch_bounds__(kThreads) void join_kernel(GemmArgs a) {
@@ -34,28 +48,58 @@ __global__ __launch_bounds__(kThreads) void join_kernel(GemmArgs a) {
 
 }  // namespace
 
-TileSize gemm_tile(int, GemmKind kind, int64_t M, int64_t N, int products) {
-    if (tiles(kTile256, kind, M, N, products) >= 192) return kTile256;
-    if (tiles(kTile128, kind, M, N, products) >= 192) return kTile128;
-    return kTile64;
+GemmPlan plan_gemm(int dtype, GemmKind kind, bool direct, int64_t M, int64_t N, int64_t K, int products) {
+    const int64_t step = dtype == IABN_F32 ? 32 : 64;
+    const int64_t steps = div_up(K, step) * (kind == kGemmDx ? 2 : 1);
+    const bool splittable = kind != kGemmUp && kind != kGemmDh;
+    GemmPlan best = {kTile128, 1};
+    float best_us = 0.0f;
+    for (TileSize t : {kTile256, kTile128, kTile64, kTile32}) {
+        const TileCost& cost = kCost[dtype == IABN_F32][direct][t];
+        if (cost.ends == 0.0f) continue;
+        const int64_t tm = t == kTile256 ? 256 : t == kTile128 ? 128 : t == kTile64 ? 64 : 32;
+        const int64_t tn = (t == kTile256 ? 256 : 128) / (kind == kGemmUp ? 2 : 1);
+        const int64_t tiles = div_up(M, tm) * div_up(N, tn) * products;
+        for (int s = 1; s <= (splittable ? kMaxSplits : 1) && s <= steps; s *= 2) {
+            const int64_t on_cu = div_up(tiles * s, kCUs);  // blocks that the busiest CU gets
+            const float full = static_cast<float>((on_cu - 1) / 4);
+            const float per_step = full * cost.step[3] + cost.step[(on_cu - 1) % 4];
+            const float ends = cost.ends * (kind == kGemmDh ? kGatingEnds : 1.0f);
+            float us = static_cast<float>(div_up(steps, s)) * per_step + static_cast<float>(on_cu) * ends;
+            if (s > 1) us += kJoinUs + 8.0f * s * M * N * products / kJoinBytesPerUs;
+            if (best_us == 0.0f || us < best_us) {
+                best_us = us;
+                best = {t, s};
+            }
+        }
+    }
+    return best;
 }
 
-int gemm_splits(int dtype, GemmKind kind, int64_t M, int64_t N, int64_t K, int products) {
-    if (kind == kGemmUp || kind == kGemmDh || M == 0 || N == 0) return 1;
-    const int64_t step = dtype == IABN_F32 ? 32 : 64;  // of K
-    int64_t blocks, least;                             // steps of a split, at least
-    if (few_rows(kind, M)) {
-        blocks = div_up(N, 16);
-        least = 16;
-    } else {
-        blocks = tiles(gemm_tile(dtype, kind, M, N, products), kind, M, N, products);
-        least = 8;
-    }
+// Blocks of 16 columns over K, for few tokens: where there are fewer of them
+// than CUs, K is split for about two blocks a CU, of 16 lines of 128 bytes at
+// least ((24 tokens, 8192 -> 2048) fp16: 20.3 us -> 12.1 and 3.9 to join).
+int plan_few(int64_t N, int64_t K, int dtype) {
+    const int64_t blocks = div_up(N, 16), lines = div_up(K, dtype == IABN_F32 ? 32 : 64);
     if (blocks >= kCUs * 3 / 4) return 1;
     int64_t s = kCUs * 2 / blocks;
     if (s > kMaxSplits) s = kMaxSplits;
-    if (s > div_up(K, step) / least) s = div_up(K, step) / least;
+    if (s > lines / 16) s = lines / 16;
     return s < 2 ? 1 : static_cast<int>(s);
+}
+
+size_t part_bytes(int dtype, GemmKind kind, int64_t M, int64_t N, int64_t K, int products) {
+    if (M == 0 || N == 0 || K == 0) return 0;
+    int splits = 1;
+    if (few_rows(kind, M)) {
+        splits = plan_few(N, K, dtype);
+    } else {
+        for (bool direct : {false, true}) {
+            const int s = plan_gemm(dtype, kind, direct, M, N, K, products).splits;
+            splits = splits < s ? s : splits;
+        }
+    }
+    return splits > 1 ? static_cast<size_t>(splits) * products * M * N * sizeof(float) : 0;
 }
 
 void launch_join(int dtype, const GemmArgs& a, int products, hipStream_t st) {
