@@ -58,7 +58,7 @@ constexpr int64_t kBwdMinRows = 8;
 
 ResnormSplit split_rows(int64_t R, int64_t C, int64_t groups) {
     if (R == 0) return {1, 0, 0, 0, 0};
-    const RowShape shape = row_shape(static_cast<int>((C + kChunk - 1) / kChunk));
+    const RowShape shape = row_shape(static_cast<int>((C + kChunk - 1) / kChunk), kBwdOneWave);
     const int waves = shape.waves == 1 ? 4 : shape.waves;
     int64_t target = kBwdWaves / waves;
     if (target < 1) target = 1;

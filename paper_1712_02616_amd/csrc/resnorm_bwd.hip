@@ -28,19 +28,19 @@ struct RowRegs {
     typename ChunkOf<DT>::vec dr[K], du[K], r[K], h[K];
 };
 
-template <int DT, int K, bool POST, bool PRE>
-__device__ __forceinline__ void load_row(const ResnormBwdArgs& a, int64_t row, const int (&n)[K],
-                                         const int (&col)[K], RowRegs<DT, K>& x) {
+template <int DT, int K, int FILL, bool POST, bool PRE>
+__device__ __forceinline__ void load_row(const ResnormBwdArgs& a, int64_t row, const RowChunk (&c)[K],
+                                         RowRegs<DT, K>& x) {
     const int64_t base = row * a.C;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        if (a.dr) x.dr[k] = load_chunk<DT, kStream>(a.dr, base + col[k], n[k]);
+        if (a.dr) x.dr[k] = load_row_chunk<DT, kStream, FILL>(a.dr, base, c[k]);
         if constexpr (PRE) {
-            x.du[k] = load_chunk<DT, kStream>(a.du, base + col[k], n[k]);
-            x.r[k] = load_chunk<DT, kStream>(a.r, base + col[k], n[k]);
+            x.du[k] = load_row_chunk<DT, kStream, FILL>(a.du, base, c[k]);
+            x.r[k] = load_row_chunk<DT, kStream, FILL>(a.r, base, c[k]);
         }
         if constexpr (POST) {
-            if (a.h) x.h[k] = load_chunk<DT, kStream>(a.h, base + col[k], n[k]);
+            if (a.h) x.h[k] = load_row_chunk<DT, kStream, FILL>(a.h, base, c[k]);
         }
     }
 }
@@ -48,26 +48,28 @@ __device__ __forceinline__ void load_row(const ResnormBwdArgs& a, int64_t row, c
 // Adds up the block's columns' sums and leaves them at `out`: the threads of
 // one row at a time hold every column once; kRows waves add theirs in LDS.
 template <int K, bool ONE_WAVE, typename Put>
-__device__ __forceinline__ void flush(float (&acc)[K][kChunk], const int (&n)[K],
-                                      const int (&col)[K], float* lds, Put put) {
+__device__ __forceinline__ void flush(float (&acc)[K][kChunk], const RowChunk (&c)[K], float* lds, Put put) {
     if constexpr (ONE_WAVE) {
         const int w = threadIdx.x / kWave;
-        __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) lds[(w * kChunk + j) * kWave + lane_id()] = acc[0][j];
-        __syncthreads();
-        if (w == 0) {
+        for (int k = 0; k < K; ++k) {
+            __syncthreads();
 #pragma unroll
-            for (int j = 0; j < kChunk; ++j) {
-                float s = acc[0][j];
-                for (int i = 1; i < kRows; ++i) s += lds[(i * kChunk + j) * kWave + lane_id()];
-                acc[0][j] = s;
+            for (int j = 0; j < kChunk; ++j) lds[(w * kChunk + j) * kWave + lane_id()] = acc[k][j];
+            __syncthreads();
+            if (w == 0) {
+#pragma unroll
+                for (int j = 0; j < kChunk; ++j) {
+                    float s = acc[k][j];
+                    for (int i = 1; i < kRows; ++i) s += lds[(i * kChunk + j) * kWave + lane_id()];
+                    acc[k][j] = s;
+                }
+                put(c[k].n, c[k].col, acc[k]);
             }
-            put(0, n[0], col[0], acc[0]);
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < K; ++k) put(k, n[k], col[k], acc[k]);
+        for (int k = 0; k < K; ++k) put(c[k].n, c[k].col, acc[k]);
     }
 #pragma unroll
     for (int k = 0; k < K; ++k)
@@ -75,21 +77,23 @@ __device__ __forceinline__ void flush(float (&acc)[K][kChunk], const int (&n)[K]
         for (int j = 0; j < kChunk; ++j) acc[k][j] = 0.0f;
 }
 
-template <int DT, int K, bool ONE_WAVE, bool POST, bool PRE>
-__global__ __launch_bounds__(ONE_WAVE ? kRows * kWave : kMaxRowWaves * kWave)
-void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
+template <int DT, int K, bool ONE_WAVE, int FILL, bool POST, bool PRE, int THREADS>
+__global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
     __shared__ SumSlot slots[4];
+    if constexpr (!ONE_WAVE) clear_slots(slots, 4);
     __shared__ float lds[ONE_WAVE ? kRows * kWave * kChunk : 1];
     const int t = ONE_WAVE ? lane_id() : threadIdx.x, T = ONE_WAVE ? kWave : waves * kWave;
     const int first = ONE_WAVE ? threadIdx.x / kWave : 0;
-    constexpr int kStep = ONE_WAVE ? kRows : 1;
-    int n[K], col[K];
+    constexpr int kStep = ONE_WAVE ? kRows : 1, kAhead = THREADS > 512 ? 1 : 2;
+    RowChunk c[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int c = t + k * T;
-        n[k] = max(min(kChunk, a.C - c * kChunk), 0);
-        col[k] = c * kChunk;
-    }
+    for (int k = 0; k < K; ++k) c[k] = row_chunk<FILL>(t + k * T, a.C);
+    const auto vector = [&](const float* v, int k, float (&out)[kChunk]) {
+        widen<IABN_F32>(place_chunk<IABN_F32, FILL>(load_row_chunk<IABN_F32, kCached, FILL>(v, 0, c[k]), c[k]), out);
+    };
+    const auto values = [&](const typename ChunkOf<DT>::vec& v, int k, float (&out)[kChunk]) {
+        widen<DT>(place_chunk<DT, FILL>(v, c[k]), out);
+    };
     // The columns' sums: dw, db, dgate; dw', db'.
     float sw[POST ? K : 1][kChunk] = {}, sb[POST ? K : 1][kChunk] = {}, sg[POST ? K : 1][kChunk] = {};
     float tw[PRE ? K : 1][kChunk] = {}, tb[PRE ? K : 1][kChunk] = {};
@@ -100,7 +104,7 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
         for (int k = 0; k < K; ++k) {
 #pragma unroll
             for (int j = 0; j < kChunk; ++j) pre_w[k][j] = 1.0f;
-            if (a.pre_w) widen<IABN_F32>(load_chunk<IABN_F32, kCached>(a.pre_w, col[k], n[k]), pre_w[k]);
+            if (a.pre_w) vector(a.pre_w, k, pre_w[k]);
         }
     }
     if constexpr (POST) {
@@ -108,7 +112,7 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
         for (int k = 0; k < K; ++k) {
 #pragma unroll
             for (int j = 0; j < kChunk; ++j) post_w[k][j] = 1.0f;
-            if (a.post_w) widen<IABN_F32>(load_chunk<IABN_F32, kCached>(a.post_w, col[k], n[k]), post_w[k]);
+            if (a.post_w) vector(a.post_w, k, post_w[k]);
         }
     }
     const int64_t seg_rows = (a.split.group_rows + a.split.per_group - 1) / a.split.per_group;
@@ -120,29 +124,35 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
         const int64_t in_group = (seg - group * a.split.per_group) * seg_rows, at = group * a.split.group_rows;
         const int64_t lo = at + min(in_group, a.split.group_rows);
         const int64_t hi = at + min(in_group + seg_rows, a.split.group_rows);
-        RowRegs<DT, K> next;
-        if (lo + first < hi) load_row<DT, K, POST, PRE>(a, lo + first, n, col, next);
-        for (int64_t row = lo + first; row < hi; row += kStep) {
-            RowRegs<DT, K> x = next;
-            if (row + kStep < hi) load_row<DT, K, POST, PRE>(a, row + kStep, n, col, next);
+        // One row, which `x` holds; then the row `ahead` comes into x.
+        const auto row_of = [&](int64_t row, int64_t ahead, RowRegs<DT, K>& x) {
             float g[K][kChunk];
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                if (a.dr) widen<DT>(x.dr[k], g[k]);
+                if (a.dr) values(x.dr[k], k, g[k]);
                 else
 #pragma unroll
                     for (int j = 0; j < kChunk; ++j) g[k][j] = 0.0f;
             }
+            typename ChunkOf<DT>::vec raw_h[POST ? K : 1];
+            float rhat[PRE ? K : 1][kChunk], rdu[PRE ? K : 1][kChunk];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                if constexpr (POST) raw_h[k] = x.h[k];
+                if constexpr (PRE) {
+                    values(x.r[k], k, rhat[k]);
+                    values(x.du[k], k, rdu[k]);
+                }
+            }
+            if (ahead < hi) load_row<DT, K, FILL, POST, PRE>(a, ahead, c, x);
             if constexpr (PRE) {
                 const float mean = a.pre_stats[row], rstd = a.pre_stats[a.R + row];
-                float hat[K][kChunk], d[K][kChunk], s1 = 0.0f, s2 = 0.0f;
+                float (&hat)[K][kChunk] = rhat, (&d)[K][kChunk] = rdu, s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    widen<DT>(x.r[k], hat[k]);
-                    widen<DT>(x.du[k], d[k]);
 #pragma unroll
                     for (int j = 0; j < kChunk; ++j) {
-                        hat[k][j] = j < n[k] ? (hat[k][j] - mean) * rstd : 0.0f;
+                        hat[k][j] = inside_row<FILL>(c[k], j, (hat[k][j] - mean) * rstd);
                         tw[k][j] = fmaf(d[k][j], hat[k][j], tw[k][j]);
                         tb[k][j] += d[k][j];
                         d[k][j] *= pre_w[k][j];
@@ -150,7 +160,7 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
                         s2 = fmaf(d[k][j], hat[k][j], s2);
                     }
                 }
-                row_sum2<ONE_WAVE>(s1, s2, slots[par], waves);
+                row_sum2<ONE_WAVE>(s1, s2, slots[par]);
                 s1 = a.pre == IABN_NORM_LAYER ? s1 * a.inv_c : 0.0f;
                 s2 *= a.inv_c;
 #pragma unroll
@@ -166,7 +176,7 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
                     float o[kChunk];
 #pragma unroll
                     for (int j = 0; j < kChunk; ++j) o[j] = a.alpha * g[k][j];
-                    store_chunk<DT, kStream>(a.dx, base + col[k], n[k], o);
+                    store_row_chunk<DT, kStream, FILL>(a.dx, base, c[k], o);
                 }
             }
             if constexpr (POST) {
@@ -177,20 +187,19 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
                 }
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    if (a.h) widen<DT>(x.h[k], hat[k]);
+                    if (a.h) values(raw_h[k], k, hat[k]);
                     // From here g is e = beta*g*D, then dn, then dn*w.
 #pragma unroll
                     for (int j = 0; j < kChunk; ++j) {
-                        hat[k][j] = a.h && j < n[k] ? (hat[k][j] - mean) * rstd : 0.0f;
-                        g[k][j] = j < n[k] ? a.beta * g[k][j] : 0.0f;
+                        hat[k][j] = a.h ? inside_row<FILL>(c[k], j, (hat[k][j] - mean) * rstd) : 0.0f;
+                        g[k][j] = inside_row<FILL>(c[k], j, a.beta * g[k][j]);
                     }
                     if (a.drop.threshold)
-                        drop_group(a.drop, static_cast<uint64_t>(row * a.chunks + col[k] / kChunk), g[k]);
+                        drop_group(a.drop, static_cast<uint64_t>(row * a.chunks + c[k].col / kChunk), g[k]);
                     if (a.gate) {
                         float gv[kChunk], o[kChunk], bv[kChunk] = {};
-                        widen<DT>(load_chunk<DT, kCached>(a.gate, row / a.gate_rows * a.C + col[k], n[k]), gv);
-                        if (a.post_b)
-                            widen<IABN_F32>(load_chunk<IABN_F32, kCached>(a.post_b, col[k], n[k]), bv);
+                        values(load_row_chunk<DT, kCached, FILL>(a.gate, row / a.gate_rows * a.C, c[k]), k, gv);
+                        if (a.post_b) vector(a.post_b, k, bv);
 #pragma unroll
                         for (int j = 0; j < kChunk; ++j) {
                             o[j] = g[k][j] * fmaf(hat[k][j], post_w[k][j], bv[j]);
@@ -198,7 +207,7 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
                             g[k][j] *= gv[j];
                         }
                         if (a.dgate && a.gate_each_row)
-                            store_chunk<DT, kStream>(a.dgate, base + col[k], n[k], o);
+                            store_row_chunk<DT, kStream, FILL>(a.dgate, base, c[k], o);
                     }
                     if (a.post != IABN_NORM_NONE) {
 #pragma unroll
@@ -212,7 +221,7 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
                     }
                 }
                 if (a.post != IABN_NORM_NONE) {
-                    row_sum2<ONE_WAVE>(s1, s2, slots[2 + par], waves);
+                    row_sum2<ONE_WAVE>(s1, s2, slots[2 + par]);
                     s1 = a.post == IABN_NORM_LAYER ? s1 * a.inv_c : 0.0f;
                     s2 *= a.inv_c;
 #pragma unroll
@@ -223,14 +232,24 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
                 }
                 if (a.dh)
 #pragma unroll
-                    for (int k = 0; k < K; ++k) store_chunk<DT, kStream>(a.dh, base + col[k], n[k], g[k]);
+                    for (int k = 0; k < K; ++k) store_row_chunk<DT, kStream, FILL>(a.dh, base, c[k], g[k]);
             }
             par ^= 1;
-        }
+        };
+        // kAhead rows are on their way while one is worked on.
+        RowRegs<DT, K> x[kAhead];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+            if (lo + first + q * kStep < hi)
+                load_row<DT, K, FILL, POST, PRE>(a, lo + first + q * kStep, c, x[q]);
+        for (int64_t row = lo + first; row < hi; row += kAhead * kStep)
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+                if (row + q * kStep < hi) row_of(row + q * kStep, row + (q + kAhead) * kStep, x[q]);
         if constexpr (POST) {
             if (a.dgate && !a.gate_each_row) {
                 const int64_t out = (a.split.per_group == 1 ? group : int64_t(blockIdx.x)) * a.C;
-                flush<K, ONE_WAVE>(sg, n, col, lds, [&](int, int m, int c, float (&v)[kChunk]) {
+                flush<K, ONE_WAVE>(sg, c, lds, [&](int m, int c, float (&v)[kChunk]) {
                     if (a.split.per_group == 1) store_chunk<DT, kStream>(a.dgate, out + c, m, v);
                     else store_chunk<IABN_F32, kCached>(a.gpart, out + c, m, v);
                 });
@@ -238,17 +257,17 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
         }
     }
     const auto put = [&](int which) {
-        return [=](int, int m, int c, float (&v)[kChunk]) {
+        return [=](int m, int c, float (&v)[kChunk]) {
             store_chunk<IABN_F32, kCached>(a.part, (int64_t(which) * a.split.blocks + blockIdx.x) * a.C + c, m, v);
         };
     };
     if constexpr (POST) {
-        if (a.dpost_w) flush<K, ONE_WAVE>(sw, n, col, lds, put(0));
-        if (a.dpost_b) flush<K, ONE_WAVE>(sb, n, col, lds, put(1));
+        if (a.dpost_w) flush<K, ONE_WAVE>(sw, c, lds, put(0));
+        if (a.dpost_b) flush<K, ONE_WAVE>(sb, c, lds, put(1));
     }
     if constexpr (PRE) {
-        if (a.dpre_w) flush<K, ONE_WAVE>(tw, n, col, lds, put(2));
-        if (a.dpre_b) flush<K, ONE_WAVE>(tb, n, col, lds, put(3));
+        if (a.dpre_w) flush<K, ONE_WAVE>(tw, c, lds, put(2));
+        if (a.dpre_b) flush<K, ONE_WAVE>(tb, c, lds, put(3));
     }
 }
 
@@ -293,16 +312,31 @@ __global__ __launch_bounds__(kThreads) void resnorm_bwd_sum_kernel(ResnormBwdArg
     }
 }
 
+template <int DT, int FILL, bool POST, bool PRE>
+void launch_filled(const ResnormBwdArgs& a, const RowShape& s, hipStream_t st) {
+    const dim3 grid(static_cast<uint32_t>(a.split.blocks));
+    const int threads = s.waves == 1 ? kRows * kWave : s.waves * kWave;
+    // (The registers of a thread follow from the most threads that a block may have.)
+    if (s.waves == 1)
+        resnorm_bwd_kernel<DT, 1, true, FILL, POST, PRE, kRows * kWave><<<grid, threads, 0, st>>>(a, 1);
+    else if constexpr (FILL != kShort) {
+        if (s.waves <= 4)
+            resnorm_bwd_kernel<DT, 1, false, FILL, POST, PRE, 256><<<grid, threads, 0, st>>>(a, s.waves);
+        else if (s.waves <= 8)
+            resnorm_bwd_kernel<DT, 1, false, FILL, POST, PRE, 512><<<grid, threads, 0, st>>>(a, s.waves);
+        else if (s.k == 1)
+            resnorm_bwd_kernel<DT, 1, false, FILL, POST, PRE, 1024><<<grid, threads, 0, st>>>(a, s.waves);
+        else
+            resnorm_bwd_kernel<DT, 2, false, FILL, POST, PRE, 1024><<<grid, threads, 0, st>>>(a, s.waves);
+    }
+}
+
 template <int DT, bool POST, bool PRE>
 void launch_rows(const ResnormBwdArgs& a, hipStream_t st) {
-    const RowShape s = row_shape(a.chunks);
-    const dim3 grid(static_cast<uint32_t>(a.split.blocks));
-    if (s.waves == 1)
-        resnorm_bwd_kernel<DT, 1, true, POST, PRE><<<grid, kRows * kWave, 0, st>>>(a, 1);
-    else if (s.k == 1)
-        resnorm_bwd_kernel<DT, 1, false, POST, PRE><<<grid, s.waves * kWave, 0, st>>>(a, s.waves);
-    else
-        resnorm_bwd_kernel<DT, 2, false, POST, PRE><<<grid, s.waves * kWave, 0, st>>>(a, s.waves);
+    const RowShape s = row_shape(a.chunks, kBwdOneWave);
+    if (a.C < kChunk) launch_filled<DT, kShort, POST, PRE>(a, s, st);
+    else if (a.C == s.waves * s.k * kWave * kChunk) launch_filled<DT, kFull, POST, PRE>(a, s, st);
+    else launch_filled<DT, kPartial, POST, PRE>(a, s, st);
 }
 
 template <int DT>

@@ -72,6 +72,62 @@ __device__ __forceinline__ void widen(const typename ChunkOf<DT>::vec& v, float 
     for (int j = 0; j < kChunk; ++j) f[j] = w[j];
 }
 
+// The chunks of a row over the threads that hold it.  A load under a branch is
+// waited for where the branches join, so where a row does not fill its threads
+// (kPartial) every thread loads 8 elements of it whatever it has of them, the
+// last 8 where its chunk ends beyond the row, and they are put in their place
+// when they are used (place_chunk).  kFull: every thread has a whole chunk, and
+// nothing is masked; kShort: rows of fewer than 8 elements, one by one.
+enum RowFill { kFull, kPartial, kShort };
+
+struct RowChunk {
+    int col;   // the chunk's first element
+    int from;  // the first element to load
+    int n;     // elements inside the row (0 for a thread that has none)
+};
+template <int FILL>
+__device__ __forceinline__ RowChunk row_chunk(int chunk, int C) {
+    const int col = chunk * kChunk;
+    if constexpr (FILL == kFull) return {col, col, kChunk};
+    return {col, FILL == kShort ? col : min(col, C - kChunk), max(min(kChunk, C - col), 0)};
+}
+template <int DT, int HINT, int FILL>
+__device__ __forceinline__ typename ChunkOf<DT>::vec load_row_chunk(const void* __restrict__ base,
+                                                                    int64_t row, const RowChunk& c) {
+    return load_chunk<DT, HINT>(base, row + c.from, FILL == kShort ? c.n : kChunk);
+}
+template <int DT, int HINT, int FILL>
+__device__ __forceinline__ void store_row_chunk(void* __restrict__ base, int64_t row, const RowChunk& c,
+                                                const float (&v)[kChunk]) {
+    store_chunk<DT, HINT>(base, row + c.col, FILL == kFull ? kChunk : c.n, v);
+}
+
+// The loaded elements in their place: those before the chunk's leave, zeros
+// follow the row's last.  A shift by 8 - n elements, in steps of 8, 4, 2 and 1.
+template <int DT, int FILL>
+__device__ __forceinline__ typename ChunkOf<DT>::vec place_chunk(typename ChunkOf<DT>::vec v,
+                                                                 const RowChunk& c) {
+    if constexpr (FILL != kPartial) return v;
+    const int shift = kChunk - c.n;
+    typename ChunkOf<DT>::vec w;
+#pragma unroll
+    for (int step = kChunk; step >= 1; step >>= 1) {
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) {
+            const auto moved = j + step < kChunk ? v[j + step < kChunk ? j + step : 0]
+                                                 : static_cast<typename ChunkOf<DT>::T>(0.0f);
+            w[j] = shift & step ? moved : v[j];
+        }
+        v = w;
+    }
+    return v;
+}
+// v where it is inside the row, else 0.
+template <int FILL>
+__device__ __forceinline__ float inside_row(const RowChunk& c, int j, float v) {
+    return FILL == kFull || j < c.n ? v : 0.0f;
+}
+
 // ---------------------------------------------------------------- sums
 
 template <int CTRL, int ROW_MASK>
@@ -95,16 +151,45 @@ __device__ __forceinline__ float wave_sum_f32(float v) {
 
 constexpr int kMaxRowWaves = 16;
 
-// Two sums over the waves of a row's threads, each in a fixed order, in every
-// thread.  One wave needs no more than its DPP steps.  More waves exchange
+// One or two sums over the waves of a row's threads, each in a fixed order, in
+// every thread.  One wave needs no more than its DPP steps.  More waves exchange
 // their sums through `slot`, with one barrier: consecutive sums of a block
 // have to use different slots, and a slot may come again after one other.
 struct alignas(8) SumSlot {
     float a[kMaxRowWaves], b[kMaxRowWaves];
 };
 
+// Sum over each row of 16 lanes, in its lane 15, read from the first row.
+__device__ __forceinline__ float row16_sum_f32(float v) {
+    v += dpp_f32<0x111, 0xF>(v);
+    v += dpp_f32<0x112, 0xF>(v);
+    v += dpp_f32<0x114, 0xF>(v);
+    v += dpp_f32<0x118, 0xF>(v);
+    return __builtin_bit_cast(float,
+                              __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 15));
+}
+
+// Before a block's first row_sum2 (with a barrier between): the places of
+// waves that the block does not have.
+__device__ __forceinline__ void clear_slots(SumSlot* slots, int n) {
+    for (int i = threadIdx.x; i < n * 2 * kMaxRowWaves; i += blockDim.x)
+        reinterpret_cast<float*>(slots)[i] = 0.0f;
+    __syncthreads();
+}
+
 template <bool ONE_WAVE>
-__device__ __forceinline__ void row_sum2(float& a, float& b, SumSlot& slot, int waves) {
+__device__ __forceinline__ float row_sum(float a, SumSlot& slot) {
+    a = wave_sum_f32(a);
+    if constexpr (!ONE_WAVE) {
+        if (lane_id() == 0) slot.a[threadIdx.x / kWave] = a;
+        __syncthreads();
+        a = row16_sum_f32(slot.a[lane_id() % kMaxRowWaves]);
+    }
+    return a;
+}
+
+template <bool ONE_WAVE>
+__device__ __forceinline__ void row_sum2(float& a, float& b, SumSlot& slot) {
     a = wave_sum_f32(a);
     b = wave_sum_f32(b);
     if constexpr (!ONE_WAVE) {
@@ -114,11 +199,8 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, SumSlot& slot, int 
             slot.b[w] = b;
         }
         __syncthreads();
-        a = b = 0.0f;
-        for (int i = 0; i < waves; ++i) {
-            a += slot.a[i];
-            b += slot.b[i];
-        }
+        a = row16_sum_f32(slot.a[lane_id() % kMaxRowWaves]);
+        b = row16_sum_f32(slot.b[lane_id() % kMaxRowWaves]);
     }
 }
 
@@ -229,9 +311,15 @@ bool launch_resnorm_bwd(int dtype, const ResnormBwdArgs& a, hipStream_t st);
 struct RowShape {
     int waves, k;
 };
-inline RowShape row_shape(int chunks) {
+// one_wave: the most chunks of a thread for which a row stays in one wave.
+inline RowShape row_shape(int chunks, int one_wave) {
+    for (int k = 1; k <= one_wave; ++k)
+        if (chunks <= k * kWave) return {1, k};
     const int k = chunks <= kMaxRowWaves * kWave ? 1 : 2;
     return {(chunks + k * kWave - 1) / (k * kWave), k};
 }
+
+// (measured: see the kernels)
+constexpr int kFwdOneWave = 2, kBwdOneWave = 1;
 
 }  // namespace iabn_impl
