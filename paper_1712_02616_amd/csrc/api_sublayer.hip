@@ -52,16 +52,18 @@ int check_gate(const void* gate, int64_t groups, int64_t R) {
 // How the backward's rows go over its blocks.  Enough blocks to fill the
 // chip, few enough that their columns' sums (4 or 5 vectors of C floats,
 // written and read once) stay small against the rows: a block takes at least
-// kMinRows of them.
-constexpr int64_t kBwdWaves = 2048;
-constexpr int64_t kBwdMinRows = 8;
+// kBwdMinRows of them, or two while there are fewer blocks than CUs ((1031,
+// 1501) fp32: 30.6 us with 8, 22.3 with 4, 25.4 with 2; (512, 1024) fp16 14.0,
+// 9.1, 7.2).
+constexpr int64_t kCUs = 256, kBwdWavesPerCU = 12;
+constexpr int64_t kBwdMinRows = 4;
 
 ResnormSplit split_rows(int64_t R, int64_t C, int64_t groups) {
     if (R == 0) return {1, 0, 0, 0, 0};
     const RowShape shape = row_shape(static_cast<int>((C + kChunk - 1) / kChunk), kBwdOneWave);
-    const int waves = shape.waves == 1 ? 4 : shape.waves;
-    int64_t target = kBwdWaves / waves;
-    if (target < 1) target = 1;
+    // (A block of one-wave rows has four of them, and 180 registers.)
+    const int64_t on_cu = shape.waves == 1 ? 2 : kBwdWavesPerCU / shape.waves;
+    const int64_t target = kCUs * (on_cu > 1 ? on_cu : 1);
     ResnormSplit s;
     s.groups = groups > 0 && groups < R ? groups : 1;
     s.group_rows = R / s.groups;
@@ -70,9 +72,11 @@ ResnormSplit split_rows(int64_t R, int64_t C, int64_t groups) {
         s.segs = static_cast<int>((s.groups + target - 1) / target);
         s.blocks = static_cast<int>((s.groups + s.segs - 1) / s.segs);
     } else {
+        const int64_t fewest = kCUs / s.groups, two = (s.group_rows + 1) / 2;
         const int64_t most = (s.group_rows + kBwdMinRows - 1) / kBwdMinRows;
         int64_t per = target / s.groups;
         if (per > most) per = most;
+        if (per < fewest) per = fewest < two ? fewest : two;
         s.per_group = static_cast<int>(per);
         s.segs = 1;
         s.blocks = static_cast<int>(s.groups * per);

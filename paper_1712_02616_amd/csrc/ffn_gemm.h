@@ -214,39 +214,26 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
     f32x4 acc[NM][NN] = {};
     SX sx;
     SY sy;
-    const auto multiply = [&](const char* __restrict__ cur) {
-        if constexpr (NM * NN <= 16) {
-            // One or two waves of a SIMD have to keep it busy: every read of
-            // the step is under way before its first product.
-            u32x4 fy[kSteps][NN], fx[kSteps][NM];
+    // A step goes in phases, each of one half of K and (in the largest tile) one
+    // half of a wave's rows of x: its fragments, and their products.
+    constexpr bool kAhead = NM * NN > 16;
+    constexpr int kHalves = kAhead ? 2 : 1, kPhases = kSteps * kHalves, NH = NM / kHalves;
+    u32x4 fy[kSteps][NN], fx[2][NH];
+    const auto read = [&](const char* __restrict__ buf, int phase) __attribute__((always_inline)) {
+        const int s = phase / kHalves, h = phase % kHalves;
+        if (h == 0)
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
+            for (int j = 0; j < NN; ++j) fy[s][j] = SY::frag(buf + SX::kBytes, wn + j * 16, s);
 #pragma unroll
-                for (int j = 0; j < NN; ++j) fy[s][j] = SY::frag(cur + SX::kBytes, wn + j * 16, s);
+        for (int i = 0; i < NH; ++i) fx[phase & 1][i] = SX::frag(buf, wm + (h * NH + i) * 16, s);
+    };
+    const auto products = [&](int phase) __attribute__((always_inline)) {
+        const int s = phase / kHalves, h = phase % kHalves;
 #pragma unroll
-                for (int i = 0; i < NM; ++i) fx[s][i] = SX::frag(cur, wm + i * 16, s);
-            }
-            __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < NH; ++i)
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-                for (int i = 0; i < NM; ++i)
-#pragma unroll
-                    for (int j = 0; j < NN; ++j) acc[i][j] = Mma<DT>::run(fy[s][j], fx[s][i], acc[i][j]);
-            return;
-        }
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            u32x4 fy[NN];
-#pragma unroll
-            for (int j = 0; j < NN; ++j) fy[j] = SY::frag(cur + SX::kBytes, wn + j * 16, s);
-#pragma unroll
-            for (int i = 0; i < NM; ++i) {
-                const u32x4 fx = SX::frag(cur, wm + i * 16, s);
-#pragma unroll
-                for (int j = 0; j < NN; ++j) acc[i][j] = Mma<DT>::run(fy[j], fx, acc[i][j]);
-            }
-        }
+            for (int j = 0; j < NN; ++j)
+                acc[h * NH + i][j] = Mma<DT>::run(fy[s][j], fx[phase & 1][i], acc[h * NH + i][j]);
     };
     // Steps of K: whole ones that go straight to LDS, those of the first
     // product and then those of the second, and the others, through
@@ -259,46 +246,86 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
     const int lo = min(begin, steps), hi = min(end, steps);
     const int from = max(begin - steps, 0), to = max(end - steps, 0);
     if constexpr (DMA) {
-        const auto fetch = [&](int kt, char* buf) {
+        const auto fetch = [&](int kt, char* buf) __attribute__((always_inline)) {
             const int seg = Kind::kSegs > 1 ? (kt >= whole ? 1 : 0) : z;
             const int64_t k0 = int64_t(Kind::kSegs > 1 && seg ? kt - whole : kt) * BK;
             sx.fetch(a.x, seg, k0, buf);
             sy.fetch(a.y, seg, k0, buf + SX::kBytes);
         };
-        // Step kt from `cur`: what is fetched there has arrived when each wave
-        // has waited for its own fetches and all have met; then `free` may be
-        // filled, whose reads have ended (each wave has waited for its own).
-        const auto turn = [&](int kt, const char* __restrict__ cur, char* __restrict__ free) {
+        // At `meet` what was fetched has arrived (each wave has waited for its
+        // own) and the reads of the buffer to be filled next have ended.  The
+        // largest tile, alone on its CU, has the matrix cores at work on both
+        // sides of it: the fragments of a phase are read while the one before is
+        // multiplied, those of the next step's first phase while this one's last
+        // is ((4096, 2048 -> 2x8192) bf16 250 -> 245 us, the products of two
+        // sums (8192, 2x10240 -> 4096) 1032 -> 1002).  Of the smaller ones two
+        // or more share a CU; there every read of a step before its first
+        // product is better ((4096, 1024) fp16 weights' gradients of 2085 tokens
+        // 37 us against 40).
+        const auto meet = []() __attribute__((always_inline)) {
             __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            if (kt + 1 < hi) fetch(kt + 1, free);
-            multiply(cur);
+        };
+        const auto turn = [&](int kt, char* __restrict__ cur, char* __restrict__ next) __attribute__((always_inline)) {
+            if constexpr (kAhead) {
+#pragma unroll
+                for (int p = 0; p + 1 < kPhases; ++p) {
+                    read(cur, p + 1);
+                    products(p);
+                    __builtin_amdgcn_sched_barrier(0);  // (products stay on their side)
+                }
+                meet();
+                if (kt + 2 < hi) fetch(kt + 2, cur);
+                if (kt + 1 < hi) read(next, 0);
+                products(kPhases - 1);
+                __builtin_amdgcn_sched_barrier(0);
+            } else {
+                meet();
+                if (kt + 1 < hi) fetch(kt + 1, next);
+#pragma unroll
+                for (int p = 0; p < kPhases; ++p) read(cur, p);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int p = 0; p < kPhases; ++p) products(p);
+            }
         };
         // (The buffers are told apart, restrict, so that the compiler does not
         // make the reads of one wait for what arrives in the other.)
-        const auto round = [&](int kt, char* __restrict__ b0, char* __restrict__ b1) {
+        const auto round = [&](int kt, char* __restrict__ b0, char* __restrict__ b1) __attribute__((always_inline)) {
             turn(kt, b0, b1);
             if (kt + 1 < hi) turn(kt + 1, b1, b0);
         };
         sx.prepare(a.x, m0, a.M - m0);
         sy.prepare(a.y, n0, a.N - n0);
         if (lo < hi) fetch(lo, lds0);
+        if (kAhead && lo < hi) {
+            meet();
+            if (lo + 1 < hi) fetch(lo + 1, lds1);
+            read(lds0, 0);
+        }
         for (int kt = lo; kt < hi; kt += 2) round(kt, lds0, lds1);
         __syncthreads();
     }
     if (from < to) {
-        const auto load = [&](int kt) {
+        const auto load = [&](int kt) __attribute__((always_inline)) {
             const int seg = Kind::kSegs > 1 ? (kt >= per_seg ? 1 : 0) : z;
             const int64_t k0 = int64_t(whole + (Kind::kSegs > 1 && seg ? kt - per_seg : kt)) * BK;
             sx.load(a.x, seg, m0, a.M - m0, k0, a.K);
             sy.load(a.y, seg, n0, a.N - n0, k0, a.K);
         };
-        const auto store = [&](char* buf) {
+        const auto store = [&](char* buf) __attribute__((always_inline)) {
             sx.store(buf);
             sy.store(buf + SX::kBytes);
             __syncthreads();
+        };
+        const auto multiply = [&](const char* buf) __attribute__((always_inline)) {
+#pragma unroll
+            for (int p = 0; p < kPhases; ++p) {
+                read(buf, p);
+                products(p);
+            }
         };
         load(from);
         store(lds0);

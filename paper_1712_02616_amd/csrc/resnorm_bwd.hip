@@ -84,7 +84,7 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(ResnormBwdArgs a, 
     __shared__ float lds[ONE_WAVE ? kRows * kWave * kChunk : 1];
     const int t = ONE_WAVE ? lane_id() : threadIdx.x, T = ONE_WAVE ? kWave : waves * kWave;
     const int first = ONE_WAVE ? threadIdx.x / kWave : 0;
-    constexpr int kStep = ONE_WAVE ? kRows : 1, kAhead = THREADS > 512 ? 1 : 2;
+    constexpr int kStep = ONE_WAVE ? kRows : 1;
     RowChunk c[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) c[k] = row_chunk<FILL>(t + k * T, a.C);
@@ -117,6 +117,8 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(ResnormBwdArgs a, 
     }
     const int64_t seg_rows = (a.split.group_rows + a.split.per_group - 1) / a.split.per_group;
     int par = 0;  // alternates the slots of consecutive rows
+    Dropout dropped = a.drop;
+    dropped.scale *= a.beta;
 
     for (int s = 0; s < a.split.segs; ++s) {
         const int64_t seg = int64_t(blockIdx.x) * a.split.segs + s, group = seg / a.split.per_group;
@@ -124,8 +126,9 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(ResnormBwdArgs a, 
         const int64_t in_group = (seg - group * a.split.per_group) * seg_rows, at = group * a.split.group_rows;
         const int64_t lo = at + min(in_group, a.split.group_rows);
         const int64_t hi = at + min(in_group + seg_rows, a.split.group_rows);
-        // One row, which `x` holds; then the row `ahead` comes into x.
-        const auto row_of = [&](int64_t row, int64_t ahead, RowRegs<DT, K>& x) {
+        RowRegs<DT, K> x;
+        if (lo + first < hi) load_row<DT, K, FILL, POST, PRE>(a, lo + first, c, x);
+        for (int64_t row = lo + first; row < hi; row += kStep) {
             float g[K][kChunk];
 #pragma unroll
             for (int k = 0; k < K; ++k) {
@@ -144,30 +147,47 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(ResnormBwdArgs a, 
                     values(x.du[k], k, rdu[k]);
                 }
             }
-            if (ahead < hi) load_row<DT, K, FILL, POST, PRE>(a, ahead, c, x);
+            // The next row is on its way while this one is worked on.
+            if (row + kStep < hi) load_row<DT, K, FILL, POST, PRE>(a, row + kStep, c, x);
             if constexpr (PRE) {
                 const float mean = a.pre_stats[row], rstd = a.pre_stats[a.R + row];
                 float (&hat)[K][kChunk] = rhat, (&d)[K][kChunk] = rdu, s1 = 0.0f, s2 = 0.0f;
+                if (a.dpre_b) {
+#pragma unroll
+                    for (int k = 0; k < K; ++k)
+#pragma unroll
+                        for (int j = 0; j < kChunk; ++j) tb[k][j] += d[k][j];
+                }
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
 #pragma unroll
                     for (int j = 0; j < kChunk; ++j) {
-                        hat[k][j] = inside_row<FILL>(c[k], j, (hat[k][j] - mean) * rstd);
+                        hat[k][j] = inside_row<FILL>(c[k], j, fmaf(hat[k][j], rstd, -mean * rstd));
                         tw[k][j] = fmaf(d[k][j], hat[k][j], tw[k][j]);
-                        tb[k][j] += d[k][j];
                         d[k][j] *= pre_w[k][j];
-                        s1 += d[k][j];
                         s2 = fmaf(d[k][j], hat[k][j], s2);
                     }
                 }
-                row_sum2<ONE_WAVE>(s1, s2, slots[par]);
-                s1 = a.pre == IABN_NORM_LAYER ? s1 * a.inv_c : 0.0f;
-                s2 *= a.inv_c;
+                if (a.pre == IABN_NORM_LAYER) {
+#pragma unroll
+                    for (int k = 0; k < K; ++k)
+#pragma unroll
+                        for (int j = 0; j < kChunk; ++j) s1 += d[k][j];
+                    row_sum2<ONE_WAVE>(s1, s2, slots[par]);
+                    s1 *= -rstd * a.inv_c;
+#pragma unroll
+                    for (int k = 0; k < K; ++k)
+#pragma unroll
+                        for (int j = 0; j < kChunk; ++j) g[k][j] += s1;
+                } else {
+                    s2 = row_sum<ONE_WAVE>(s2, slots[par]);
+                }
+                s2 *= -rstd * a.inv_c;
 #pragma unroll
                 for (int k = 0; k < K; ++k)
 #pragma unroll
                     for (int j = 0; j < kChunk; ++j)
-                        g[k][j] = fmaf(rstd, d[k][j] - s1 - hat[k][j] * s2, g[k][j]);
+                        g[k][j] = fmaf(rstd, d[k][j], fmaf(s2, hat[k][j], g[k][j]));
             }
             const int64_t base = row * a.C;
             if (a.dx) {
@@ -191,11 +211,14 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(ResnormBwdArgs a, 
                     // From here g is e = beta*g*D, then dn, then dn*w.
 #pragma unroll
                     for (int j = 0; j < kChunk; ++j) {
-                        hat[k][j] = a.h ? inside_row<FILL>(c[k], j, (hat[k][j] - mean) * rstd) : 0.0f;
-                        g[k][j] = inside_row<FILL>(c[k], j, a.beta * g[k][j]);
+                        hat[k][j] = a.h ? inside_row<FILL>(c[k], j, fmaf(hat[k][j], rstd, -mean * rstd)) : 0.0f;
+                        if constexpr (FILL != kFull) g[k][j] = inside_row<FILL>(c[k], j, g[k][j]);
                     }
                     if (a.drop.threshold)
-                        drop_group(a.drop, static_cast<uint64_t>(row * a.chunks + c[k].col / kChunk), g[k]);
+                        drop_group(dropped, static_cast<uint64_t>(row * a.chunks + c[k].col / kChunk), g[k]);
+                    else
+#pragma unroll
+                        for (int j = 0; j < kChunk; ++j) g[k][j] *= a.beta;
                     if (a.gate) {
                         float gv[kChunk], o[kChunk], bv[kChunk] = {};
                         values(load_row_chunk<DT, kCached, FILL>(a.gate, row / a.gate_rows * a.C, c[k]), k, gv);
@@ -210,42 +233,42 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(ResnormBwdArgs a, 
                             store_row_chunk<DT, kStream, FILL>(a.dgate, base, c[k], o);
                     }
                     if (a.post != IABN_NORM_NONE) {
+                        if (a.dpost_b) {
+#pragma unroll
+                            for (int j = 0; j < kChunk; ++j) sb[k][j] += g[k][j];
+                        }
 #pragma unroll
                         for (int j = 0; j < kChunk; ++j) {
                             sw[k][j] = fmaf(g[k][j], hat[k][j], sw[k][j]);
-                            sb[k][j] += g[k][j];
                             g[k][j] *= post_w[k][j];
-                            s1 += g[k][j];
                             s2 = fmaf(g[k][j], hat[k][j], s2);
                         }
                     }
                 }
                 if (a.post != IABN_NORM_NONE) {
-                    row_sum2<ONE_WAVE>(s1, s2, slots[2 + par]);
-                    s1 = a.post == IABN_NORM_LAYER ? s1 * a.inv_c : 0.0f;
-                    s2 *= a.inv_c;
+                    if (a.post == IABN_NORM_LAYER) {
+#pragma unroll
+                        for (int k = 0; k < K; ++k)
+#pragma unroll
+                            for (int j = 0; j < kChunk; ++j) s1 += g[k][j];
+                        row_sum2<ONE_WAVE>(s1, s2, slots[2 + par]);
+                    } else {
+                        s2 = row_sum<ONE_WAVE>(s2, slots[2 + par]);
+                    }
+                    s1 *= -rstd * a.inv_c;
+                    s2 *= -rstd * a.inv_c;
 #pragma unroll
                     for (int k = 0; k < K; ++k)
 #pragma unroll
                         for (int j = 0; j < kChunk; ++j)
-                            g[k][j] = rstd * (g[k][j] - s1 - hat[k][j] * s2);
+                            g[k][j] = fmaf(s2, hat[k][j], fmaf(rstd, g[k][j], s1));
                 }
                 if (a.dh)
 #pragma unroll
                     for (int k = 0; k < K; ++k) store_row_chunk<DT, kStream, FILL>(a.dh, base, c[k], g[k]);
             }
             par ^= 1;
-        };
-        // kAhead rows are on their way while one is worked on.
-        RowRegs<DT, K> x[kAhead];
-#pragma unroll
-        for (int q = 0; q < kAhead; ++q)
-            if (lo + first + q * kStep < hi)
-                load_row<DT, K, FILL, POST, PRE>(a, lo + first + q * kStep, c, x[q]);
-        for (int64_t row = lo + first; row < hi; row += kAhead * kStep)
-#pragma unroll
-            for (int q = 0; q < kAhead; ++q)
-                if (row + q * kStep < hi) row_of(row + q * kStep, row + (q + kAhead) * kStep, x[q]);
+        }
         if constexpr (POST) {
             if (a.dgate && !a.gate_each_row) {
                 const int64_t out = (a.split.per_group == 1 ? group : int64_t(blockIdx.x)) * a.C;

@@ -68,6 +68,8 @@ __global__ __launch_bounds__(THREADS) void resnorm_fwd_kernel(ResnormArgs a, int
     RowChunk c[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) c[k] = row_chunk<FILL>(t + k * T, a.C);
+    Dropout dropped = a.drop;
+    dropped.scale *= a.beta;
     for (int64_t row = ONE_WAVE ? int64_t(blockIdx.x) * kRows + threadIdx.x / kWave : blockIdx.x;
          row < a.R; row += int64_t(gridDim.x) * (ONE_WAVE ? kRows : 1)) {
         const int64_t base = row * a.C;
@@ -98,16 +100,22 @@ __global__ __launch_bounds__(THREADS) void resnorm_fwd_kernel(ResnormArgs a, int
             widen<DT>(place_chunk<DT, FILL>(xr[k], c[k]), xv);
             if (a.h) {
                 if (a.drop.threshold)
-                    drop_group(a.drop, static_cast<uint64_t>(row * a.chunks + c[k].col / kChunk), v[k]);
+                    drop_group(dropped, static_cast<uint64_t>(row * a.chunks + c[k].col / kChunk), v[k]);
+                else
+#pragma unroll
+                    for (int j = 0; j < kChunk; ++j) v[k][j] *= a.beta;
                 if (a.gate) {
                     float gv[kChunk];
                     widen<DT>(place_chunk<DT, FILL>(gr[k], c[k]), gv);
 #pragma unroll
-                    for (int j = 0; j < kChunk; ++j) v[k][j] *= gv[j];
-                }
+                    for (int j = 0; j < kChunk; ++j) v[k][j] = fmaf(v[k][j], gv[j], a.alpha * xv[j]);
+                } else {
 #pragma unroll
-                for (int j = 0; j < kChunk; ++j)
-                    v[k][j] = inside_row<FILL>(c[k], j, fmaf(a.beta, v[k][j], a.alpha * xv[j]));
+                    for (int j = 0; j < kChunk; ++j) v[k][j] = fmaf(a.alpha, xv[j], v[k][j]);
+                }
+                if constexpr (FILL != kFull)
+#pragma unroll
+                    for (int j = 0; j < kChunk; ++j) v[k][j] = inside_row<FILL>(c[k], j, v[k][j]);
             } else {
 #pragma unroll
                 for (int j = 0; j < kChunk; ++j) v[k][j] = a.alpha * xv[j];
