@@ -448,8 +448,8 @@ typedef enum { IABN_ACT_SILU = 0, IABN_ACT_GELU = 1, IABN_ACT_LEAKY = 2 } iabn_a
  *   g, u           [M, F] out: the projections, which the backward takes, or
  *                  both NULL (inference).
  *   act, slope     an iabn_act_t; slope >= 0 and finite (LEAKY only).
- *   M, C, F        tokens, width, hidden width; C, F <= 2^24, M < 2^31.
- *                  C or F = 0: y is 0.
+ *   M, C, F        tokens, width, hidden width; C, F <= 2^24, M <= 2^26, no
+ *                  matrix of more than 2^37 elements.  C or F = 0: y is 0.
  * The workspace holds iabn_ffn_workspace_size(M, C, F, dtype) bytes, 16-byte
  * aligned: enough for either direction.
  *

@@ -91,7 +91,9 @@ size_t resnorm_workspace(const ResnormSplit& s, int64_t C) {
 // ---------------------------------------------------------------- gated feed-forward block
 
 constexpr int64_t kMaxFfnWidth = int64_t(1) << 24;
-constexpr int64_t kMaxFfnRows = (int64_t(1) << 31) - 1;
+constexpr int64_t kMaxFfnRows = int64_t(1) << 26;
+// Elements of any of its matrices (so that its tiles fit a launch).
+constexpr int64_t kMaxFfnElems = int64_t(1) << 37;
 
 int elem_bytes(int dtype) { return dtype == IABN_F32 ? 4 : 2; }
 
@@ -103,6 +105,9 @@ int check_ffn(int dtype, int act, float slope, int64_t M, int64_t C, int64_t F) 
     if (M > kMaxFfnRows || C > kMaxFfnWidth || F > kMaxFfnWidth)
         return fail(IABN_ERR_SHAPE, "M=%lld, C=%lld or F=%lld is too large", (long long)M,
                     (long long)C, (long long)F);
+    if (M * C > kMaxFfnElems || M * F > kMaxFfnElems || C * F > kMaxFfnElems)
+        return fail(IABN_ERR_SHAPE, "a matrix of M=%lld, C=%lld, F=%lld exceeds 2^37 elements",
+                    (long long)M, (long long)C, (long long)F);
     if (act != IABN_ACT_SILU && act != IABN_ACT_GELU && act != IABN_ACT_LEAKY)
         return fail(IABN_ERR_PARAM, "unknown activation %d", act);
     if (act == IABN_ACT_LEAKY && !(slope >= 0.0f && std::isfinite(slope)))

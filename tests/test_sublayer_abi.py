@@ -136,7 +136,7 @@ def test_ffn_refuses(lib):
     need = lib.iabn_ffn_workspace_size(4, 16, 24, F16)
     assert need >= 4 * 24 * 2
     both = ((ERR_DTYPE, dict(dtype=3)), (ERR_SHAPE, dict(M=-1)), (ERR_SHAPE, dict(C=(1 << 24) + 1)),
-            (ERR_SHAPE, dict(F=-8)), (ERR_SHAPE, dict(M=1 << 31)), (ERR_PARAM, dict(act=3)),
+            (ERR_SHAPE, dict(F=-8)), (ERR_SHAPE, dict(M=(1 << 26) + 1)), (ERR_SHAPE, dict(M=1 << 26, F=1 << 20)), (ERR_PARAM, dict(act=3)),
             (ERR_PARAM, dict(act=2, slope=-0.1)), (ERR_PARAM, dict(act=2, slope=NAN)),
             (ERR_NULL, dict(ws=None)), (ERR_WORKSPACE, dict(ws_bytes=need - 1)),
             (ERR_WORKSPACE, dict(ws=ctypes.c_void_p(4096 + 8))))
