@@ -97,7 +97,8 @@ def parse():
 
 
 def kernel_source_digest() -> str:
-    """sha256 of the sources libiabn.so is built from (csrc/ and the header)."""
+    """sha256 of the sources of the InPlace-ABN kernels (csrc/, without the
+    sublayer's folder, and the header)."""
     import glob
     import hashlib
     h = hashlib.sha256()

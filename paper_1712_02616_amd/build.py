@@ -19,8 +19,10 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
-HEADERS = sorted(glob.glob(os.path.join(CSRC, "*.h"))) + [os.path.join(ROOT, "include", "iabn.h")]
+# csrc/: InPlace-ABN; csrc/sublayer/: the feed-forward sublayer.
+SOURCES = sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "sublayer", "*.hip")))
+HEADERS = sorted(glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "sublayer", "*.h"))) + [
+    os.path.join(ROOT, "include", "iabn.h")]
 LIB = os.path.join(HERE, "libiabn.so")
 ABANDON_LIB = os.path.join(HERE, "libiabn_abandon.so")
 ABANDON_SOURCES = ("slice_fwd_f16.hip", "slice_bwd_f16.hip", "slice_fwd_f32.hip", "slice_bwd_f32.hip")
@@ -33,7 +35,7 @@ ARCH = "gfx950"
 FLAGS = ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # Packed fp32 VALU instructions stay off on this target.
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-         "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+         "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-I", os.path.join(CSRC, "sublayer")]
 
 
 def hipcc() -> str:
@@ -60,8 +62,8 @@ def build(verbose: bool = False, abandon: bool = False) -> str:
             return obj
 
         # The largest units first.
-        for src in sorted(SOURCES, key=lambda s: "slice" not in s):
-            name = os.path.basename(src)
+        for src in sorted(SOURCES, key=lambda s: "slice" not in s and "gemm" not in s):
+            name = os.path.relpath(src, CSRC).replace(os.sep, "_")
             objs.append(compile_(src, os.path.join(tmp, name + ".o")))
             abandon_objs.append(compile_(src, os.path.join(tmp, name + ".abandon.o"), [ABANDON_FLAG])
                                 if abandon and name in ABANDON_SOURCES else objs[-1])
