@@ -54,15 +54,17 @@ int check_gate(const void* gate, int64_t groups, int64_t R) {
 // written and read once) stay small against the rows: a block takes at least
 // kBwdMinRows of them, or two while there are fewer blocks than CUs ((1031,
 // 1501) fp32: 30.6 us with 8, 22.3 with 4, 25.4 with 2; (512, 1024) fp16 14.0,
-// 9.1, 7.2).
-constexpr int64_t kCUs = 256, kBwdWavesPerCU = 12;
+// 9.1, 7.2).  The kernels' registers let 8 waves run on a CU; unmasked rows of
+// 16-bit values in at most 4 waves are held to 12 ((16384, 2048) bf16: 109 us
+// with 8, 81 with 12; masked ones spill: (1031, 1501) fp32 20.6, 31.7).
+constexpr int64_t kCUs = 256;
 constexpr int64_t kBwdMinRows = 4;
 
-ResnormSplit split_rows(int64_t R, int64_t C, int64_t groups) {
+ResnormSplit split_rows(int64_t R, int64_t C, int64_t groups, int64_t waves_on_cu) {
     if (R == 0) return {1, 0, 0, 0, 0};
     const RowShape shape = row_shape(static_cast<int>((C + kChunk - 1) / kChunk), kBwdOneWave);
-    // (A block of one-wave rows has four of them, and 180 registers.)
-    const int64_t on_cu = shape.waves == 1 ? 2 : kBwdWavesPerCU / shape.waves;
+    // (A block of one-wave rows has four of them.)
+    const int64_t on_cu = shape.waves == 1 ? 2 : waves_on_cu / shape.waves;
     const int64_t target = kCUs * (on_cu > 1 ? on_cu : 1);
     ResnormSplit s;
     s.groups = groups > 0 && groups < R ? groups : 1;
@@ -82,6 +84,10 @@ ResnormSplit split_rows(int64_t R, int64_t C, int64_t groups) {
         s.blocks = static_cast<int>(s.groups * per);
     }
     return s;
+}
+
+int64_t waves_on_cu(int dtype, int64_t C) {
+    return dtype != IABN_F32 && C % (kWave * kChunk) == 0 && C <= 4 * kWave * kChunk ? 12 : 8;
 }
 
 size_t resnorm_workspace(const ResnormSplit& s, int64_t C) {
@@ -215,7 +221,10 @@ int iabn_resnorm_forward(const void* x, const void* h, void* r, void* u, int dty
 
 size_t iabn_resnorm_workspace_size(int64_t R, int64_t C, int64_t groups) {
     if (R < 0 || C < 0 || C > kMaxNormWidth || (C != 0 && R > kMaxElems / C)) return 0;
-    return resnorm_workspace(split_rows(R, C, groups), C);
+    // (Enough for every storage type.)
+    const size_t a = resnorm_workspace(split_rows(R, C, groups, 8), C);
+    const size_t b = resnorm_workspace(split_rows(R, C, groups, 12), C);
+    return a > b ? a : b;
 }
 
 int iabn_resnorm_backward(const void* dr, const void* du, const void* r, const void* h, void* dx,
@@ -251,7 +260,7 @@ int iabn_resnorm_backward(const void* dr, const void* du, const void* r, const v
         if ((post || dgate) && !h) return fail(IABN_ERR_NULL, "h is NULL");
         if (dh && dh == dx) return fail(IABN_ERR_PARAM, "dx and dh are one buffer");
     }
-    a.split = split_rows(R, C, gate ? groups : 0);
+    a.split = split_rows(R, C, gate ? groups : 0, waves_on_cu(dtype, C));
     if ((rc = check_workspace(workspace, workspace_bytes, resnorm_workspace(a.split, C)))) return rc;
     if (R == 0) {
         float* const vectors[] = {dpost_weight, dpost_bias, dpre_weight, dpre_bias};

@@ -26,12 +26,27 @@ constexpr int kRows = 4;
 template <int DT, int K>
 struct RowRegs {
     typename ChunkOf<DT>::vec dr[K], du[K], r[K], h[K];
+    float pre_mean, pre_rstd, post_mean, post_rstd;
 };
 
+// (`zero` is 0 in a vector register: a row's statistics come by vector loads, in
+// the order of the others.  By scalar ones, which the wait for LDS waits for
+// too, or when they are needed, they cost a round trip to memory per row:
+// (1031, 1501) fp32 22 us.)
 template <int DT, int K, int FILL, bool POST, bool PRE>
 __device__ __forceinline__ void load_row(const ResnormBwdArgs& a, int64_t row, const RowChunk (&c)[K],
-                                         RowRegs<DT, K>& x) {
+                                         int zero, RowRegs<DT, K>& x) {
     const int64_t base = row * a.C;
+    if constexpr (PRE) {
+        x.pre_mean = a.pre_stats[row + zero];
+        x.pre_rstd = a.pre_stats[a.R + row + zero];
+    }
+    if constexpr (POST) {
+        if (a.post != IABN_NORM_NONE) {
+            x.post_mean = a.post_stats[row + zero];
+            x.post_rstd = a.post_stats[a.R + row + zero];
+        }
+    }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         if (a.dr) x.dr[k] = load_row_chunk<DT, kStream, FILL>(a.dr, base, c[k]);
@@ -78,7 +93,8 @@ __device__ __forceinline__ void flush(float (&acc)[K][kChunk], const RowChunk (&
 }
 
 template <int DT, int K, bool ONE_WAVE, int FILL, bool POST, bool PRE, int THREADS>
-__global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
+__global__ __launch_bounds__(THREADS, !ONE_WAVE && THREADS == 256 && FILL == kFull && DT != IABN_F32 ? 3 : 1)
+void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
     __shared__ SumSlot slots[4];
     if constexpr (!ONE_WAVE) clear_slots(slots, 4);
     __shared__ float lds[ONE_WAVE ? kRows * kWave * kChunk : 1];
@@ -115,6 +131,8 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(ResnormBwdArgs a, 
             if (a.post_w) vector(a.post_w, k, post_w[k]);
         }
     }
+    int zero = 0;
+    asm volatile("" : "+v"(zero));
     const int64_t seg_rows = (a.split.group_rows + a.split.per_group - 1) / a.split.per_group;
     int par = 0;  // alternates the slots of consecutive rows
     Dropout dropped = a.drop;
@@ -126,8 +144,15 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(ResnormBwdArgs a, 
         const int64_t in_group = (seg - group * a.split.per_group) * seg_rows, at = group * a.split.group_rows;
         const int64_t lo = at + min(in_group, a.split.group_rows);
         const int64_t hi = at + min(in_group + seg_rows, a.split.group_rows);
+        typename ChunkOf<DT>::vec gate[POST ? K : 1];  // the segment's (or each row's)
+        if constexpr (POST) {
+            if (a.gate && lo + first < hi)
+#pragma unroll
+                for (int k = 0; k < K; ++k)
+                    gate[k] = load_row_chunk<DT, kCached, FILL>(a.gate, (lo + first) / a.gate_rows * a.C, c[k]);
+        }
         RowRegs<DT, K> x;
-        if (lo + first < hi) load_row<DT, K, FILL, POST, PRE>(a, lo + first, c, x);
+        if (lo + first < hi) load_row<DT, K, FILL, POST, PRE>(a, lo + first, c, zero, x);
         for (int64_t row = lo + first; row < hi; row += kStep) {
             float g[K][kChunk];
 #pragma unroll
@@ -147,10 +172,12 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(ResnormBwdArgs a, 
                     values(x.du[k], k, rdu[k]);
                 }
             }
+            const float pre_mean = x.pre_mean, pre_rstd = x.pre_rstd;
+            const float post_mean = x.post_mean, post_rstd = x.post_rstd;
             // The next row is on its way while this one is worked on.
-            if (row + kStep < hi) load_row<DT, K, FILL, POST, PRE>(a, row + kStep, c, x);
+            if (row + kStep < hi) load_row<DT, K, FILL, POST, PRE>(a, row + kStep, c, zero, x);
             if constexpr (PRE) {
-                const float mean = a.pre_stats[row], rstd = a.pre_stats[a.R + row];
+                const float mean = pre_mean, rstd = pre_rstd;
                 float (&hat)[K][kChunk] = rhat, (&d)[K][kChunk] = rdu, s1 = 0.0f, s2 = 0.0f;
                 if (a.dpre_b) {
 #pragma unroll
@@ -202,8 +229,8 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(ResnormBwdArgs a, 
             if constexpr (POST) {
                 float hat[K][kChunk], s1 = 0.0f, s2 = 0.0f, mean = 0.0f, rstd = 1.0f;
                 if (a.post != IABN_NORM_NONE) {
-                    mean = a.post_stats[row];
-                    rstd = a.post_stats[a.R + row];
+                    mean = post_mean;
+                    rstd = post_rstd;
                 }
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
@@ -221,8 +248,10 @@ __global__ __launch_bounds__(THREADS) void resnorm_bwd_kernel(ResnormBwdArgs a, 
                         for (int j = 0; j < kChunk; ++j) g[k][j] *= a.beta;
                     if (a.gate) {
                         float gv[kChunk], o[kChunk], bv[kChunk] = {};
-                        values(load_row_chunk<DT, kCached, FILL>(a.gate, row / a.gate_rows * a.C, c[k]), k, gv);
                         if (a.post_b) vector(a.post_b, k, bv);
+                        values(gate[k], k, gv);
+                        if (a.gate_each_row && row + kStep < hi)
+                            gate[k] = load_row_chunk<DT, kStream, FILL>(a.gate, (row + kStep) * a.C, c[k]);
 #pragma unroll
                         for (int j = 0; j < kChunk; ++j) {
                             o[j] = g[k][j] * fmaf(hat[k][j], post_w[k][j], bv[j]);
