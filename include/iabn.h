@@ -10,7 +10,10 @@
  * xhat = (y - beta)/gamma from z, then forms the BN gradient (Algorithm 2,
  * InPlace-ABN I, with the BN backward of Sec. 3.3).  Also InPlace-ABN II,
  * and the two blocks the paper compares against (the standard block and the
- * proposed checkpointing, Sec. 3.2), on the same kernels.
+ * proposed checkpointing, Sec. 3.2), on the same kernels.  At the end: the
+ * operators of a transformer's feed-forward sublayer (norms around a block,
+ * dropout, a gated feed-forward block), which recompute where they can instead
+ * of storing, as the method does.
  *
  * Conventions shared by every entry point
  * ---------------------------------------

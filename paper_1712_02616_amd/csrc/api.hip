@@ -17,7 +17,7 @@
 #include "launch.h"
 #include "tile.h"
 
-#define IABN_VERSION 10100
+#define IABN_VERSION 10200
 
 namespace iabn_impl {
 

@@ -101,6 +101,9 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
     const int t = ONE_WAVE ? lane_id() : threadIdx.x, T = ONE_WAVE ? kWave : waves * kWave;
     const int first = ONE_WAVE ? threadIdx.x / kWave : 0;
     constexpr int kStep = ONE_WAVE ? kRows : 1;
+    // The widest rows' threads have 128 registers: no row ahead, and the weights
+    // come from the caches for each row.
+    constexpr bool kLean = THREADS > 512;
     RowChunk c[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) c[k] = row_chunk<FILL>(t + k * T, a.C);
@@ -120,7 +123,7 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
         for (int k = 0; k < K; ++k) {
 #pragma unroll
             for (int j = 0; j < kChunk; ++j) pre_w[k][j] = 1.0f;
-            if (a.pre_w) vector(a.pre_w, k, pre_w[k]);
+            if (a.pre_w && !kLean) vector(a.pre_w, k, pre_w[k]);
         }
     }
     if constexpr (POST) {
@@ -128,7 +131,7 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
         for (int k = 0; k < K; ++k) {
 #pragma unroll
             for (int j = 0; j < kChunk; ++j) post_w[k][j] = 1.0f;
-            if (a.post_w) vector(a.post_w, k, post_w[k]);
+            if (a.post_w && !kLean) vector(a.post_w, k, post_w[k]);
         }
     }
     int zero = 0;
@@ -152,8 +155,9 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
                     gate[k] = load_row_chunk<DT, kCached, FILL>(a.gate, (lo + first) / a.gate_rows * a.C, c[k]);
         }
         RowRegs<DT, K> x;
-        if (lo + first < hi) load_row<DT, K, FILL, POST, PRE>(a, lo + first, c, zero, x);
+        if (!kLean && lo + first < hi) load_row<DT, K, FILL, POST, PRE>(a, lo + first, c, zero, x);
         for (int64_t row = lo + first; row < hi; row += kStep) {
+            if constexpr (kLean) load_row<DT, K, FILL, POST, PRE>(a, row, c, zero, x);
             float g[K][kChunk];
 #pragma unroll
             for (int k = 0; k < K; ++k) {
@@ -175,7 +179,7 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
             const float pre_mean = x.pre_mean, pre_rstd = x.pre_rstd;
             const float post_mean = x.post_mean, post_rstd = x.post_rstd;
             // The next row is on its way while this one is worked on.
-            if (row + kStep < hi) load_row<DT, K, FILL, POST, PRE>(a, row + kStep, c, zero, x);
+            if (!kLean && row + kStep < hi) load_row<DT, K, FILL, POST, PRE>(a, row + kStep, c, zero, x);
             if constexpr (PRE) {
                 const float mean = pre_mean, rstd = pre_rstd;
                 float (&hat)[K][kChunk] = rhat, (&d)[K][kChunk] = rdu, s1 = 0.0f, s2 = 0.0f;
@@ -187,6 +191,7 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
                 }
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
+                    if (kLean && a.pre_w) vector(a.pre_w, k, pre_w[k]);
 #pragma unroll
                     for (int j = 0; j < kChunk; ++j) {
                         hat[k][j] = inside_row<FILL>(c[k], j, fmaf(hat[k][j], rstd, -mean * rstd));
@@ -235,6 +240,7 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
                     if (a.h) values(raw_h[k], k, hat[k]);
+                    if (kLean && a.post_w) vector(a.post_w, k, post_w[k]);
                     // From here g is e = beta*g*D, then dn, then dn*w.
 #pragma unroll
                     for (int j = 0; j < kChunk; ++j) {
