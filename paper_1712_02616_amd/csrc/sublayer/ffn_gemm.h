@@ -1,9 +1,9 @@
 // The block's matrix products on the matrix cores: tiles of TM x TN outputs,
 // K in steps of 128 bytes per row, both operands staged through two LDS
 // buffers: while the waves multiply out of one, the next step's tiles arrive
-// in the other.  Operands whose rows are whole 16-byte accesses go straight
-// from memory to LDS (DMA); others, and a last step that K does not fill, go
-// through registers, which hold zeros for what is not there.
+// in the other.  Operands whose addresses are whole dwords go straight from
+// memory to LDS (DMA); others, and a last step that K does not fill, go through
+// registers, which hold zeros for what is not there.
 //
 // A block's waves each own WM x WN outputs in 16x16 accumulators (fp32).  The
 // operand with the n index (the weights, mostly) takes the first place of the
@@ -238,7 +238,11 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
     // Steps of K: whole ones that go straight to LDS, those of the first
     // product and then those of the second, and the others, through
     // registers.  This block's share of them all: [lo, hi) and [from, to).
-    const int whole = DMA ? static_cast<int>(a.K / BK) : 0, steps = whole * Kind::kSegs;
+    // (A strided operand whose last chunk of a row reaches into the next one may
+    // not fetch its last row.)
+    constexpr int E = SX::E;
+    const bool reaches = (Kind::kXStrided && a.M % E != 0) || (Kind::kYStrided && a.N % E != 0);
+    const int whole = DMA ? static_cast<int>((a.K - (reaches ? 1 : 0)) / BK) : 0, steps = whole * Kind::kSegs;
     const int per_seg = static_cast<int>((a.K + BK - 1) / BK) - whole, rest = per_seg * Kind::kSegs;
     const int64_t all = steps + rest;
     const int begin = static_cast<int>(all * blockIdx.y / gridDim.y);
@@ -452,14 +456,14 @@ void launch_tiles(const GemmArgs& a, int products, hipStream_t st) {
             a, static_cast<int>(tm), static_cast<int>(tn));
 }
 
-// Whether an operand's tiles can go straight to LDS: every chunk of 16 bytes
-// is whole and aligned, and a tile's offsets fit 31 bits.
+// Whether an operand's tiles can go straight to LDS: its addresses are whole
+// dwords, a row of it holds a chunk, and a tile's offsets fit 31 bits.
 template <int DT>
-bool whole_chunks(const Operand& o, bool strided, int64_t rows, int64_t K) {
+bool fetchable(const Operand& o, int64_t row) {
     constexpr int64_t es = sizeof(typename Elem<DT>::T), E = 16 / es;
-    if ((strided ? rows : K) % E != 0 || o.ld % E != 0 || o.ld * es * 256 >= int64_t(1) << 31) return false;
+    if (row < E || o.ld * es % 4 != 0 || o.ld * es * 256 >= int64_t(1) << 31) return false;
     for (const void* p : o.p)
-        if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return false;
+        if (reinterpret_cast<uintptr_t>(p) % 4 != 0) return false;
     return true;
 }
 
@@ -481,8 +485,8 @@ void launch_planned(GemmArgs a, int products, hipStream_t st) {
 
 template <int DT, int KIND>
 void launch_kind(const GemmArgs& a, int products, hipStream_t st) {
-    if (whole_chunks<DT>(a.x, KindOf<KIND>::kXStrided, a.M, a.K) &&
-        whole_chunks<DT>(a.y, KindOf<KIND>::kYStrided, a.N, a.K))
+    if (fetchable<DT>(a.x, KindOf<KIND>::kXStrided ? a.M : a.K) &&
+        fetchable<DT>(a.y, KindOf<KIND>::kYStrided ? a.N : a.K))
         launch_planned<DT, KIND, true>(a, products, st);
     else
         launch_planned<DT, KIND, false>(a, products, st);
