@@ -21,11 +21,15 @@ struct TileCost {
 };
 // [fp32][direct][tile]
 constexpr TileCost kCost[2][2][4] = {
-    {{{{0, 0, 0, 0}, 0}, {{1.05f, 2.1f, 3.1f, 4.2f}, 2}, {{0.76f, 0.97f, 1.65f, 1.85f}, 1}, {{0.58f, 0.8f, 0.93f, 1.5f}, 0.5f}},
+    {{{{0, 0, 0, 0}, 0}, {{1.5f, 3.0f, 4.4f, 5.9f}, 2}, {{1.1f, 1.3f, 2.0f, 2.6f}, 1}, {{0.9f, 1.1f, 1.4f, 2.2f}, 0.5f}},
      {{{1.27f, 2.54f, 3.81f, 5.08f}, 8}, {{0.67f, 0.68f, 1.36f, 1.4f}, 1.6f}, {{0.32f, 0.55f, 0.75f, 1.16f}, 0.8f}, {{0.26f, 0.45f, 0.68f, 0.87f}, 0.4f}}},
     {{{{0, 0, 0, 0}, 0}, {{2.65f, 5.2f, 7.8f, 10.4f}, 4}, {{1.6f, 2.6f, 4.8f, 5.0f}, 2}, {{1.0f, 1.6f, 2.25f, 3.2f}, 1}},
      {{{0, 0, 0, 0}, 0}, {{2.05f, 3.7f, 7.2f, 7.4f}, 4}, {{1.1f, 1.93f, 2.8f, 3.9f}, 2}, {{0.63f, 1.02f, 1.5f, 1.95f}, 1}}}};
 constexpr float kGatingEnds = 3.0f;  // kGemmDh's end is so much longer
+// 16-bit rows at odd addresses, through registers: the loads are what a step
+// takes, and a strided operand's are so much slower ((1777, 4003 -> 1501) fp16
+// dx: 211 us in 64x128 tiles of four splits, 511 in 32x128 ones of one).
+constexpr float kStridedLoads = 2.5f;
 // Joining split sums: a launch, and the sums written and read.
 constexpr float kJoinUs = 3.0f, kJoinBytesPerUs = 4e6f;
 
@@ -63,7 +67,8 @@ GemmPlan plan_gemm(int dtype, GemmKind kind, bool direct, int64_t M, int64_t N, 
         for (int s = 1; s <= (splittable ? kMaxSplits : 1) && s <= steps; s *= 2) {
             const int64_t on_cu = div_up(tiles * s, kCUs);  // blocks that the busiest CU gets
             const float full = static_cast<float>((on_cu - 1) / 4);
-            const float per_step = full * cost.step[3] + cost.step[(on_cu - 1) % 4];
+            const float slow = dtype != IABN_F32 && !direct && kind >= kGemmDh ? kStridedLoads : 1.0f;
+            const float per_step = slow * (full * cost.step[3] + cost.step[(on_cu - 1) % 4]);
             const float ends = cost.ends * (kind == kGemmDh ? kGatingEnds : 1.0f);
             float us = static_cast<float>(div_up(steps, s)) * per_step + static_cast<float>(on_cu) * ends;
             if (s > 1) us += kJoinUs + 8.0f * s * M * N * products / kJoinBytesPerUs;
