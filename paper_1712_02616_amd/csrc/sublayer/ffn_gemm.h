@@ -9,6 +9,16 @@
 // operand with the n index (the weights, mostly) takes the first place of the
 // matrix instruction, so that a lane's 4 results are consecutive in n, which
 // is how every output is stored.
+//
+// Bound by the matrix cores at the clock that their power leaves: bf16, random
+// values, the two products of dx (8192, 2x10240 -> 4096) 1.00 ms, 1.37 PFLOP/s
+// (a library's product of that layout 1.30-1.37 on the same card); both
+// projections (4096, 2048 -> 2x8192) 245 us, 1.12 (200 MB of results leave in
+// that time, of which a 256x256 tile, alone on its CU, hides none); the
+// weights' gradients 1.08-1.34 (library 1.06-1.16); dh with the gating's
+// gradient (8192, 4096 -> 10240) 622 us, 1.10 (840 MB in its epilogue); the
+// down projection (4096, 8192 -> 2048) 111 us, 1.24.  fp32: 93% of the matrix
+// cores' rate at full grids.
 #pragma once
 
 #include "ffn.h"
