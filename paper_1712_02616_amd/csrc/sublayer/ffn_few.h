@@ -6,11 +6,11 @@
 // line by line of 128 bytes, so that a block reads each row of the weights in
 // long runs; their sums meet in LDS.
 //
-// Bound by HBM: one token (4096 -> 2x10240) bf16 33 us for 168 MB, 5.1 TB/s, and
-// 16 us for the 84 MB back, 5.2; 24 tokens (2048 -> 2x8192) fp16 16 us, 4.2, and
-// back 12 and 4 to join, where the tokens' h, read by every block, is as much
-// traffic as the weights.  The weights' loads keep lines in the caches: a line
-// is two loads (non-temporal ones: 35 and 21 us).
+// Bound by HBM: one token (4096 -> 2x10240) bf16 34 us for 168 MB, 4.9 TB/s, and
+// 16 us for the 84 MB back, 5.3; 24 tokens (2048 -> 2x8192) fp16 16 us, 4.3, and
+// back 12 and 4 to join, where the tokens' h, read by every block, is more
+// traffic than the weights.  The weights' loads keep lines in the caches: a line
+// is two loads (one token: 32 and 16 us, non-temporal 35 and 21).
 #pragma once
 
 #include "ffn.h"
@@ -19,7 +19,8 @@
 namespace iabn_impl {
 
 // Lines of 128 bytes of every row in a batch; a wave has two batches in flight
-// (four lines spill: 43 us).
+// (four lines spill: one
+// token 41 us instead of 34, 24 tokens 32 instead of 16).
 constexpr int kFewLines = 2;
 
 template <int DT, int KIND, int MT>

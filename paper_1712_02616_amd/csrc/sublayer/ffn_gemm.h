@@ -10,15 +10,17 @@
 // matrix instruction, so that a lane's 4 results are consecutive in n, which
 // is how every output is stored.
 //
-// Bound by the matrix cores at the clock that their power leaves: bf16, random
-// values, the two products of dx (8192, 2x10240 -> 4096) 1.00 ms, 1.37 PFLOP/s
-// (a library's product of that layout 1.30-1.37 on the same card); both
-// projections (4096, 2048 -> 2x8192) 245 us, 1.12 (200 MB of results leave in
-// that time, of which a 256x256 tile, alone on its CU, hides none); the
-// weights' gradients 1.08-1.34 (library 1.06-1.16); dh with the gating's
-// gradient (8192, 4096 -> 10240) 622 us, 1.10 (840 MB in its epilogue); the
-// down projection (4096, 8192 -> 2048) 111 us, 1.24.  fp32: 93% of the matrix
-// cores' rate at full grids.
+// Bound by the matrix cores at the clock that their power leaves, which falls in
+// a long run of products (random values; the fastest of 20 passes and the
+// median; a large library product 1.39-1.61 PFLOP/s NT, 1.2-1.37 NN, 1.05-1.16
+// TN).  bf16: dx (8192, 2x10240 -> 4096) 0.998 and 1.034 ms, 1.38 and 1.33
+// PFLOP/s; both projections (4096, 2048 -> 2x8192) 244 and 281 us, 1.13 and 0.98
+// (200 MB of results leave in that time, of which a 256x256 tile, alone on its
+// CU, hides none); the weights' gradients over 8192 tokens 1.36 and 1.31 (gate
+// and up), 1.06 and 1.02 (down); dh with the gating's gradient (8192, 4096 ->
+// 10240) 627 and 637 us, 1.10 and 1.08 (840 MB in its epilogue); the down
+// projection (4096, 8192 -> 2048) 111 and 117 us, 1.23 and 1.17.  fp32, the sizes
+// of that forward: 1.94 and 0.95 ms, 141 and 144 TFLOP/s (the library 153).
 #pragma once
 
 #include "ffn.h"

@@ -17,14 +17,14 @@
 // leaves its columns' sums in the workspace and a second kernel adds the
 // blocks' in double, in a fixed order.
 //
-// (16384, 2048) bf16, RMS norms, gate and dropout: 82 us and 7 for the sums,
-// against 71 us of HBM traffic at 5.7 TB/s and about 60 us of arithmetic (rows
-// that fill their threads are not masked, sums that a norm does not need are
-// left out, the branch's scale goes with the dropout's).  (65536, 512) bf16 68
-// us (73 of traffic at that rate; part of it stays in the 256 MB cache), (1031,
-// 1501) fp32 21 and 4: four rows one after the other in each of 258 blocks.
-// Rows of 4097 to 8192 have 128 registers per thread and spill some ((4096,
-// 8192) bf16 109 us, 153 with a row ahead), those of up to 16384 many.
+// bf16, RMS norms, gate and dropout: (16384, 2048) 83 us and 7 for the sums,
+// against 71 us for its 403 MB of HBM traffic at 5.7 TB/s (rows that fill their
+// threads are not masked, sums that a norm does not need are left out, the
+// branch's scale goes with the dropout's); (65536, 512), the same traffic, 82 and
+// 5, and 68 and 5 with no more than the norm before the next block.  (1031, 1501)
+// fp32 21 and 4: four rows one after the other in each of 258 blocks.  Rows of
+// 4097 to 8192 have 128 registers per thread: (4096, 8192) bf16 125 us, 171 with a
+// row ahead; those of up to 16384 spill: (2048, 16384) 450 us.
 #include "sublayer.h"
 
 namespace iabn_impl {

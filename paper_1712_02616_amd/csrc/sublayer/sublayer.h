@@ -319,8 +319,10 @@ inline RowShape row_shape(int chunks, int one_wave) {
     return {(chunks + k * kWave - 1) / (k * kWave), k};
 }
 
-// Rows of one wave: up to 2 chunks a thread in the forward; 1 in the backward,
-// whose columns' sums take 40 registers a chunk.
+// Rows of one wave: up to 2 chunks a thread in the forward ((32768, 1024) fp16,
+// all parts: 62 us, 69 in two waves); 1 in the backward, whose columns' sums take
+// 40 registers a chunk (the same rows 93 us and 11 for the sums in two waves, 108
+// and 5 in one; bf16 with RMS norms 86 and 11, 101 and 5).
 constexpr int kFwdOneWave = 2, kBwdOneWave = 1;
 
 }  // namespace iabn_impl
