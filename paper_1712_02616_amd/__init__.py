@@ -225,21 +225,27 @@ def _stream(device, stream):
     return ctypes.c_void_p(int(stream))
 
 
-def _workspace(N, C, HW, code, device, workspace, stream=None):
-    """The caller's workspace, or a new one from torch's caching allocator.
-    A new one is released when this call returns, while the kernels may still
-    run: the allocator reuses it only in the order of the stream it was
-    recorded on, so it is recorded on the stream the kernels run on."""
-    need = iabn_workspace_size(N, C, HW, code)
+def _take(need, device, workspace, stream):
+    """The caller's workspace, or ``need`` bytes from torch's caching allocator:
+    (tensor, address, bytes).  A new one is taken from the blocks of the stream
+    that the kernels run on, in whose order it was used before and is again when
+    this call has released it, which is before the kernels have run.  (A block
+    of another stream may have work there that is not done yet.)"""
     if workspace is None:
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
-        if stream is not None:
-            if not isinstance(stream, torch.cuda.Stream):
-                stream = torch.cuda.ExternalStream(int(stream), device=device)
-            workspace.record_stream(stream)
+        if stream is None:
+            stream = torch.cuda.current_stream(device)
+        elif not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream), device=device)
+        with torch.cuda.stream(stream):
+            workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
     if workspace.device != device or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on %s" % device)
     return workspace, ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size()
+
+
+def _workspace(N, C, HW, code, device, workspace, stream=None):
+    """The workspace of an entry point on [N, C, HW] tensors (see _take)."""
+    return _take(iabn_workspace_size(N, C, HW, code), device, workspace, stream)
 
 
 def iabn_version() -> int:

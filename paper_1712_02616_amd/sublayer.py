@@ -129,19 +129,6 @@ def _word(v, what):
     return v
 
 
-def _workspace(need, device, workspace, stream):
-    """The caller's workspace, or a new one (see _workspace of the package)."""
-    if workspace is None:
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
-        if stream is not None:
-            if not isinstance(stream, torch.cuda.Stream):
-                stream = torch.cuda.ExternalStream(int(stream), device=device)
-            workspace.record_stream(stream)
-    if workspace.device != device or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous tensor on %s" % device)
-    return workspace, _iabn._ptr(workspace), workspace.numel() * workspace.element_size()
-
-
 def iabn_dropout(x, y, p, seed, offset=0, stream=None):
     """y = D(x): the dropout of (p, seed, offset), whose mask is not stored (the
     same call on a gradient is the backward); ``y`` may be ``x``.  Returns ``y``."""
@@ -222,7 +209,7 @@ def iabn_resnorm_backward(dr, du, r, h, dx, dh, gate=None, post_norm=None, post_
         (dpre_bias, "dpre_bias"))}
     stats = [rows.floats(t, 2 * R, n) for t, n in ((post_stats, "post_stats"),
                                                     (pre_stats, "pre_stats"))]
-    ws, wp, wb = _workspace(iabn_resnorm_workspace_size(R, C, groups), rows.device, workspace, stream)
+    ws, wp, wb = _iabn._take(iabn_resnorm_workspace_size(R, C, groups), rows.device, workspace, stream)
     rc = _iabn.load().iabn_resnorm_backward(
         *tensors, rows.code, gp, groups, post, v["post_weight"], v["post_bias"], pre, v["pre_weight"],
         *stats, dgp, v["dpost_weight"], v["dpost_bias"], v["dpre_weight"], v["dpre_bias"],
@@ -255,7 +242,7 @@ def iabn_ffn_forward(x, w_gate, w_up, w_down, y, g=None, u=None, act="silu", slo
     R, C, F = rows.R, rows.C, rows.F
     yp = rows(y, "y")
     gp, up = rows.matrix(g, R, F, "g", True), rows.matrix(u, R, F, "u", True)
-    ws, wp, wb = _workspace(iabn_ffn_workspace_size(R, C, F, rows.code), rows.device, workspace, stream)
+    ws, wp, wb = _iabn._take(iabn_ffn_workspace_size(R, C, F, rows.code), rows.device, workspace, stream)
     rc = _iabn.load().iabn_ffn_forward(xp, *weights, yp, gp, up, rows.code, code, float(slope), R, C, F,
                                        wp, wb, _iabn._stream(rows.device, stream))
     _iabn._check("iabn_ffn_forward", rc)
@@ -278,7 +265,7 @@ def iabn_ffn_backward(dy, x, g, u, w_gate, w_up, w_down, dx, dg, du, dw_gate, dw
     outs = [rows(dx, "dx")] + [rows.matrix(t, a, b, n) for t, a, b, n in (
         (dg, R, F, "dg"), (du, R, F, "du"), (dw_gate, F, C, "dw_gate"), (dw_up, F, C, "dw_up"),
         (dw_down, C, F, "dw_down"))]
-    ws, wp, wb = _workspace(iabn_ffn_workspace_size(R, C, F, rows.code), rows.device, workspace, stream)
+    ws, wp, wb = _iabn._take(iabn_ffn_workspace_size(R, C, F, rows.code), rows.device, workspace, stream)
     rc = _iabn.load().iabn_ffn_backward(dyp, xp, *kept, *weights, *outs, rows.code, code, float(slope),
                                         R, C, F, wp, wb, _iabn._stream(rows.device, stream))
     _iabn._check("iabn_ffn_backward", rc)
