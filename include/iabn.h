@@ -27,7 +27,9 @@
  *  - The caller owns all memory.  The library never allocates, frees or
  *    synchronises; every call only enqueues kernels on `stream` (a
  *    hipStream_t; NULL is the default stream) and returns.  Results are valid
- *    once the stream has reached them.
+ *    once the stream has reached them.  The stream's device, which holds the
+ *    tensors, must be the calling thread's current one (the Python binding
+ *    sees to it).
  *  - `workspace` is caller-owned device memory of at least
  *    iabn_workspace_size(N, C, HW, dtype) bytes, 16-byte aligned.  A forward
  *    (or backward) split into its two phases must hand the same workspace,

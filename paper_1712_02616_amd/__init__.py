@@ -225,6 +225,15 @@ def _stream(device, stream):
     return ctypes.c_void_p(int(stream))
 
 
+def _enqueue(name, device, stream, *args):
+    """Entry point ``name`` with ``args`` and the stream.  The tensors' device is
+    current meanwhile: a default stream has no device of its own, and a launch
+    goes to the current one."""
+    with torch.cuda.device(device):
+        rc = getattr(load(), name)(*args, _stream(device, stream))
+    _check(name, rc)
+
+
 def _take(need, device, workspace, stream):
     """The caller's workspace, or ``need`` bytes from torch's caching allocator:
     (tensor, address, bytes).  A new one is taken from the blocks of the stream
@@ -287,9 +296,8 @@ def iabn_forward_train(x_z, gamma, beta, running_mean, running_var, save_mean, s
             (running_mean, "running_mean"), (running_var, "running_var"),
             (save_mean, "save_mean"), (save_var, "save_var"))]
     ws, wp, wb = _workspace(N, C, HW, code, dev, workspace, stream)
-    rc = load().iabn_forward_train(_ptr(x_z), code, *args, float(eps), float(momentum),
-                                   float(slope), N, C, HW, wp, wb, _stream(dev, stream))
-    _check("iabn_forward_train", rc)
+    _enqueue("iabn_forward_train", dev, stream, _ptr(x_z), code, *args, float(eps), float(momentum),
+             float(slope), N, C, HW, wp, wb)
     return x_z
 
 
@@ -306,9 +314,8 @@ def iabn_forward_train_noalloc(x_z, gamma, beta, running_mean, running_var, save
     args = [_chan(t, C, dev, n) for t, n in ((gamma, "gamma"), (beta, "beta"),
             (running_mean, "running_mean"), (running_var, "running_var"),
             (save_mean, "save_mean"), (save_var, "save_var"))]
-    rc = load().iabn_forward_train_noalloc(_ptr(x_z), code, *args, float(eps), float(momentum),
-                                           float(slope), N, C, HW, _stream(dev, stream))
-    _check("iabn_forward_train_noalloc", rc)
+    _enqueue("iabn_forward_train_noalloc", dev, stream, _ptr(x_z), code, *args, float(eps),
+             float(momentum), float(slope), N, C, HW)
     return x_z
 
 
@@ -323,9 +330,8 @@ def iabn_forward_eval(x_z, gamma, beta, running_mean, running_var, eps=1e-5, slo
     dev = x_z.device
     args = [_chan(t, C, dev, n) for t, n in ((gamma, "gamma"), (beta, "beta"),
             (running_mean, "running_mean"), (running_var, "running_var"))]
-    rc = load().iabn_forward_eval(_ptr(x_z), code, *args, float(eps), float(slope), N, C, HW,
-                                  _stream(dev, stream))
-    _check("iabn_forward_eval", rc)
+    _enqueue("iabn_forward_eval", dev, stream, _ptr(x_z), code, *args, float(eps), float(slope), N,
+             C, HW)
     return x_z
 
 
@@ -343,9 +349,8 @@ def iabn_backward(z, dz_dx, gamma, beta, save_var, dgamma, dbeta, eps=1e-5, slop
     args = [_chan(t, C, dev, n) for t, n in ((gamma, "gamma"), (beta, "beta"),
             (save_var, "save_var"), (dgamma, "dgamma"), (dbeta, "dbeta"))]
     ws, wp, wb = _workspace(N, C, HW, code, dev, workspace, stream)
-    rc = load().iabn_backward(_ptr(z), _ptr(dz_dx), code, *args, float(eps), float(slope), N, C, HW,
-                              wp, wb, _stream(dev, stream))
-    _check("iabn_backward", rc)
+    _enqueue("iabn_backward", dev, stream, _ptr(z), _ptr(dz_dx), code, *args, float(eps),
+             float(slope), N, C, HW, wp, wb)
     return dz_dx
 
 
@@ -368,9 +373,8 @@ def iabn_backward_ii(z, dz_dx, gamma, beta, save_var, dgamma, dbeta, eps=1e-5, s
     args = [_chan(t, C, dev, n) for t, n in ((gamma, "gamma"), (beta, "beta"),
             (save_var, "save_var"), (dgamma, "dgamma"), (dbeta, "dbeta"))]
     ws, wp, wb = _workspace(N, C, HW, code, dev, workspace, stream)
-    rc = load().iabn_backward_ii(_ptr(z), _ptr(dz_dx), code, *args, float(eps), float(slope), N, C,
-                                 HW, wp, wb, _stream(dev, stream))
-    _check("iabn_backward_ii", rc)
+    _enqueue("iabn_backward_ii", dev, stream, _ptr(z), _ptr(dz_dx), code, *args, float(eps),
+             float(slope), N, C, HW, wp, wb)
     return dz_dx
 
 
@@ -387,9 +391,8 @@ def iabn_std_forward_train(x, z, gamma, beta, running_mean, running_var, save_me
             (running_mean, "running_mean"), (running_var, "running_var"),
             (save_mean, "save_mean"), (save_var, "save_var"))]
     ws, wp, wb = _workspace(N, C, HW, code, dev, workspace, stream)
-    rc = load().iabn_std_forward_train(_ptr(x), _ptr(z), code, *args, float(eps), float(momentum),
-                                       float(slope), N, C, HW, wp, wb, _stream(dev, stream))
-    _check("iabn_std_forward_train", rc)
+    _enqueue("iabn_std_forward_train", dev, stream, _ptr(x), _ptr(z), code, *args, float(eps),
+             float(momentum), float(slope), N, C, HW, wp, wb)
     return z
 
 
@@ -406,9 +409,8 @@ def iabn_std_backward(x, z, dz_dx, gamma, beta, save_mean, save_var, dgamma, dbe
     args = [_chan(t, C, dev, n) for t, n in ((gamma, "gamma"), (beta, "beta"),
             (save_mean, "save_mean"), (save_var, "save_var"), (dgamma, "dgamma"), (dbeta, "dbeta"))]
     ws, wp, wb = _workspace(N, C, HW, code, dev, workspace, stream)
-    rc = load().iabn_std_backward(_ptr(x), _ptr(z), _ptr(dz_dx), code, *args, float(eps),
-                                  float(slope), N, C, HW, wp, wb, _stream(dev, stream))
-    _check("iabn_std_backward", rc)
+    _enqueue("iabn_std_backward", dev, stream, _ptr(x), _ptr(z), _ptr(dz_dx), code, *args,
+             float(eps), float(slope), N, C, HW, wp, wb)
     return dz_dx
 
 
@@ -426,10 +428,8 @@ def iabn_ckpt_forward_train(x_xhat, z, gamma, beta, running_mean, running_var, s
             (running_mean, "running_mean"), (running_var, "running_var"),
             (save_mean, "save_mean"), (save_var, "save_var"))]
     ws, wp, wb = _workspace(N, C, HW, code, dev, workspace, stream)
-    rc = load().iabn_ckpt_forward_train(_ptr(x_xhat), _ptr(z), code, *args, float(eps),
-                                        float(momentum), float(slope), N, C, HW, wp, wb,
-                                        _stream(dev, stream))
-    _check("iabn_ckpt_forward_train", rc)
+    _enqueue("iabn_ckpt_forward_train", dev, stream, _ptr(x_xhat), _ptr(z), code, *args, float(eps),
+             float(momentum), float(slope), N, C, HW, wp, wb)
     return z
 
 
@@ -442,9 +442,8 @@ def iabn_ckpt_recompute(xhat, z, gamma, beta, slope=0.01, stream=None):
     dev = xhat.device
     g = _chan(gamma, C, dev, "gamma")
     b = _chan(beta, C, dev, "beta")
-    rc = load().iabn_ckpt_recompute(_ptr(xhat), _ptr(z), code, g, b, float(slope), N, C, HW,
-                                    _stream(dev, stream))
-    _check("iabn_ckpt_recompute", rc)
+    _enqueue("iabn_ckpt_recompute", dev, stream, _ptr(xhat), _ptr(z), code, g, b, float(slope), N,
+             C, HW)
     return z
 
 
@@ -460,9 +459,8 @@ def iabn_ckpt_backward(xhat, dz_dx, gamma, beta, save_var, dgamma, dbeta, eps=1e
     args = [_chan(t, C, dev, n) for t, n in ((gamma, "gamma"), (beta, "beta"),
             (save_var, "save_var"), (dgamma, "dgamma"), (dbeta, "dbeta"))]
     ws, wp, wb = _workspace(N, C, HW, code, dev, workspace, stream)
-    rc = load().iabn_ckpt_backward(_ptr(xhat), _ptr(dz_dx), code, *args, float(eps), float(slope),
-                                   N, C, HW, wp, wb, _stream(dev, stream))
-    _check("iabn_ckpt_backward", rc)
+    _enqueue("iabn_ckpt_backward", dev, stream, _ptr(xhat), _ptr(dz_dx), code, *args, float(eps),
+             float(slope), N, C, HW, wp, wb)
     return dz_dx
 
 
@@ -471,8 +469,7 @@ def iabn_forward_stats(x, workspace, stream=None):
     N, C, HW = _nchw(x, "x")
     code = DTYPE_CODES[x.dtype]
     ws, wp, wb = _workspace(N, C, HW, code, x.device, workspace, stream)
-    rc = load().iabn_forward_stats(_ptr(x), code, N, C, HW, wp, wb, _stream(x.device, stream))
-    _check("iabn_forward_stats", rc)
+    _enqueue("iabn_forward_stats", x.device, stream, _ptr(x), code, N, C, HW, wp, wb)
 
 
 def iabn_forward_apply(x_z, gamma, beta, running_mean, running_var, save_mean, save_var,
@@ -485,9 +482,8 @@ def iabn_forward_apply(x_z, gamma, beta, running_mean, running_var, save_mean, s
             (running_mean, "running_mean"), (running_var, "running_var"),
             (save_mean, "save_mean"), (save_var, "save_var"))]
     ws, wp, wb = _workspace(N, C, HW, code, dev, workspace, stream)
-    rc = load().iabn_forward_apply(_ptr(x_z), code, *args, float(eps), float(momentum),
-                                   float(slope), N, C, HW, wp, wb, _stream(dev, stream))
-    _check("iabn_forward_apply", rc)
+    _enqueue("iabn_forward_apply", dev, stream, _ptr(x_z), code, *args, float(eps), float(momentum),
+             float(slope), N, C, HW, wp, wb)
     return x_z
 
 
@@ -501,9 +497,8 @@ def iabn_backward_reduce(z, dz, gamma, beta, slope, workspace, stream=None):
     g = _chan(gamma, C, dev, "gamma")
     b = _chan(beta, C, dev, "beta")
     ws, wp, wb = _workspace(N, C, HW, code, dev, workspace, stream)
-    rc = load().iabn_backward_reduce(_ptr(z), _ptr(dz), code, g, b, float(slope), N, C, HW, wp, wb,
-                                     _stream(dev, stream))
-    _check("iabn_backward_reduce", rc)
+    _enqueue("iabn_backward_reduce", dev, stream, _ptr(z), _ptr(dz), code, g, b, float(slope), N, C,
+             HW, wp, wb)
 
 
 def iabn_backward_apply(z, dz_dx, gamma, beta, save_var, dgamma, dbeta, eps, slope, workspace,
@@ -517,9 +512,8 @@ def iabn_backward_apply(z, dz_dx, gamma, beta, save_var, dgamma, dbeta, eps, slo
     args = [_chan(t, C, dev, n) for t, n in ((gamma, "gamma"), (beta, "beta"),
             (save_var, "save_var"), (dgamma, "dgamma"), (dbeta, "dbeta"))]
     ws, wp, wb = _workspace(N, C, HW, code, dev, workspace, stream)
-    rc = load().iabn_backward_apply(_ptr(z), _ptr(dz_dx), code, *args, float(eps), float(slope),
-                                    N, C, HW, wp, wb, _stream(dev, stream))
-    _check("iabn_backward_apply", rc)
+    _enqueue("iabn_backward_apply", dev, stream, _ptr(z), _ptr(dz_dx), code, *args, float(eps),
+             float(slope), N, C, HW, wp, wb)
     return dz_dx
 
 

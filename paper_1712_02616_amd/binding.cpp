@@ -2,7 +2,8 @@
 // an entry point, takes a workspace where none is given, finds torch's
 // current stream and calls libiabn.  Marshalling only, as in __init__.py,
 // which this does not replace: whatever is not the plain case (a wrong
-// argument, a tensor subclass, an explicit stream) returns NotImplemented,
+// argument, a tensor subclass, an explicit stream, tensors on another device
+// than the current one) returns NotImplemented,
 // and the Python function then does the same checks and reports what is
 // wrong.
 //
@@ -10,6 +11,7 @@
 // took 10-13 us per call, more than the kernels of a small layer.
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <cxxabi.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -66,6 +68,10 @@ int dtype_code(at::ScalarType t) {
         default: return -1;
     }
 }
+
+// A launch on a default stream, which has no device of its own, goes to the
+// thread's current one.
+bool on_current(const at::Device& dev) { return c10::hip::current_device() == dev.index(); }
 
 template <typename Fn>
 Fn* entry(void* const* table, Op op) {
@@ -184,6 +190,8 @@ PyObject* call_checked(PyObject* const* args, Py_ssize_t n) {
             if (ws.device() != dev || !ws.is_contiguous()) return not_plain();
         }
     }
+
+    if (!on_current(dev)) return not_plain();
 
     // An allocation can wait for the device and a launch for room in the
     // queue, so other Python threads go on meanwhile.
@@ -322,6 +330,7 @@ struct Args {
         if (t.device() != dev || !t.is_contiguous()) plain = false;
         return t;
     }
+    bool ready() const { return plain && on_current(dev); }
     void* stream() const { return c10::hip::getCurrentHIPStream(dev.index()).stream(); }
     void take(at::Tensor& ws, bool own, size_t need) const {
         if (own)
@@ -353,7 +362,7 @@ PyObject* dropout_checked(void* const* table, Args& a) {
     void* const y = a.rows();
     const float p = a.number();
     const uint64_t seed = a.word(), offset = a.word();
-    if (!a.plain) return not_plain();
+    if (!a.ready()) return not_plain();
     return without_gil([&] {
         return entry<decltype(iabn_dropout)>(table, kDropout)(x, y, a.code, p, seed, offset, a.R, a.C,
                                                               a.stream());
@@ -377,7 +386,7 @@ PyObject* resnorm_forward_checked(void* const* table, Args& a) {
     float* const pre_stats = a.floats(2 * a.R);
     const float alpha = a.number(), beta = a.number(), eps = a.number(), p = a.number();
     const uint64_t seed = a.word(), offset = a.word();
-    if (!a.plain) return not_plain();
+    if (!a.ready()) return not_plain();
     return without_gil([&] {
         return entry<decltype(iabn_resnorm_forward)>(table, kResnormForward)(
             x, h, r, u, a.code, gate, groups, post, post_w, post_b, pre, pre_w, pre_b, post_stats,
@@ -411,7 +420,7 @@ PyObject* resnorm_backward_checked(void* const* table, Args& a) {
     const uint64_t seed = a.word(), offset = a.word();
     bool own;
     at::Tensor ws = a.workspace(own);
-    if (!a.plain || (dgate && dgroups != groups)) return not_plain();
+    if (!a.ready() || (dgate && dgroups != groups)) return not_plain();
     return without_gil([&] {
         a.take(ws, own, entry<decltype(iabn_resnorm_workspace_size)>(table, kResnormWorkspaceSize)(
                             a.R, a.C, groups));
@@ -434,7 +443,7 @@ PyObject* ffn_forward_checked(void* const* table, Args& a) {
     const float slope = a.number();
     bool own;
     at::Tensor ws = a.workspace(own);
-    if (!a.plain) return not_plain();
+    if (!a.ready()) return not_plain();
     return without_gil([&] {
         a.take(ws, own, entry<decltype(iabn_ffn_workspace_size)>(table, kFfnWorkspaceSize)(
                             a.R, a.C, a.F, a.code));
@@ -468,7 +477,7 @@ PyObject* ffn_backward_checked(void* const* table, Args& a) {
     const float slope = a.number();
     bool own;
     at::Tensor ws = a.workspace(own);
-    if (!a.plain) return not_plain();
+    if (!a.ready()) return not_plain();
     return without_gil([&] {
         a.take(ws, own, entry<decltype(iabn_ffn_workspace_size)>(table, kFfnWorkspaceSize)(
                             a.R, a.C, a.F, a.code));

@@ -136,10 +136,8 @@ def iabn_dropout(x, y, p, seed, offset=0, stream=None):
         return y
     rows = _Rows()
     xp, yp = rows(x, "x"), rows(y, "y")
-    rc = _iabn.load().iabn_dropout(xp, yp, rows.code, float(p), _word(seed, "seed"),
-                                   _word(offset, "offset"), rows.R, rows.C,
-                                   _iabn._stream(rows.device, stream))
-    _iabn._check("iabn_dropout", rc)
+    _iabn._enqueue("iabn_dropout", rows.device, stream, xp, yp, rows.code, float(p),
+                   _word(seed, "seed"), _word(offset, "offset"), rows.R, rows.C)
     return y
 
 
@@ -167,12 +165,10 @@ def iabn_resnorm_forward(x, h, r, u, gate=None, post_norm=None, post_weight=None
         (pre_bias, "pre_bias"))}
     stats = [rows.floats(t, 2 * R, n) for t, n in ((post_stats, "post_stats"),
                                                     (pre_stats, "pre_stats"))]
-    rc = _iabn.load().iabn_resnorm_forward(
-        *tensors, rows.code, gp, groups, post, vectors["post_weight"], vectors["post_bias"], pre,
-        vectors["pre_weight"], vectors["pre_bias"], *stats, float(alpha), float(beta), float(eps),
-        float(p), _word(seed, "seed"), _word(offset, "offset"), R, C,
-        _iabn._stream(rows.device, stream))
-    _iabn._check("iabn_resnorm_forward", rc)
+    _iabn._enqueue("iabn_resnorm_forward", rows.device, stream, *tensors, rows.code, gp, groups,
+                   post, vectors["post_weight"], vectors["post_bias"], pre, vectors["pre_weight"],
+                   vectors["pre_bias"], *stats, float(alpha), float(beta), float(eps), float(p),
+                   _word(seed, "seed"), _word(offset, "offset"), R, C)
     return r, u
 
 
@@ -210,12 +206,11 @@ def iabn_resnorm_backward(dr, du, r, h, dx, dh, gate=None, post_norm=None, post_
     stats = [rows.floats(t, 2 * R, n) for t, n in ((post_stats, "post_stats"),
                                                     (pre_stats, "pre_stats"))]
     ws, wp, wb = _iabn._take(iabn_resnorm_workspace_size(R, C, groups), rows.device, workspace, stream)
-    rc = _iabn.load().iabn_resnorm_backward(
-        *tensors, rows.code, gp, groups, post, v["post_weight"], v["post_bias"], pre, v["pre_weight"],
-        *stats, dgp, v["dpost_weight"], v["dpost_bias"], v["dpre_weight"], v["dpre_bias"],
-        float(alpha), float(beta), float(p), _word(seed, "seed"), _word(offset, "offset"), R, C, wp,
-        wb, _iabn._stream(rows.device, stream))
-    _iabn._check("iabn_resnorm_backward", rc)
+    _iabn._enqueue("iabn_resnorm_backward", rows.device, stream, *tensors, rows.code, gp, groups,
+                   post, v["post_weight"], v["post_bias"], pre, v["pre_weight"], *stats, dgp,
+                   v["dpost_weight"], v["dpost_bias"], v["dpre_weight"], v["dpre_bias"],
+                   float(alpha), float(beta), float(p), _word(seed, "seed"),
+                   _word(offset, "offset"), R, C, wp, wb)
     return dx, dh
 
 
@@ -243,9 +238,8 @@ def iabn_ffn_forward(x, w_gate, w_up, w_down, y, g=None, u=None, act="silu", slo
     yp = rows(y, "y")
     gp, up = rows.matrix(g, R, F, "g", True), rows.matrix(u, R, F, "u", True)
     ws, wp, wb = _iabn._take(iabn_ffn_workspace_size(R, C, F, rows.code), rows.device, workspace, stream)
-    rc = _iabn.load().iabn_ffn_forward(xp, *weights, yp, gp, up, rows.code, code, float(slope), R, C, F,
-                                       wp, wb, _iabn._stream(rows.device, stream))
-    _iabn._check("iabn_ffn_forward", rc)
+    _iabn._enqueue("iabn_ffn_forward", rows.device, stream, xp, *weights, yp, gp, up, rows.code,
+                   code, float(slope), R, C, F, wp, wb)
     return y
 
 
@@ -266,7 +260,6 @@ def iabn_ffn_backward(dy, x, g, u, w_gate, w_up, w_down, dx, dg, du, dw_gate, dw
         (dg, R, F, "dg"), (du, R, F, "du"), (dw_gate, F, C, "dw_gate"), (dw_up, F, C, "dw_up"),
         (dw_down, C, F, "dw_down"))]
     ws, wp, wb = _iabn._take(iabn_ffn_workspace_size(R, C, F, rows.code), rows.device, workspace, stream)
-    rc = _iabn.load().iabn_ffn_backward(dyp, xp, *kept, *weights, *outs, rows.code, code, float(slope),
-                                        R, C, F, wp, wb, _iabn._stream(rows.device, stream))
-    _iabn._check("iabn_ffn_backward", rc)
+    _iabn._enqueue("iabn_ffn_backward", rows.device, stream, dyp, xp, *kept, *weights, *outs,
+                   rows.code, code, float(slope), R, C, F, wp, wb)
     return dx

@@ -131,3 +131,38 @@ def test_a_new_workspace_belongs_to_the_calls_stream(seen, call, handle):
 def test_the_callers_workspace_is_taken_as_it_is(seen, call):
     CALLS[call](stream=Stream(99), workspace=t(1 << 16, dtype=torch.uint8))
     assert seen.allocated == [] and seen.called[0][2] == 99
+
+
+ALL = dict(CALLS)
+ALL.update({
+    "dropout": lambda **kw: iabn.iabn_dropout(t(4, 16), t(4, 16), 0.1, 1, **kw),
+    "resnorm_forward": lambda **kw: iabn.iabn_resnorm_forward(t(4, 16), None, t(4, 16), None, **kw),
+    "forward_train_noalloc": lambda **kw: iabn.iabn_forward_train_noalloc(t(2, 3, 4), *[t(3)] * 6, **kw),
+    "forward_eval": lambda **kw: iabn.iabn_forward_eval(t(2, 3, 4), *[t(3)] * 4, **kw),
+    "backward_ii": lambda **kw: iabn.iabn_backward_ii(t(2, 3, 4), t(2, 3, 4), *[t(3)] * 5, **kw),
+    "std_forward_train": lambda **kw: iabn.iabn_std_forward_train(t(2, 3, 4), t(2, 3, 4), *[t(3)] * 6, **kw),
+    "std_backward": lambda **kw: iabn.iabn_std_backward(*[t(2, 3, 4)] * 3, *[t(3)] * 6, **kw),
+    "ckpt_forward_train": lambda **kw: iabn.iabn_ckpt_forward_train(t(2, 3, 4), t(2, 3, 4), *[t(3)] * 6, **kw),
+    "ckpt_recompute": lambda **kw: iabn.iabn_ckpt_recompute(t(2, 3, 4), t(2, 3, 4), t(3), t(3), **kw),
+    "ckpt_backward": lambda **kw: iabn.iabn_ckpt_backward(t(2, 3, 4), t(2, 3, 4), *[t(3)] * 5, **kw),
+    "forward_stats": lambda **kw: iabn.iabn_forward_stats(t(2, 3, 4), t(4096), **kw),
+    "forward_apply": lambda **kw: iabn.iabn_forward_apply(t(2, 3, 4), *[t(3)] * 6, 1e-5, 0.1, 0.01, t(4096), **kw),
+    "backward_reduce": lambda **kw: iabn.iabn_backward_reduce(*[t(2, 3, 4)] * 2, t(3), t(3), 0.01, t(4096), **kw),
+    "backward_apply": lambda **kw: iabn.iabn_backward_apply(*[t(2, 3, 4)] * 2, *[t(3)] * 5, 1e-5, 0.01, t(4096), **kw),
+})
+
+
+def test_every_entry_point_is_here():
+    on_a_stream = {n[len("iabn_"):] for n in iabn.__all__
+                   if n.startswith("iabn_") and not n.endswith(("_size", "_string", "version", "plan"))}
+    assert on_a_stream == set(ALL)
+
+
+@pytest.mark.parametrize("call", ALL)
+@pytest.mark.parametrize("stream", [None, 0, 99])
+def test_the_tensors_device_is_current(seen, call, stream):
+    """The default stream has one handle for every device (NULL), which means
+    the current one's."""
+    ALL[call](stream=stream)
+    assert seen.called == [("iabn_" + call, DEVICE, {None: 7, 0: None, 99: 99}[stream])]
+    assert seen.device is None
