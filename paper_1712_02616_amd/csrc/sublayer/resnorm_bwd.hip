@@ -1,5 +1,7 @@
 // Backward of the norms around a block (resnorm_fwd.hip).  Per row, with
-// rhat, hhat the normalised rows of r and h (from the saved statistics):
+// rhat, hhat the normalised rows of r and h (from the saved statistics; (v - mean)*rho,
+// whose subtraction loses nothing where the mean is large against the spread, as
+// v*rho - mean*rho would):
 //
 //   a  = du*w',  g = dr + rho'*(a - [mean a] - rhat*mean(a*rhat))
 //   dx = alpha*g,  e = beta*g*D,  dn = e*gate
@@ -204,7 +206,7 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
                     if (kLean && a.pre_w) vector(a.pre_w, k, pre_w[k]);
 #pragma unroll
                     for (int j = 0; j < kChunk; ++j) {
-                        hat[k][j] = inside_row<FILL>(c[k], j, fmaf(hat[k][j], rstd, -mean * rstd));
+                        hat[k][j] = inside_row<FILL>(c[k], j, (hat[k][j] - mean) * rstd);
                         tw[k][j] = fmaf(d[k][j], hat[k][j], tw[k][j]);
                         d[k][j] *= pre_w[k][j];
                         s2 = fmaf(d[k][j], hat[k][j], s2);
@@ -254,7 +256,7 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
                     // From here g is e = beta*g*D, then dn, then dn*w.
 #pragma unroll
                     for (int j = 0; j < kChunk; ++j) {
-                        hat[k][j] = a.h ? inside_row<FILL>(c[k], j, fmaf(hat[k][j], rstd, -mean * rstd)) : 0.0f;
+                        hat[k][j] = a.h ? inside_row<FILL>(c[k], j, (hat[k][j] - mean) * rstd) : 0.0f;
                         if constexpr (FILL != kFull) g[k][j] = inside_row<FILL>(c[k], j, g[k][j]);
                     }
                     if (a.drop.threshold)
