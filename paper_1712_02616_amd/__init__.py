@@ -20,6 +20,7 @@ stream for the tensor's device).
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import importlib.util
 import math
@@ -241,11 +242,11 @@ def _take(need, device, workspace, stream):
     this call has released it, which is before the kernels have run.  (A block
     of another stream may have work there that is not done yet.)"""
     if workspace is None:
-        if stream is None:
-            stream = torch.cuda.current_stream(device)
-        elif not isinstance(stream, torch.cuda.Stream):
+        if stream is not None and not isinstance(stream, torch.cuda.Stream):
             stream = torch.cuda.ExternalStream(int(stream), device=device)
-        with torch.cuda.stream(stream):
+        # (A change of the current stream costs more than all else here.)
+        same = stream is None or stream.cuda_stream == torch.cuda.current_stream(device).cuda_stream
+        with contextlib.nullcontext() if same else torch.cuda.stream(stream):
             workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
     if workspace.device != device or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on %s" % device)

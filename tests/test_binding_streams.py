@@ -166,3 +166,11 @@ def test_the_tensors_device_is_current(seen, call, stream):
     ALL[call](stream=stream)
     assert seen.called == [("iabn_" + call, DEVICE, {None: 7, 0: None, 99: 99}[stream])]
     assert seen.device is None
+
+
+@pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("stream", [None, 7])
+def test_the_current_stream_is_not_changed_for_itself(seen, call, stream, monkeypatch):
+    monkeypatch.setattr(torch.cuda, "stream", None)
+    CALLS[call](stream=stream)
+    assert len(seen.allocated) == 1 and seen.called[0][2] == 7
