@@ -512,7 +512,7 @@ PyMethodDef methods[] = {
     {"dropout", method<dropout_checked, 5>(), METH_FASTCALL, "iabn_dropout, as call"},
     {"resnorm_forward", method<resnorm_forward_checked, 19>(), METH_FASTCALL,
      "iabn_resnorm_forward, as call"},
-    {"resnorm_backward", method<resnorm_backward_checked, 24>(), METH_FASTCALL,
+    {"resnorm_backward", method<resnorm_backward_checked, 25>(), METH_FASTCALL,
      "iabn_resnorm_backward, as call"},
     {"ffn_forward", method<ffn_forward_checked, 10>(), METH_FASTCALL, "iabn_ffn_forward, as call"},
     {"ffn_backward", method<ffn_backward_checked, 16>(), METH_FASTCALL, "iabn_ffn_backward, as call"},
