@@ -62,7 +62,7 @@ constexpr int64_t kBwdMinRows = 4;
 
 ResnormSplit split_rows(int64_t R, int64_t C, int64_t groups, int64_t waves_on_cu) {
     if (R == 0) return {1, 0, 0, 0, 0};
-    const RowShape shape = row_shape(static_cast<int>((C + kChunk - 1) / kChunk), kBwdOneWave);
+    const RowShape shape = row_shape(chunks_of(C), kBwdOneWave);
     // (A block of one-wave rows has four of them.)
     const int64_t on_cu = shape.waves == 1 ? 2 : waves_on_cu / shape.waves;
     const int64_t target = kCUs * (on_cu > 1 ? on_cu : 1);
@@ -214,7 +214,7 @@ int iabn_resnorm_forward(const void* x, const void* h, void* r, void* u, int dty
     a.R = R;
     a.gate_rows = gate ? R / groups : R;
     a.C = static_cast<int>(C);
-    a.chunks = static_cast<int>((C + kChunk - 1) / kChunk);
+    a.chunks = chunks_of(C);
     launch_resnorm_fwd(dtype, a, static_cast<hipStream_t>(stream));
     return launched("resnorm_forward");
 }
@@ -280,7 +280,7 @@ int iabn_resnorm_backward(const void* dr, const void* du, const void* r, const v
     a.gate_rows = gate ? R / groups : R;
     a.gate_each_row = gate && groups == R;
     a.C = static_cast<int>(C);
-    a.chunks = static_cast<int>((C + kChunk - 1) / kChunk);
+    a.chunks = chunks_of(C);
     a.part = static_cast<float*>(workspace);
     a.gpart = a.part + static_cast<size_t>(4) * a.split.blocks * C;
     launch_resnorm_bwd(dtype, a, st);

@@ -51,7 +51,7 @@ void launch_zero(void* p, int64_t bytes, hipStream_t st) {
 
 bool launch_dropout(int dtype, const void* x, void* y, int64_t R, int C, const Dropout& d,
                     hipStream_t st) {
-    const int chunks = (C + kChunk - 1) / kChunk;
+    const int chunks = chunks_of(C);
     const int64_t groups = R * chunks, blocks = (groups + kThreads - 1) / kThreads;
     // (A launch holds fewer than 2^32 threads.)
     const dim3 grid(static_cast<uint32_t>(blocks < kMaxBlocks ? blocks : kMaxBlocks));

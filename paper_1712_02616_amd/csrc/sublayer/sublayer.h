@@ -17,6 +17,11 @@ namespace iabn_impl {
 // one by one.
 constexpr int kChunk = 8;
 
+// Chunks of a row of C elements, C < 2^31 (C + 7 in an int would overflow for the
+// last seven widths).
+constexpr int chunks_of(int64_t C) { return static_cast<int>((C + kChunk - 1) / kChunk); }
+static_assert(chunks_of((int64_t(1) << 31) - 1) == 1 << 28 && chunks_of((int64_t(1) << 31) - 8) == (1 << 28) - 1, "");
+
 template <int DT>
 struct ChunkOf {
     using T = typename Elem<DT>::T;
