@@ -59,6 +59,14 @@ int check_gate(const void* gate, int64_t groups, int64_t R) {
 // with 8, 81 with 12; masked ones spill: (1031, 1501) fp32 20.6, 31.7).
 constexpr int64_t kCUs = 256;
 constexpr int64_t kBwdMinRows = 4;
+// A wave's fp32 sum over its rows, one after the other, has at most so many
+// terms: what a chain can lose, 1024 * 2^-24 of its terms, does not grow with the
+// rows (the blocks' sums are joined in double).  Past 2^20 blocks' worth of rows
+// it does again, which rows of 8 or more elements on one GPU do not reach.
+constexpr int64_t kChain = 1024;
+constexpr int64_t kMaxBwdBlocks = int64_t(1) << 20;
+
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 ResnormSplit split_rows(int64_t R, int64_t C, int64_t groups, int64_t waves_on_cu) {
     if (R == 0) return {1, 0, 0, 0, 0};
@@ -66,23 +74,27 @@ ResnormSplit split_rows(int64_t R, int64_t C, int64_t groups, int64_t waves_on_c
     // (A block of one-wave rows has four of them.)
     const int64_t on_cu = shape.waves == 1 ? 2 : waves_on_cu / shape.waves;
     const int64_t target = kCUs * (on_cu > 1 ? on_cu : 1);
+    int64_t most_rows = kChain * (shape.waves == 1 ? 4 : 1);  // of a block
+    if (most_rows < div_up(R, kMaxBwdBlocks)) most_rows = div_up(R, kMaxBwdBlocks);
     ResnormSplit s;
     s.groups = groups > 0 && groups < R ? groups : 1;
     s.group_rows = R / s.groups;
+    int64_t per = 1, segs = 1;
     if (s.groups >= target) {
-        s.per_group = 1;
-        s.segs = static_cast<int>((s.groups + target - 1) / target);
-        s.blocks = static_cast<int>((s.groups + s.segs - 1) / s.segs);
+        segs = div_up(s.groups, target);
     } else {
         const int64_t fewest = kCUs / s.groups, two = (s.group_rows + 1) / 2;
-        const int64_t most = (s.group_rows + kBwdMinRows - 1) / kBwdMinRows;
-        int64_t per = target / s.groups;
+        const int64_t most = div_up(s.group_rows, kBwdMinRows);
+        per = target / s.groups;
         if (per > most) per = most;
         if (per < fewest) per = fewest < two ? fewest : two;
-        s.per_group = static_cast<int>(per);
-        s.segs = 1;
-        s.blocks = static_cast<int>(s.groups * per);
     }
+    if (per < div_up(s.group_rows, most_rows)) per = div_up(s.group_rows, most_rows);
+    if (per > 1) segs = 1;
+    else if (segs > 1 && segs * s.group_rows > most_rows) segs = most_rows / s.group_rows;
+    s.per_group = static_cast<int>(per);
+    s.segs = static_cast<int>(segs);
+    s.blocks = static_cast<int>(div_up(s.groups * per, segs));
     return s;
 }
 

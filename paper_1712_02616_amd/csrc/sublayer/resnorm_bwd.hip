@@ -17,7 +17,8 @@
 // therefore goes through many rows (a segment); the next row's loads are
 // issued before this row's sums (two rows ahead were no faster).  Each block
 // leaves its columns' sums in the workspace and a second kernel adds the
-// blocks' in double, in a fixed order.
+// blocks' in double, in a fixed order.  (A wave adds at most 1024 rows in fp32: more
+// rows are more blocks.)
 //
 // bf16, RMS norms, gate and dropout: (16384, 2048) 83 us and 7 for the sums,
 // against 71 us for its 403 MB of HBM traffic at 5.7 TB/s (rows that fill their
@@ -344,6 +345,7 @@ void resnorm_bwd_kernel(ResnormBwdArgs a, int waves) {
 // out[c] = sum over `count` rows of part[., c], in double.  A block takes 32
 // columns; 8 of its threads share a column.
 constexpr int kSumCols = 32;
+constexpr int64_t kMaxSumGroups = 1 << 15;  // of a launch; more take turns
 
 template <int DT>
 __device__ __forceinline__ void column_sum(const float* __restrict__ part, int count, int C,
@@ -376,9 +378,11 @@ __global__ __launch_bounds__(kThreads) void resnorm_bwd_sum_kernel(ResnormBwdArg
         if (out)
             column_sum<IABN_F32>(a.part + int64_t(blockIdx.y) * a.split.blocks * a.C, a.split.blocks, a.C, out);
     } else {
-        const int64_t g = blockIdx.y - 4;
-        column_sum<DT>(a.gpart + g * a.split.per_group * a.C, a.split.per_group, a.C,
-                       static_cast<typename Elem<DT>::T*>(a.dgate) + g * a.C);
+        for (int64_t g = blockIdx.y - 4; g < a.split.groups; g += gridDim.y - 4) {
+            column_sum<DT>(a.gpart + g * a.split.per_group * a.C, a.split.per_group, a.C,
+                           static_cast<typename Elem<DT>::T*>(a.dgate) + g * a.C);
+            __syncthreads();
+        }
     }
 }
 
@@ -419,7 +423,7 @@ void launch(const ResnormBwdArgs& a, hipStream_t st) {
     const bool gate = a.dgate && a.split.per_group > 1 && !a.gate_each_row;
     if (a.dpost_w || a.dpost_b || a.dpre_w || a.dpre_b || gate) {
         const dim3 grid((a.C + kSumCols - 1) / kSumCols,
-                        4 + (gate ? static_cast<uint32_t>(a.split.groups) : 0u));
+                        4 + (gate ? static_cast<uint32_t>(min(a.split.groups, kMaxSumGroups)) : 0u));
         resnorm_bwd_sum_kernel<DT><<<grid, kThreads, 0, st>>>(a);
     }
 }
