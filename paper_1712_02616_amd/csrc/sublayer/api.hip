@@ -42,7 +42,7 @@ int check_norm(const char* what, int kind, const void* weight, const void* bias)
 }
 
 int check_gate(const void* gate, int64_t groups, int64_t R) {
-    if (gate == nullptr) return IABN_OK;
+    if (gate == nullptr || (R == 0 && groups == 0)) return IABN_OK;
     if (groups < 1 || R % groups != 0)
         return fail(IABN_ERR_SHAPE, "%lld rows of the gate do not divide R=%lld", (long long)groups,
                     (long long)R);
