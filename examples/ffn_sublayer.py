@@ -82,7 +82,9 @@ class Sublayer(torch.autograd.Function):
                                    seed=ctx.seed)
         du = torch.empty_like(u)
         dws = [torch.empty_like(w) for w in (w_gate, w_up, w_down)]
-        # The projections' gradients overwrite the projections.
+        # The projections' gradients overwrite the projections, which autograd is
+        # told: a second backward through this graph fails.
+        torch.autograd.graph.increment_version((g, up))
         iabn.iabn_ffn_backward(dh, u, g, up, w_gate, w_up, w_down, du, g, up, *dws)
         return (dx, du, *dws, dgate, dpost, dpre, None, None)
 
