@@ -488,7 +488,10 @@ void launch_planned(GemmArgs a, int products, hipStream_t st) {
             // (Through registers, and in fp32, it would spill them.)
             if constexpr (DMA && DT != IABN_F32) launch_tiles<DT, KIND, 256, 256, 2, 4, DMA>(a, products, st);
             break;
-        case kTile128: launch_tiles<DT, KIND, 128, 128, 2, 2, DMA>(a, products, st); break;
+        case kTile128:
+            // (Through registers, two blocks of 64x128 take less: the plan's costs.)
+            if constexpr (DMA) launch_tiles<DT, KIND, 128, 128, 2, 2, DMA>(a, products, st);
+            break;
         case kTile64: launch_tiles<DT, KIND, 64, 128, 2, 2, DMA>(a, products, st); break;
         case kTile32: launch_tiles<DT, KIND, 32, 128, 2, 2, DMA>(a, products, st); break;
     }

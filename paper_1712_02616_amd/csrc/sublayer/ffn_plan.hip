@@ -15,15 +15,17 @@ int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // larger tile reads half of LDS per product but holds a CU alone; two blocks
 // of 128x128 hide each other's waits (0.68 us for both, 0.67 for one).  fp32
 // is bound by the matrix cores at every size: the tiles matter where they do
-// not fill the last round.
+// not fill the last round.  Through registers, 128x128 is no choice: 1.5, 3.0, 4.4,
+// 5.9 us a step (fp32 2.65, 5.2, 7.8, 10.4), more than two blocks of 64x128 at every
+// number of blocks, and the same ends.
 struct TileCost {
     float step[4], ends;
 };
 // [fp32][direct][tile]
 constexpr TileCost kCost[2][2][4] = {
-    {{{{0, 0, 0, 0}, 0}, {{1.5f, 3.0f, 4.4f, 5.9f}, 2}, {{1.1f, 1.3f, 2.0f, 2.6f}, 1}, {{0.9f, 1.1f, 1.4f, 2.2f}, 0.5f}},
+    {{{{0, 0, 0, 0}, 0}, {{0, 0, 0, 0}, 0}, {{1.1f, 1.3f, 2.0f, 2.6f}, 1}, {{0.9f, 1.1f, 1.4f, 2.2f}, 0.5f}},
      {{{1.27f, 2.54f, 3.81f, 5.08f}, 8}, {{0.67f, 0.68f, 1.36f, 1.4f}, 1.6f}, {{0.32f, 0.55f, 0.75f, 1.16f}, 0.8f}, {{0.26f, 0.45f, 0.68f, 0.87f}, 0.4f}}},
-    {{{{0, 0, 0, 0}, 0}, {{2.65f, 5.2f, 7.8f, 10.4f}, 4}, {{1.6f, 2.6f, 4.8f, 5.0f}, 2}, {{1.0f, 1.6f, 2.25f, 3.2f}, 1}},
+    {{{{0, 0, 0, 0}, 0}, {{0, 0, 0, 0}, 0}, {{1.6f, 2.6f, 4.8f, 5.0f}, 2}, {{1.0f, 1.6f, 2.25f, 3.2f}, 1}},
      {{{0, 0, 0, 0}, 0}, {{2.05f, 3.7f, 7.2f, 7.4f}, 4}, {{1.1f, 1.93f, 2.8f, 3.9f}, 2}, {{0.63f, 1.02f, 1.5f, 1.95f}, 1}}}};
 constexpr float kGatingEnds = 3.0f;  // kGemmDh's end is so much longer
 // 16-bit rows at odd addresses, through registers: the loads are what a step
