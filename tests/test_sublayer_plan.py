@@ -73,3 +73,27 @@ def test_instances_are_the_tiles_that_are_chosen():
         dt, kind, tm, tn = (int(m.group(i)) for i in range(1, 5))
         have.add((list(DTYPES)[dt], KINDS[kind], m.group(5) == "true", (tm, tn)))
     assert have == scan()
+
+
+# Ragged sizes whose products take every instance of the tiles, with split sums
+# and without where both occur (test_gpu_ffn_tiles.py runs them).
+SIZES = [
+    ("bf16", 65, 1, 1), ("bf16", 65, 2, 4236), ("bf16", 65, 7, 341), ("bf16", 65, 10, 386), ("bf16", 235, 646, 4824),
+    ("bf16", 891, 78, 88), ("bf16", 1748, 2352, 8956), ("bf16", 2101, 4, 729), ("bf16", 2712, 770, 5674),
+    ("bf16", 5384, 1170, 12), ("bf16", 7063, 152, 1544), ("bf16", 8239, 1524, 796), ("bf16", 9614, 2, 2),
+    ("f16", 65, 1, 1), ("f16", 65, 1, 335), ("f16", 65, 8, 454), ("f16", 249, 2, 1040), ("f16", 321, 226, 3955),
+    ("f16", 510, 442, 6692), ("f16", 836, 76, 66), ("f16", 1745, 3068, 2328), ("f16", 4258, 10, 5700),
+    ("f16", 4629, 2662, 2896), ("f16", 8618, 1, 2), ("f16", 9372, 324, 704), ("f32", 65, 2, 4232),
+    ("f32", 219, 134, 94), ("f32", 612, 640, 5830), ("f32", 709, 1, 734), ("f32", 1338, 516, 2), ("f32", 5657, 10, 7762),
+    ("f32", 7247, 30, 9706), ("f32", 7928, 398, 1004), ("f32", 8720, 798, 188), ("f32", 9431, 2, 2)]
+
+
+def test_sizes_take_every_instance():
+    plan = planner()
+    taken = {(size[0],) + p for size in SIZES for p in products(plan, *size)}
+    assert {t[:4] for t in taken} == scan()
+    # The products that may split their sum do both, where their tiles do at all.
+    for dtype in DTYPES:
+        for kind in ("down", "dx", "dw"):
+            for direct, tile in ((True, (128, 128)), (True, (64, 128)), (True, (32, 128))):
+                assert {t[4] for t in taken if t[:4] == (dtype, kind, direct, tile)} == {False, True}
