@@ -73,3 +73,40 @@ def test_values(act, dtype, M):
                                act=act, slope=0.125)
         near("du", du[:, 0], a, rel * asize, d)
         near("dg", dg[:, 0], da, rel * dsize, d)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "leaky"])
+@pytest.mark.parametrize("dtype,large", [("f32", 3e38), ("f16", 6e4), ("bf16", 3e38)])
+@pytest.mark.parametrize("M", [8, 80])
+def test_large_values(act, dtype, large, M):
+    """Far out the activations are v (or v's slope) and 0; a NaN and an infinity
+    stay in their rows."""
+    say("activation %s %s: large values" % (act, dtype))
+    d = TORCH_DTYPES[dtype]
+    inf, nan = float("inf"), float("nan")
+    v = torch.tensor([large, 100.0, 0.0, -0.0, -150.0, -large, inf, nan]).repeat(M // 8).to(d)
+    slope = 0.0
+    g, u = v[:, None].cuda(), torch.ones(M, 1, dtype=d, device="cuda")
+    low = 0.0 if act == "leaky" else 0.5
+    a = torch.tensor([float(v[0]), 100.0, 0.0, 0.0, 0.0, 0.0, inf, nan]).repeat(M // 8)
+    da = torch.tensor([1.0, 1.0, low or 1.0, low or 1.0, 0.0, 0.0, 1.0, nan]).repeat(M // 8)
+    # The block as a whole: h = act(g), y = h.
+    x = torch.stack([v, torch.ones_like(v)], 1)
+    x[torch.isinf(v), 0] = large  # (0 * inf would be another value's NaN)
+    x[torch.isnan(v), 0] = 1.0
+    wg = torch.tensor([[1.0, 0.0]], dtype=d, device="cuda")
+    wu = torch.tensor([[0.0, 1.0]], dtype=d, device="cuda")
+    wd = torch.tensor([[1.0], [0.0]], dtype=d, device="cuda")
+    y = torch.empty(M, 2, dtype=d, device="cuda")
+    iabn.iabn_ffn_forward(x.cuda(), wg, wu, wd, y, act=act, slope=slope)
+    finite = torch.isfinite(v)
+    assert torch.equal(y[:, 0].cpu()[finite] + 0.0, a.to(d)[finite] + 0.0)
+    dy = torch.tensor([[1.0, 0.0]], dtype=d, device="cuda").repeat(M, 1)
+    dx, dg, du = torch.empty(M, 2, dtype=d, device="cuda"), torch.empty_like(g), torch.empty_like(g)
+    iabn.iabn_ffn_backward(dy, x.cuda(), g, u, wg, wu, wd, dx, dg, du, *[torch.empty_like(w) for w in (wg, wu, wd)],
+                           act=act, slope=slope)
+    rows = ~torch.isnan(v)
+    assert torch.equal(du[:, 0].cpu()[rows] + 0.0, a.to(d)[rows] + 0.0)
+    assert torch.equal(dg[:, 0].cpu()[finite] + 0.0, da.to(d)[finite] + 0.0)
+    if act != "leaky":
+        assert torch.isnan(du[:, 0].cpu()[~rows]).all() and torch.isnan(dg[:, 0].cpu()[~rows]).all()
