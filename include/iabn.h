@@ -436,7 +436,8 @@ int iabn_resnorm_backward(const void *dr, const void *du, const void *r, const v
                           int64_t C, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Activations of the gated feed-forward block.  LEAKY takes slope (0: a
- * rectifier); its derivative at 0 is 1.  GELU is the exact one, v*Phi(v). */
+ * rectifier); its derivative at 0 is 1.  GELU is the exact one, v*Phi(v).  Of an
+ * infinite v (one that overflowed when it was stored) all give their limits. */
 typedef enum { IABN_ACT_SILU = 0, IABN_ACT_GELU = 1, IABN_ACT_LEAKY = 2 } iabn_act_t;
 
 /*

@@ -45,6 +45,12 @@ struct GemmArgs {
 // out[z][m][n] = sum over the splits, rounded once.
 void launch_join(int dtype, const GemmArgs& a, int products, hipStream_t st);
 
+// v with its infinities (below: the negative one) as the largest finite values.
+__device__ __forceinline__ float from_below(float v) { return fmaxf(v, -__FLT_MAX__); }
+__device__ __forceinline__ float finite_part(float v) {
+    return __builtin_amdgcn_fmed3f(v, -__FLT_MAX__, __FLT_MAX__);
+}
+
 // act(v) and its derivative, for values stored as DT, each to an error relative to
 // itself (the tails too, where they are small).  fp32 values: the library's
 // functions and a division.  16-bit ones: the hardware's exponential and
@@ -57,14 +63,17 @@ void launch_join(int dtype, const GemmArgs& a, int products, hipStream_t st);
 // library's function.  P has degree 7; p and P were fitted here to the least
 // largest relative error over all v (iterated weighted least squares on
 // Chebyshev nodes in t): 6.8e-7, evaluated in fp32 9.6e-7.
+//
+// An infinite v (a projection that overflowed when it was stored) gives the limits,
+// no inf * 0; a NaN stays one through s, c or the slope.
 template <int ACT, int DT>
 __device__ __forceinline__ void activate(float slope, float v, float& a, float& da) {
     if constexpr (ACT == IABN_ACT_SILU) {
         float s;
         if constexpr (DT == IABN_F32) s = 1.0f / (1.0f + expf(-v));
         else s = __builtin_amdgcn_rcpf(1.0f + __expf(-v));
-        a = v * s;
-        da = s * (1.0f + v * (1.0f - s));
+        a = from_below(v) * s;
+        da = s * (1.0f + finite_part(v) * (1.0f - s));
     } else if constexpr (ACT == IABN_ACT_GELU) {
         float e, c;
         if constexpr (DT == IABN_F32) {
@@ -83,10 +92,10 @@ __device__ __forceinline__ void activate(float slope, float v, float& a, float& 
             q *= 0.5f * t * e;  // Phi(-|v|)
             c = v < 0.0f ? q : 1.0f - q;
         }
-        a = v * c;
-        da = c + v * e * 0.39894228040143268f;
+        a = from_below(v) * c;
+        da = c + finite_part(v) * e * 0.39894228040143268f;
     } else {
-        a = v >= 0.0f ? v : slope * v;
+        a = v >= 0.0f ? v : slope == 0.0f && v < 0.0f ? 0.0f : slope * v;
         da = v >= 0.0f ? 1.0f : slope;
     }
 }
