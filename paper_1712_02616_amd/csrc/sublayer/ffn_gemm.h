@@ -270,14 +270,16 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
         };
         // At `meet` what was fetched has arrived (each wave has waited for its
         // own) and the reads of the buffer to be filled next have ended.  The
-        // largest tile, alone on its CU, has the matrix cores at work on both
-        // sides of it: the fragments of a phase are read while the one before is
-        // multiplied, those of the next step's first phase while this one's last
-        // is ((4096, 2048 -> 2x8192) bf16 250 -> 245 us, the products of two
-        // sums (8192, 2x10240 -> 4096) 1032 -> 1002).  Of the smaller ones two
-        // or more share a CU; there every read of a step before its first
-        // product is better ((4096, 1024) fp16 weights' gradients of 2085 tokens
-        // 37 us against 40).
+        // largest tile, alone on its CU, goes in phases: the fragments of one
+        // are read while the one before is multiplied (all reads of a step first
+        // would spill: (4096, 2048 -> 2x8192) bf16 517 us instead of 280, the
+        // products of two sums (8192, 2x10240 -> 4096) 3098 instead of 1020),
+        // those of the next step's first phase while this one's last is, so that
+        // products run on both sides of the barrier (237 us instead of 243 in a
+        // first pass; nothing in a long run, where the clock has fallen).  Of the
+        // smaller tiles two or more share a CU; there every read of a step before
+        // its first product is better ((4096, 1024) fp16 weights' gradients of
+        // 2085 tokens 37 us against 40).
         const auto meet = []() __attribute__((always_inline)) {
             __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
             asm volatile("" ::: "memory");

@@ -100,3 +100,21 @@ def test_normalisation_layer():
     for _ in range(3):
         got = run(side, lambda: _release_a_block_in_use(nbytes))
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_the_default_stream_by_its_handle():
+    """stream=0 with another stream current: the workspace is the default stream's."""
+    M, C, F, d = 100, 96, 128, torch.float32
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    new = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    x, wg, wu, wd = new(M, C), new(F, C), new(F, C), new(C, F)
+    want, got = torch.empty_like(x), torch.empty_like(x)
+    iabn.iabn_ffn_forward(x, wg, wu, wd, want)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        _release_a_block_in_use(iabn.iabn_ffn_workspace_size(M, C, F, d))
+        iabn.iabn_ffn_forward(x, wg, wu, wd, got, stream=0)
+        assert torch.cuda.current_stream() == side
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
