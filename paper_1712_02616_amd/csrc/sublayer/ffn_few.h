@@ -7,7 +7,7 @@
 // long runs; their sums meet in LDS.
 //
 // Bound by HBM: one token (4096 -> 2x10240) bf16 34 us for 168 MB, 4.9 TB/s, and
-// 16 us for the 84 MB back, 5.3; 24 tokens (2048 -> 2x8192) fp16 16 us, 4.3, and
+// 16 us for the 84 MB back, 5.3; 24 tokens (2048 -> 2x8192) fp16 17 us, 4.0, and
 // back 12 and 4 to join, where the tokens' h, read by every block, is more
 // traffic than the weights.  The weights' loads keep lines in the caches: a line
 // is two loads (one token: 32 and 16 us, non-temporal 35 and 21).

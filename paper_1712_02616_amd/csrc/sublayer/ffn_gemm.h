@@ -13,13 +13,13 @@
 // Bound by the matrix cores at the clock that their power leaves, which falls in
 // a long run of products (random values; the fastest of 20 passes and the
 // median; a large library product 1.39-1.61 PFLOP/s NT, 1.2-1.37 NN, 1.05-1.16
-// TN).  bf16: dx (8192, 2x10240 -> 4096) 1.026 and 1.049 ms, 1.34 and 1.31
-// PFLOP/s; both projections (4096, 2048 -> 2x8192) 244 and 276 us, 1.12 and 1.00
+// TN).  bf16: dx (8192, 2x10240 -> 4096) 1.000 and 1.027 ms, 1.37 and 1.34
+// PFLOP/s; both projections (4096, 2048 -> 2x8192) 239 and 274 us, 1.15 and 1.00
 // (200 MB of results leave in that time, of which a 256x256 tile, alone on its
-// CU, hides none); the weights' gradients over 8192 tokens 1.32 and 1.27 (gate
-// and up), 1.06 and 1.01 (down); dh with the gating's gradient (8192, 4096 ->
-// 10240) 631 and 645 us, 1.09 and 1.07 (840 MB in its epilogue); the down
-// projection (4096, 8192 -> 2048) 112 and 119 us, 1.22 and 1.15.  fp32, the sizes
+// CU, hides none); the weights' gradients over 8192 tokens 1.36 and 1.32 (gate
+// and up), 1.08 and 1.02 (down); dh with the gating's gradient (8192, 4096 ->
+// 10240) 633 and 643 us, 1.09 and 1.07 (840 MB in its epilogue); the down
+// projection (4096, 8192 -> 2048) 110 and 119 us, 1.25 and 1.15.  fp32, the sizes
 // of that forward: 1.94 and 0.95 ms, 141 and 144 TFLOP/s (the library 153).
 #pragma once
 

@@ -14,11 +14,12 @@
 //
 // Rows of up to 1024 elements are one wave's, whose sums need no barrier
 // ((32768, 1024) fp16, both norms layer norms, a gate per sample, dropout:
-// 62 us, 69 in two waves); wider ones have a block of their own.  That case is
-// bound by its arithmetic as much as by HBM, where its 268 MB take 47 us at 5.7
-// TB/s.  (16384, 2048) bf16, the same traffic, takes 60 us with RMS norms, a
-// gate and dropout, and 46, 5.8 TB/s, with no more than the sum and the RMS norm
-// before the next block.  One row of 2048 bf16: 2.8 us, a launch.
+// 61 us, 69 in two waves); wider ones have a block of their own.  That case is
+// bound by its arithmetic (vector instructions in 0.79 of the busy cycles) as much
+// as by HBM, where its 270 MB (each tensor once) take 47 us at 5.7 TB/s.  (16384,
+// 2048) bf16, the same traffic, takes 60 us with RMS norms, a gate and dropout,
+// and 46, 5.8 TB/s, with no more than the sum and the RMS norm before the next
+// block.  One row of 2048 bf16: 2.5 us, a launch.
 #include "sublayer.h"
 
 namespace iabn_impl {
