@@ -48,7 +48,8 @@ def test_small_terms_after_a_large_one():
 
 @pytest.mark.parametrize("rows,width,groups,dtype", [
     (3_000_017, 8, 0, torch.float32), (600 * 7001, 8, 600, torch.float32), (3000 * 1501, 16, 3000, torch.bfloat16),
-    (66_000 * 41, 8, 66_000, torch.float32), (1100 * 1100, 520, 1100, torch.bfloat16)])
+    (66_000 * 41, 8, 66_000, torch.float32), (1100 * 1100, 520, 1100, torch.bfloat16),
+    (33_000 * 4100, 1, 33_000, torch.bfloat16)])
 def test_many_rows(rows, width, groups, dtype):
     say("long sums: %dx%d, %d groups" % (rows, width, groups))
     gen = torch.Generator(device="cuda").manual_seed(8)
@@ -71,5 +72,5 @@ def test_many_rows(rows, width, groups, dtype):
     near(w, lambda c: dr[:, c].double() * h[:, c].double())
     near(b, lambda c: dr[:, c].double())
     if groups:
-        near(dgate, lambda c: (dr[:, c].double() * h[:, c].double()).view(groups, -1, 8),
+        near(dgate, lambda c: (dr[:, c].double() * h[:, c].double()).view(groups, rows // groups, -1),
              2.0 ** -8 if dtype is torch.bfloat16 else 0.0)
