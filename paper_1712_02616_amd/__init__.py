@@ -20,7 +20,6 @@ stream for the tensor's device).
 
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import importlib.util
 import math
@@ -230,8 +229,12 @@ def _enqueue(name, device, stream, *args):
     """Entry point ``name`` with ``args`` and the stream.  The tensors' device is
     current meanwhile: a default stream has no device of its own, and a launch
     goes to the current one."""
-    with torch.cuda.device(device):
-        rc = getattr(load(), name)(*args, _stream(device, stream))
+    call = getattr(_lib or load(), name)
+    if torch.cuda.current_device() == device.index:
+        rc = call(*args, _stream(device, stream))
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args, _stream(device, stream))
     _check(name, rc)
 
 
@@ -245,9 +248,11 @@ def _take(need, device, workspace, stream):
         if stream is not None and not isinstance(stream, torch.cuda.Stream):
             stream = torch.cuda.ExternalStream(int(stream), device=device)
         # (A change of the current stream costs more than all else here.)
-        same = stream is None or stream.cuda_stream == torch.cuda.current_stream(device).cuda_stream
-        with contextlib.nullcontext() if same else torch.cuda.stream(stream):
+        if stream is None or stream.cuda_stream == torch.cuda.current_stream(device).cuda_stream:
             workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
+        else:
+            with torch.cuda.stream(stream):
+                workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
     if workspace.device != device or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on %s" % device)
     return workspace, ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size()

@@ -75,6 +75,7 @@ def seen(monkeypatch):
     monkeypatch.setattr(torch.cuda, "Stream", Stream)
     monkeypatch.setattr(torch.cuda, "stream", seen.on_stream)
     monkeypatch.setattr(torch.cuda, "device", seen.on_device)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: Stream(handle))
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream(7))
     monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, stream: None)
@@ -174,3 +175,12 @@ def test_the_current_stream_is_not_changed_for_itself(seen, call, stream, monkey
     monkeypatch.setattr(torch.cuda, "stream", None)
     CALLS[call](stream=stream)
     assert len(seen.allocated) == 1 and seen.called[0][2] == 7
+
+
+def test_a_device_that_is_current_is_not_set(seen, monkeypatch):
+    monkeypatch.setattr(torch.cuda, "device", None)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: DEVICE.index)
+    for name, call in ALL.items():
+        seen.called.clear()
+        call(stream=99)
+        assert seen.called == [("iabn_" + name, None, 99)]
