@@ -12,8 +12,8 @@
  * and the two blocks the paper compares against (the standard block and the
  * proposed checkpointing, Sec. 3.2), on the same kernels.  At the end: the
  * operators of a transformer's feed-forward sublayer (norms around a block,
- * dropout, a gated feed-forward block), which recompute where they can instead
- * of storing, as the method does.
+ * dropout, a gated feed-forward block, routed experts), which recompute where
+ * they can instead of storing, as the method does, and the clipping of gradients.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -477,6 +477,145 @@ int iabn_ffn_backward(const void *dy, const void *x, const void *g, const void *
                       void *du, void *dw_gate, void *dw_up, void *dw_down, int dtype, int act,
                       float slope, int64_t M, int64_t C, int64_t F, void *workspace,
                       size_t workspace_bytes, void *stream);
+
+/*
+ * A feed-forward sublayer of routed experts
+ * -----------------------------------------
+ * A router gives every token k of E experts, each a gated feed-forward block of
+ * its own, whose outputs are added up with the router's weights.  E <= 1024,
+ * k <= 64, M <= 2^25 tokens, M*k <= 2^30 pairs (token, slot); the pair (t, s) has
+ * the number t*k + s.
+ */
+
+/* What makes a score of a logit: softmax over the experts, or the logistic
+ * function of each. */
+typedef enum { IABN_SCORE_SOFTMAX = 0, IABN_SCORE_SIGMOID = 1 } iabn_score_t;
+
+/*
+ * Routing: s = score(logits), c = s + bias; the k experts of the highest c, in that
+ * order, and w_j = scale*s_j, or scale*s_j/(sum of the chosen s) (renormalise).
+ *   logits         [M, E] of the storage type.
+ *   bias           [E] fp32, or NULL: added for the choice alone.
+ *   experts        [M, k] int32 out.     weights  [M, k] fp32 out.
+ *   groups, groups_kept, group_top
+ *                  the experts are `groups` (at most 64, dividing E) groups of
+ *                  consecutive ones, and only the groups_kept of them with the
+ *                  highest sums of their group_top (1 or 2) highest c are chosen
+ *                  from; groups_kept = groups leaves them all.
+ *   scale          finite.               k  at most E.
+ * Of equal ones the lower index comes first.  Without a bias the order of c is
+ * that of the logits; otherwise, and for the groups, scores are formed and compared
+ * in 64 bits.  A logit or a bias of -inf switches an expert off: it is not chosen,
+ * whatever is left, and a slot for which nothing is left has the expert -1 and the
+ * weight 0.  A NaN is above every number, so that it shows in the weights.
+ * Renormalised weights do not depend on the size of the scores (a row whose
+ * sigmoids all underflow has the weights of its formula).
+ *
+ * iabn_route_backward: the logits' gradient from the weights', for the experts
+ * that the forward chose (-1, and any number that is no expert's, adds nothing).
+ * The choice itself, and with it the bias, has no gradient.
+ *   dlogits        [M, E] out, storage type; may be logits.
+ */
+int iabn_route_forward(const void *logits, int dtype, const float *bias, int32_t *experts,
+                       float *weights, int score, int64_t groups, int64_t groups_kept,
+                       int group_top, int renormalise, float scale, int64_t M, int64_t E,
+                       int64_t k, void *stream);
+
+int iabn_route_backward(const float *dweights, const void *logits, const int32_t *experts,
+                        void *dlogits, int dtype, int score, int renormalise, float scale,
+                        int64_t M, int64_t E, int64_t k, void *stream);
+
+/*
+ * The plan of the experts' products: the pairs sorted by expert, those of one
+ * expert by number.
+ *   experts        [M, k]: any choice; a pair whose number is not in [0, E) is left
+ *                  out (a slot without an expert, a token that is padding).  A token
+ *                  may have an expert twice.
+ *   plan           out, iabn_experts_plan_size(M, k, E) int32: offsets [E + 1] (the
+ *                  sorted rows of expert e are offsets[e] to offsets[e + 1]), then
+ *                  order [M*k] (the pair of each sorted row; not written past the
+ *                  last), then place [M*k] (the sorted row of each pair, -1 where
+ *                  it is left out), then what the kernels need.
+ * The size is 0 for invalid arguments.
+ */
+int64_t iabn_experts_plan_size(int64_t M, int64_t k, int64_t E);
+
+int iabn_experts_plan(const int32_t *experts, int32_t *plan, int64_t M, int64_t k, int64_t E,
+                      void *stream);
+
+/*
+ * The experts' gated feed-forward blocks: for each pair i = (t, s) of expert e
+ *
+ *   g_i = x_t Wg_e^T,  u_i = x_t Wu_e^T,  h_i = act(g_i)*u_i,
+ *   y_t = sum over s of w_ts * (h_i Wd_e^T)
+ *
+ *   x, y           [M, C]; y is out and must not overlap the inputs.
+ *   plan           of iabn_experts_plan, for the same M, k and E.
+ *   weights        [M, k] fp32.
+ *   w_gate, w_up   [E, F, C].    w_down  [E, C, F].
+ *   g, u           [M*k, F] out: the projections, a row for each sorted row of the
+ *                  plan (rows past its last are not written), which the backward
+ *                  takes, or both NULL (inference).
+ *   act, slope     as in iabn_ffn_forward.
+ *   C, F           at most 2^17; no tensor of more than 2^35 elements.  Where C or F
+ *                  or k is 0, y (and g, u) are 0.
+ * Products are summed in fp32 (matrix cores).  h and, for more than 64 tokens, each
+ * pair's weighted term of y are rounded to the storage type between the kernels.
+ * A token without experts has y = 0.  The workspace holds
+ * iabn_experts_workspace_size(M, k, E, C, F, dtype) bytes, 16-byte aligned: enough
+ * for either direction.
+ *
+ * iabn_experts_backward: its gradients from dy, and the g, u that the forward kept.
+ *   dx             [M, C] out.   dweights  [M, k] fp32 out; 0 for a pair left out.
+ *   dg, du         [M*k, F] out: the gradients of the projections, in the plan's
+ *                  order.  dg may be g and du may be u.
+ *   dw_gate, dw_up [E, F, C], dw_down [E, C, F] out; an expert without tokens gets 0.
+ * All outputs are overwritten (dg and du up to the plan's last row).
+ */
+size_t iabn_experts_workspace_size(int64_t M, int64_t k, int64_t E, int64_t C, int64_t F, int dtype);
+
+int iabn_experts_forward(const void *x, const int32_t *plan, const float *weights,
+                         const void *w_gate, const void *w_up, const void *w_down, void *y,
+                         void *g, void *u, int dtype, int act, float slope, int64_t M, int64_t k,
+                         int64_t E, int64_t C, int64_t F, void *workspace, size_t workspace_bytes,
+                         void *stream);
+
+int iabn_experts_backward(const void *dy, const void *x, const int32_t *plan, const float *weights,
+                          const void *g, const void *u, const void *w_gate, const void *w_up,
+                          const void *w_down, void *dx, float *dweights, void *dg, void *du,
+                          void *dw_gate, void *dw_up, void *dw_down, int dtype, int act, float slope,
+                          int64_t M, int64_t k, int64_t E, int64_t C, int64_t F, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+/*
+ * Clipping a training step's gradients to a global norm
+ * -----------------------------------------------------
+ * A list of `count` (at most 2^20) tensors: host arrays of their device pointers,
+ * storage types and numbers of elements (any, 0 too; at most 2^42 in all), which are
+ * read before the call returns.
+ *
+ * iabn_grad_norm: norm[0] = sqrt(sum over all tensors of g^2), fp32 on the device.
+ * Squares and sums are 64-bit, in a fixed order: no square overflows.  No tensors: 0.
+ * An infinity gives inf, a NaN NaN.  Ranks of one training step that hold different
+ * tensors add up norm^2 between the two calls.  The workspace holds
+ * iabn_grad_norm_workspace_size(sizes, count) bytes (0 for an invalid list), 16-byte
+ * aligned.
+ *
+ * iabn_grad_clip: out = g*min(1, max_norm/(norm[0] + 1e-6)).
+ *   outs           of the gradients' types and sizes; outs[i] may be grads[i], which
+ *                  is then not touched where nothing is clipped.
+ *   max_norm       >= 0 (inf: no clipping).  A norm that is NaN makes every output
+ *                  NaN.
+ */
+size_t iabn_grad_norm_workspace_size(const int64_t *sizes, int64_t count);
+
+int iabn_grad_norm(const void *const *grads, const int *dtypes, const int64_t *sizes,
+                   int64_t count, float *norm, void *workspace, size_t workspace_bytes,
+                   void *stream);
+
+int iabn_grad_clip(const void *const *grads, void *const *outs, const int *dtypes,
+                   const int64_t *sizes, int64_t count, const float *norm, float max_norm,
+                   void *stream);
 
 #ifdef __cplusplus
 }

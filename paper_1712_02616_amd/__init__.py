@@ -66,7 +66,10 @@ _NATIVE = ("iabn_workspace_size", "iabn_forward_train", "iabn_forward_train_noal
            "iabn_std_backward", "iabn_ckpt_forward_train", "iabn_ckpt_recompute",
            "iabn_ckpt_backward", "iabn_dropout", "iabn_resnorm_forward",
            "iabn_resnorm_workspace_size", "iabn_resnorm_backward", "iabn_ffn_workspace_size",
-           "iabn_ffn_forward", "iabn_ffn_backward")
+           "iabn_ffn_forward", "iabn_ffn_backward", "iabn_route_forward", "iabn_route_backward",
+           "iabn_experts_plan", "iabn_experts_workspace_size", "iabn_experts_forward",
+           "iabn_experts_backward", "iabn_grad_norm_workspace_size", "iabn_grad_norm", "iabn_grad_clip",
+           "iabn_experts_plan_size")
 (_WORKSPACE_SIZE, _FORWARD_TRAIN, _FORWARD_TRAIN_NOALLOC, _FORWARD_EVAL, _BACKWARD, _BACKWARD_II,
  _STD_FORWARD, _STD_BACKWARD, _CKPT_FORWARD, _CKPT_RECOMPUTE, _CKPT_BACKWARD) = range(11)
 
@@ -129,6 +132,16 @@ def declare(lib):
         "iabn_ffn_workspace_size": ([i64, i64, i64, i32], sz),
         "iabn_ffn_forward": ([vp] * 7 + [i32, i32, f32, i64, i64, i64, vp, sz, vp], i32),
         "iabn_ffn_backward": ([vp] * 13 + [i32, i32, f32, i64, i64, i64, vp, sz, vp], i32),
+        "iabn_route_forward": ([vp, i32, vp, vp, vp, i32, i64, i64, i32, i32, f32, i64, i64, i64, vp], i32),
+        "iabn_route_backward": ([vp, vp, vp, vp, i32, i32, i32, f32, i64, i64, i64, vp], i32),
+        "iabn_experts_plan_size": ([i64, i64, i64], i64),
+        "iabn_experts_plan": ([vp, vp, i64, i64, i64, vp], i32),
+        "iabn_experts_workspace_size": ([i64] * 5 + [i32], sz),
+        "iabn_experts_forward": ([vp] * 9 + [i32, i32, f32] + [i64] * 5 + [vp, sz, vp], i32),
+        "iabn_experts_backward": ([vp] * 16 + [i32, i32, f32] + [i64] * 5 + [vp, sz, vp], i32),
+        "iabn_grad_norm_workspace_size": ([vp, i64], sz),
+        "iabn_grad_norm": ([vp, vp, vp, i64, vp, vp, sz, vp], i32),
+        "iabn_grad_clip": ([vp, vp, vp, vp, i64, vp, f32, vp], i32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -527,3 +540,7 @@ from . import sublayer as _sublayer  # noqa: E402
 from .sublayer import (ACTIVATIONS, NORMS, iabn_dropout, iabn_ffn_backward,  # noqa: E402
                        iabn_ffn_forward, iabn_ffn_workspace_size, iabn_resnorm_backward,
                        iabn_resnorm_forward, iabn_resnorm_workspace_size)
+from .routed import (SCORES, iabn_experts_backward, iabn_experts_forward,  # noqa: E402
+                     iabn_experts_plan, iabn_experts_plan_size, iabn_experts_workspace_size,
+                     iabn_grad_clip, iabn_grad_norm, iabn_grad_norm_workspace_size,
+                     iabn_route_backward, iabn_route_forward)

@@ -16,6 +16,8 @@
 #include <cxxabi.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <vector>
+
 #include "iabn.h"
 
 namespace {
@@ -42,7 +44,17 @@ enum Op : long {
     kResnormBackward,
     kFfnWorkspaceSize,
     kFfnForward,
-    kFfnBackward
+    kFfnBackward,
+    kRouteForward,
+    kRouteBackward,
+    kExpertsPlan,
+    kExpertsWorkspaceSize,
+    kExpertsForward,
+    kExpertsBackward,
+    kGradNormWorkspaceSize,
+    kGradNorm,
+    kGradClip,
+    kExpertsPlanSize
 };
 
 // What follows the table and the op in a call: activation tensors,
@@ -487,6 +499,245 @@ PyObject* ffn_backward_checked(void* const* table, Args& a) {
     });
 }
 
+// ---------------------------------------------------------------- routed experts
+
+// A contiguous tensor of [rows, k] and `type`: choices or their weights.  k < 0: the
+// tensor says it.
+void* choices(Args& a, at::ScalarType type, int64_t& k) {
+    const at::Tensor* const t = a.tensor(false);
+    if (t == nullptr) return nullptr;
+    const int64_t d = t->dim();
+    if (d < 1 || t->scalar_type() != type || t->device() != a.dev || (k >= 0 && t->size(d - 1) != k) ||
+        t->numel() != a.R * t->size(d - 1))
+        return a.plain = false, nullptr;
+    k = t->size(d - 1);
+    return t->data_ptr();
+}
+
+PyObject* route_forward_checked(void* const* table, Args& a) {
+    void* const logits = a.rows();
+    int64_t k = -1;
+    int32_t* const experts = static_cast<int32_t*>(choices(a, at::kInt, k));
+    float* const weights = static_cast<float*>(choices(a, at::kFloat, k));
+    float* const bias = a.floats(a.C);
+    const int score = a.choice(), groups = a.choice(), kept = a.choice(), top = a.choice(), norm = a.choice();
+    const float scale = a.number();
+    if (!a.ready()) return not_plain();
+    return without_gil([&] {
+        return entry<decltype(iabn_route_forward)>(table, kRouteForward)(
+            logits, a.code, bias, experts, weights, score, groups, kept, top, norm, scale, a.R, a.C, k, a.stream());
+    });
+}
+
+PyObject* route_backward_checked(void* const* table, Args& a) {
+    // The rows are the logits', which come second.
+    PyObject* const* const at_dweights = a.at;
+    ++a.at;
+    void* const logits = a.rows();
+    int64_t k = -1;
+    int32_t* const experts = static_cast<int32_t*>(choices(a, at::kInt, k));
+    void* const dlogits = a.rows();
+    PyObject* const* const after = a.at;
+    a.at = at_dweights;
+    float* const dweights = static_cast<float*>(choices(a, at::kFloat, k));
+    a.at = after;
+    const int score = a.choice(), norm = a.choice();
+    const float scale = a.number();
+    if (!a.ready()) return not_plain();
+    return without_gil([&] {
+        return entry<decltype(iabn_route_backward)>(table, kRouteBackward)(
+            dweights, logits, experts, dlogits, a.code, score, norm, scale, a.R, a.C, k, a.stream());
+    });
+}
+
+// A plan for M tokens with k of E experts each.
+int32_t* plan_of(void* const* table, Args& a, int64_t M, int64_t k, int64_t E) {
+    const at::Tensor* const t = a.tensor(false);
+    if (t == nullptr) return nullptr;
+    const int64_t need = entry<decltype(iabn_experts_plan_size)>(table, kExpertsPlanSize)(M, k, E);
+    if (t->scalar_type() != at::kInt || t->device() != a.dev || need == 0 || t->numel() < need)
+        return a.plain = false, nullptr;
+    return static_cast<int32_t*>(t->data_ptr());
+}
+
+PyObject* experts_plan_checked(void* const* table, Args& a) {
+    const at::Tensor* const t = a.tensor(false);
+    if (t == nullptr || t->dim() < 1 || t->scalar_type() != at::kInt) return not_plain();
+    a.dev = t->device();
+    const int64_t k = t->size(t->dim() - 1);
+    int64_t M = 1;
+    for (int64_t i = 0; i + 1 < t->dim(); ++i) M *= t->size(i);
+    PyObject* const* const at_plan = a.at;
+    ++a.at;
+    PyObject* const o = *a.at;
+    const long long E = PyLong_CheckExact(o) ? PyLong_AsLongLong(o) : -1;
+    if (E < 0 || PyErr_Occurred()) return not_plain();
+    a.at = at_plan;
+    int32_t* const plan = plan_of(table, a, M, k, E);
+    if (!a.ready()) return not_plain();
+    const int32_t* const experts = static_cast<const int32_t*>(t->data_ptr());
+    return without_gil([&] {
+        return entry<decltype(iabn_experts_plan)>(table, kExpertsPlan)(experts, plan, M, k, E, a.stream());
+    });
+}
+
+// The experts' weights, [E, F, C] and (down) [E, C, F]; the first one says E and F.
+struct Experts {
+    int64_t E = -1, F = 0;
+    void* weight(Args& a, bool down) {
+        const at::Tensor* const t = a.tensor(false);
+        if (t == nullptr) return nullptr;
+        if (t->dim() != 3 || dtype_code(t->scalar_type()) != a.code || t->device() != a.dev)
+            return a.plain = false, nullptr;
+        if (E < 0) E = t->size(0), F = t->size(1);
+        if (t->size(0) != E || t->size(1) != (down ? a.C : F) || t->size(2) != (down ? F : a.C))
+            return a.plain = false, nullptr;
+        return t->data_ptr();
+    }
+};
+
+PyObject* experts_forward_checked(void* const* table, Args& a) {
+    void* const x = a.rows();
+    PyObject* const* const at_plan = a.at;
+    ++a.at;
+    int64_t k = -1;
+    float* const weights = static_cast<float*>(choices(a, at::kFloat, k));
+    Experts e;
+    void* const wg = e.weight(a, false);
+    void* const wu = e.weight(a, false);
+    void* const wd = e.weight(a, true);
+    void* const y = a.rows();
+    void* const g = a.matrix(a.R * k * e.F, e.F, true);
+    void* const u = a.matrix(a.R * k * e.F, e.F, true);
+    const int act = a.choice();
+    const float slope = a.number();
+    bool own;
+    at::Tensor ws = a.workspace(own);
+    if (!a.plain) return not_plain();
+    a.at = at_plan;
+    int32_t* const plan = plan_of(table, a, a.R, k, e.E);
+    if (!a.ready()) return not_plain();
+    return without_gil([&] {
+        a.take(ws, own, entry<decltype(iabn_experts_workspace_size)>(table, kExpertsWorkspaceSize)(
+                            a.R, k, e.E, a.C, e.F, a.code));
+        return entry<decltype(iabn_experts_forward)>(table, kExpertsForward)(
+            x, plan, weights, wg, wu, wd, y, g, u, a.code, act, slope, a.R, k, e.E, a.C, e.F, ws.data_ptr(),
+            bytes_of(ws), a.stream());
+    });
+}
+
+PyObject* experts_backward_checked(void* const* table, Args& a) {
+    void* const dy = a.rows();
+    void* const x = a.rows();
+    PyObject* const* const at_plan = a.at;
+    ++a.at;
+    int64_t k = -1;
+    float* const weights = static_cast<float*>(choices(a, at::kFloat, k));
+    PyObject* const* const at_g = a.at;
+    a.at += 2;
+    Experts e;
+    void* const wg = e.weight(a, false);
+    void* const wu = e.weight(a, false);
+    void* const wd = e.weight(a, true);
+    void* const dx = a.rows();
+    float* const dweights = static_cast<float*>(choices(a, at::kFloat, k));
+    void* const dg = a.matrix(a.R * k * e.F, e.F);
+    void* const du = a.matrix(a.R * k * e.F, e.F);
+    void* const dwg = e.weight(a, false);
+    void* const dwu = e.weight(a, false);
+    void* const dwd = e.weight(a, true);
+    const int act = a.choice();
+    const float slope = a.number();
+    bool own;
+    at::Tensor ws = a.workspace(own);
+    if (!a.plain) return not_plain();
+    a.at = at_g;
+    void* const g = a.matrix(a.R * k * e.F, e.F);
+    void* const u = a.matrix(a.R * k * e.F, e.F);
+    a.at = at_plan;
+    int32_t* const plan = plan_of(table, a, a.R, k, e.E);
+    if (!a.ready()) return not_plain();
+    return without_gil([&] {
+        a.take(ws, own, entry<decltype(iabn_experts_workspace_size)>(table, kExpertsWorkspaceSize)(
+                            a.R, k, e.E, a.C, e.F, a.code));
+        return entry<decltype(iabn_experts_backward)>(table, kExpertsBackward)(
+            dy, x, plan, weights, g, u, wg, wu, wd, dx, dweights, dg, du, dwg, dwu, dwd, a.code, act, slope,
+            a.R, k, e.E, a.C, e.F, ws.data_ptr(), bytes_of(ws), a.stream());
+    });
+}
+
+// ---------------------------------------------------------------- lists of gradients
+
+struct GradList {
+    std::vector<const void*> at;
+    std::vector<int> dtypes;
+    std::vector<int64_t> sizes;
+};
+
+// The tensors of a Python list or tuple, all on a.dev (the norm's device).
+bool grad_list(Args& a, GradList& list) {
+    PyObject* const o = *a.at++;
+    if (!PyList_CheckExact(o) && !PyTuple_CheckExact(o)) return false;
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+    list.at.reserve(n), list.dtypes.reserve(n), list.sizes.reserve(n);
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        PyObject* const item = PySequence_Fast_GET_ITEM(o, i);
+        if (!THPVariable_CheckExact(item)) return false;
+        const at::Tensor& t = THPVariable_Unpack(item);
+        const int code = dtype_code(t.scalar_type());
+        if (code < 0 || !t.is_cuda() || !t.is_contiguous() || t.device() != a.dev) return false;
+        list.at.push_back(t.data_ptr());
+        list.dtypes.push_back(code);
+        list.sizes.push_back(t.numel());
+    }
+    return true;
+}
+
+float* norm_value(Args& a) {
+    const at::Tensor* const t = a.tensor(false);
+    if (t == nullptr) return nullptr;
+    if (t->scalar_type() != at::kFloat || t->numel() != 1) return a.plain = false, nullptr;
+    a.dev = t->device();
+    return static_cast<float*>(t->data_ptr());
+}
+
+PyObject* grad_norm_checked(void* const* table, Args& a) {
+    PyObject* const* const at_grads = a.at;
+    ++a.at;
+    float* const norm = norm_value(a);
+    bool own;
+    at::Tensor ws = a.workspace(own);
+    if (!a.ready()) return not_plain();
+    a.at = at_grads;
+    GradList grads;
+    if (!grad_list(a, grads)) return not_plain();
+    return without_gil([&] {
+        const int64_t n = static_cast<int64_t>(grads.at.size());
+        a.take(ws, own, entry<decltype(iabn_grad_norm_workspace_size)>(table, kGradNormWorkspaceSize)(
+                            grads.sizes.data(), n));
+        return entry<decltype(iabn_grad_norm)>(table, kGradNorm)(
+            grads.at.data(), grads.dtypes.data(), grads.sizes.data(), n, norm, ws.data_ptr(), bytes_of(ws),
+            a.stream());
+    });
+}
+
+PyObject* grad_clip_checked(void* const* table, Args& a) {
+    PyObject* const* const at_grads = a.at;
+    a.at += 2;
+    const float* const norm = norm_value(a);
+    const float max_norm = a.number();
+    if (!a.ready()) return not_plain();
+    a.at = at_grads;
+    GradList grads, outs;
+    if (!grad_list(a, grads) || !grad_list(a, outs) || grads.dtypes != outs.dtypes || grads.sizes != outs.sizes)
+        return not_plain();
+    return without_gil([&] {
+        return entry<decltype(iabn_grad_clip)>(table, kGradClip)(
+            grads.at.data(), const_cast<void* const*>(outs.at.data()), grads.dtypes.data(), grads.sizes.data(),
+            static_cast<int64_t>(grads.at.size()), norm, max_norm, a.stream());
+    });
+}
+
 // fn(table, arguments...) -> status or NotImplemented, as `call`.
 template <PyObject* (*FN)(void* const*, Args&), Py_ssize_t N>
 PyObject* sublayer(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -516,6 +767,13 @@ PyMethodDef methods[] = {
      "iabn_resnorm_backward, as call"},
     {"ffn_forward", method<ffn_forward_checked, 10>(), METH_FASTCALL, "iabn_ffn_forward, as call"},
     {"ffn_backward", method<ffn_backward_checked, 16>(), METH_FASTCALL, "iabn_ffn_backward, as call"},
+    {"route_forward", method<route_forward_checked, 10>(), METH_FASTCALL, "iabn_route_forward, as call"},
+    {"route_backward", method<route_backward_checked, 7>(), METH_FASTCALL, "iabn_route_backward, as call"},
+    {"experts_plan", method<experts_plan_checked, 3>(), METH_FASTCALL, "iabn_experts_plan, as call"},
+    {"experts_forward", method<experts_forward_checked, 12>(), METH_FASTCALL, "iabn_experts_forward, as call"},
+    {"experts_backward", method<experts_backward_checked, 19>(), METH_FASTCALL, "iabn_experts_backward, as call"},
+    {"grad_norm", method<grad_norm_checked, 3>(), METH_FASTCALL, "iabn_grad_norm, as call"},
+    {"grad_clip", method<grad_clip_checked, 4>(), METH_FASTCALL, "iabn_grad_clip, as call"},
     {"call", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(call)), METH_FASTCALL,
      "call(table, op, tensors..., floats...[, workspace]) -> status or NotImplemented"},
     {nullptr, nullptr, 0, nullptr}};

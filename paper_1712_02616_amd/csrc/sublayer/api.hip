@@ -4,7 +4,7 @@
 
 #include <cmath>
 
-#include "errors.h"
+#include "checks.h"
 #include "ffn.h"
 
 namespace iabn_impl {
@@ -13,8 +13,6 @@ namespace {
 constexpr int64_t kMaxWidth = (int64_t(1) << 31) - 1;
 constexpr int64_t kMaxNormWidth = int64_t(kMaxRowWaves) * kWave * 2 * kChunk;
 constexpr int64_t kMaxElems = int64_t(1) << 46;
-
-bool valid_dtype(int dtype) { return dtype == IABN_F32 || dtype == IABN_F16 || dtype == IABN_BF16; }
 
 int check_rows(int dtype, int64_t R, int64_t C, int64_t max_width) {
     if (!valid_dtype(dtype)) return fail(IABN_ERR_DTYPE, "unknown dtype %d", dtype);
@@ -66,8 +64,6 @@ constexpr int64_t kBwdMinRows = 4;
 constexpr int64_t kChain = 1024;
 constexpr int64_t kMaxBwdBlocks = int64_t(1) << 20;
 
-int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 ResnormSplit split_rows(int64_t R, int64_t C, int64_t groups, int64_t waves_on_cu) {
     if (R == 0) return {1, 0, 0, 0, 0};
     const RowShape shape = row_shape(chunks_of(C), kBwdOneWave);
@@ -113,8 +109,6 @@ constexpr int64_t kMaxFfnRows = int64_t(1) << 26;
 // Elements of any of its matrices (so that its tiles fit a launch).
 constexpr int64_t kMaxFfnElems = int64_t(1) << 37;
 
-int elem_bytes(int dtype) { return dtype == IABN_F32 ? 4 : 2; }
-
 int check_ffn(int dtype, int act, float slope, int64_t M, int64_t C, int64_t F) {
     if (!valid_dtype(dtype)) return fail(IABN_ERR_DTYPE, "unknown dtype %d", dtype);
     if (M < 0 || C < 0 || F < 0)
@@ -144,16 +138,6 @@ size_t ffn_workspace(int64_t M, int64_t C, int64_t F, int dtype) {
                      part_bytes(dtype, kGemmDw, C, F, M, 1), part_bytes(dtype, kGemmDw, F, C, M, 2)})
         part = part < p ? p : part;
     return h_bytes(M, F, dtype) + part;
-}
-
-int check_workspace(void* workspace, size_t bytes, size_t need) {
-    if (need == 0) return IABN_OK;
-    if (!workspace) return fail(IABN_ERR_NULL, "workspace is NULL");
-    if (bytes < need)
-        return fail(IABN_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", bytes, need);
-    if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0)
-        return fail(IABN_ERR_WORKSPACE, "workspace is not 16-byte aligned");
-    return IABN_OK;
 }
 
 // A product of the block, whose split sums go behind h in the workspace.

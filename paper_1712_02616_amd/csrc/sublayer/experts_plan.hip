@@ -1,0 +1,165 @@
+// The plan of the experts' products: the M*k pairs (token, slot) sorted by expert,
+// pairs of one expert in their own order (a counting sort, the same result
+// whatever the order in which blocks run).
+//
+// Each wave has a contiguous part of the pairs.  It counts its experts in LDS;
+// the counts of the waves, and of the blocks before this one, say where its
+// pairs of an expert begin; then it goes through them again, 64 at a time, and a
+// pair's place among those is the number of lanes before it with the same expert
+// (found bit by bit of the expert's number).  Up to kPlanPairs pairs are one
+// block and one launch; more are counted by a launch of their own, and every block
+// adds up the counts before its own (blocks*E integers from the caches).
+#include "routed.h"
+
+namespace iabn_impl {
+namespace {
+
+constexpr int kPlanThreads = 256, kPlanWaves = kPlanThreads / kWave;
+constexpr int kPlanPairs = 2048;    // of a block, while there are fewer blocks than
+constexpr int kMaxPlanBlocks = 256;
+
+// Whether it is an expert at all (any other number: the pair is left out).
+__device__ __forceinline__ bool routed(int e, int E) { return e >= 0 && e < E; }
+
+// [P) of block b, wave w.
+__device__ __forceinline__ void span_of(const PlanArgs& a, int wave, int& from, int& to) {
+    const int64_t begin = int64_t(blockIdx.x) * a.span, end = min(begin + a.span, int64_t(a.P));
+    const int64_t per = a.span / kPlanWaves;
+    from = static_cast<int>(min(begin + wave * per, end));
+    to = static_cast<int>(min(begin + (wave + 1) * per, end));
+}
+
+__global__ __launch_bounds__(kPlanThreads) void plan_count_kernel(PlanArgs a) {
+    extern __shared__ int32_t counts[];  // [E]
+    for (int e = threadIdx.x; e < a.E; e += kPlanThreads) counts[e] = 0;
+    __syncthreads();
+    int from, to;
+    span_of(a, threadIdx.x / kWave, from, to);
+    for (int i = from + static_cast<int>(lane_id()); i < to; i += kWave) {
+        const int e = a.experts[i];
+        if (routed(e, a.E)) atomicAdd(&counts[e], 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.E; e += kPlanThreads)
+        a.counts[int64_t(blockIdx.x) * a.E + e] = counts[e];
+}
+
+// The sum over the lanes before this one; in `total` that over all.
+__device__ __forceinline__ int wave_before(int v, int& total) {
+    int sum = v;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const int o = __shfl_up(sum, d);
+        if (static_cast<int>(lane_id()) >= d) sum += o;
+    }
+    total = __shfl(sum, kWave - 1);
+    return sum - v;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
+    extern __shared__ int32_t next[];  // [waves][E]: where the wave's next pair of e goes
+    __shared__ int32_t wave_total[kPlanWaves];
+    const int wave = threadIdx.x / kWave;
+    int32_t* const own = next + wave * a.E;
+    for (int i = threadIdx.x; i < kPlanWaves * a.E; i += kPlanThreads) next[i] = 0;
+    __syncthreads();
+    int from, to;
+    span_of(a, wave, from, to);
+    for (int i = from + static_cast<int>(lane_id()); i < to; i += kWave) {
+        const int e = a.experts[i];
+        if (routed(e, a.E)) atomicAdd(&own[e], 1);
+    }
+    __syncthreads();
+    // Each thread has `each` consecutive experts.
+    constexpr int kEach = kMaxExperts / kPlanThreads;
+    const int each = (a.E + kPlanThreads - 1) / kPlanThreads, e0 = threadIdx.x * each;
+    int all[kEach], before[kEach], sum = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        all[j] = before[j] = 0;
+        const int e = e0 + j;
+        if (j >= each || e >= a.E) continue;
+        if (a.blocks == 1) {
+            for (int w = 0; w < kPlanWaves; ++w) all[j] += next[w * a.E + e];
+        } else {
+            for (int b = 0; b < a.blocks; ++b) {
+                const int n = a.counts[int64_t(b) * a.E + e];
+                before[j] += b < static_cast<int>(blockIdx.x) ? n : 0;
+                all[j] += n;
+            }
+        }
+        sum += all[j];
+    }
+    int total;
+    int at = wave_before(sum, total);
+    if (lane_id() == 0) wave_total[wave] = total;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) at += wave_total[w];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const int e = e0 + j;
+        if (j >= each || e >= a.E) continue;
+        if (blockIdx.x == 0) a.offsets[e] = at;
+        int to_next = at + before[j];
+        for (int w = 0; w < kPlanWaves; ++w) {
+            const int n = next[w * a.E + e];
+            next[w * a.E + e] = to_next;
+            to_next += n;
+        }
+        at += all[j];
+        if (blockIdx.x == 0 && e == a.E - 1) a.offsets[a.E] = at;
+    }
+    __syncthreads();
+    for (int base = from; base < to; base += kWave) {  // (uniform over the wave)
+        const int i = base + static_cast<int>(lane_id());
+        int e = i < to ? a.experts[i] : -1;
+        const bool is = routed(e, a.E);
+        uint64_t same = __ballot(is);
+        for (int bit = 1; bit < a.E; bit *= 2) {
+            const uint64_t have = __ballot((e & bit) != 0);
+            same &= e & bit ? have : ~have;
+        }
+        const uint64_t lower = same & ((uint64_t(1) << lane_id()) - 1);
+        int place = -1;
+        if (is) place = own[e] + __popcll(lower);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (is && lower == 0) own[e] += __popcll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (i < to) a.place[i] = place;
+        if (is) a.order[place] = i;
+    }
+}
+
+int64_t blocks_of(int64_t P) {
+    const int64_t want = (P + kPlanPairs - 1) / kPlanPairs;
+    return want < 1 ? 1 : want < kMaxPlanBlocks ? want : kMaxPlanBlocks;
+}
+
+}  // namespace
+
+int64_t plan_size(int64_t P, int64_t E) {
+    const int64_t blocks = blocks_of(P);
+    return E + 1 + 2 * P + (blocks > 1 ? blocks * E : 0);
+}
+
+PlanArgs plan_of(int64_t P, int64_t E, int32_t* plan) {
+    PlanArgs a = {};
+    a.P = static_cast<int32_t>(P), a.E = static_cast<int32_t>(E);
+    a.offsets = plan;
+    a.order = plan + E + 1;
+    a.place = a.order + P;
+    a.counts = a.place + P;
+    const int64_t blocks = blocks_of(P), per = (P + blocks - 1) / blocks;
+    a.span = static_cast<int32_t>((per + kPlanThreads - 1) / kPlanThreads * kPlanThreads);
+    a.blocks = static_cast<int32_t>(P == 0 ? 1 : (P + a.span - 1) / a.span);
+    return a;
+}
+
+void launch_plan(const PlanArgs& a, hipStream_t st) {
+    if (a.blocks > 1) plan_count_kernel<<<a.blocks, kPlanThreads, a.E * sizeof(int32_t), st>>>(a);
+    plan_kernel<<<a.blocks, kPlanThreads, kPlanWaves * a.E * sizeof(int32_t), st>>>(a);
+}
+
+}  // namespace iabn_impl

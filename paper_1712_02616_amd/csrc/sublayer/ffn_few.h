@@ -13,10 +13,24 @@
 // is two loads (one token: 32 and 16 us, non-temporal 35 and 21).
 #pragma once
 
-#include "ffn.h"
+#include "groups.h"
 #include "mma.h"
 
 namespace iabn_impl {
+
+// The row of x that row m of a block takes (the last one past it).
+template <int KIND>
+__device__ __forceinline__ int64_t few_row(const ArgsOf<KIND>& a, const Tokens& tokens, int64_t group_row, int m) {
+    const int64_t row = min(int64_t(m), a.M - 1);
+    if constexpr (KIND < kOverGroups) return row;
+    else if constexpr (KIND == kOverGroups + kGemmUp) return tokens(row);
+    else return group_row + row;
+}
+template <int KIND>
+__device__ __forceinline__ int64_t all_rows(const ArgsOf<KIND>& a) {
+    if constexpr (KIND >= kOverGroups) return a.P;
+    else return a.M;
+}
 
 // Lines of 128 bytes of every row in a batch; a wave has two batches in flight
 // (four lines spill: one
@@ -24,22 +38,38 @@ namespace iabn_impl {
 constexpr int kFewLines = 2;
 
 template <int DT, int KIND, int MT>
-__global__ __launch_bounds__(512) void few_kernel(GemmArgs a) {
+__global__ __launch_bounds__(512) void few_kernel(ArgsOf<KIND> a) {
     using T = typename Elem<DT>::T;
     constexpr int E = 16 / sizeof(T), kLine = 128 / sizeof(T);
-    constexpr int NW = KIND == kGemmUp ? 2 : 1;  // matrices of weights
+    constexpr bool kGroups = KIND >= kOverGroups, kUp = KIND % kOverGroups == kGemmUp;
+    constexpr int NW = kUp ? 2 : 1;  // matrices of weights
     extern __shared__ __align__(16) char lds[];
 
     const int waves = blockDim.x / kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int i = lane_id() & 15, g = lane_id() >> 4;
-    const int64_t n0 = int64_t(blockIdx.x) * 16;
+    int64_t n0 = int64_t(blockIdx.x) * 16;
+    int64_t group_row = 0;
+    Tokens tokens = {};
+    if constexpr (kGroups) {
+        // A block has 16 columns for up to MT*16 rows of one expert.
+        const uint32_t blocks_n = static_cast<uint32_t>((a.N + 15) / 16);
+        Group group;
+        if (!find_group<MT * 16>(a.offsets, a.E, a.P, blocks_n, 0, group)) return;
+        const int tile = static_cast<int>(group.tile / blocks_n);
+        n0 = (group.tile - tile * blocks_n) * 16;
+        a.M = min(group.rows - tile * MT * 16, MT * 16);
+        group_row = group.first + tile * MT * 16;
+        tokens = {a.order + group_row, static_cast<uint32_t>(a.P), a.top};
+#pragma unroll
+        for (int q = 0; q < NW; ++q) a.y.p[q] = static_cast<const T*>(a.y.p[q]) + group.expert * a.expert_stride;
+    }
     const T *w[NW], *x[MT];
 #pragma unroll
     for (int q = 0; q < NW; ++q)
         w[q] = static_cast<const T*>(a.y.p[q]) + min(n0 + i, a.N - 1) * a.y.ld + g * E;
 #pragma unroll
     for (int t = 0; t < MT; ++t)
-        x[t] = static_cast<const T*>(a.x.p[0]) + min(int64_t(t * 16 + i), a.M - 1) * a.x.ld + g * E;
+        x[t] = static_cast<const T*>(a.x.p[0]) + few_row<KIND>(a, tokens, group_row, t * 16 + i) * a.x.ld + g * E;
 
     f32x4 acc[NW][MT] = {};
     // This block's share of K in lines, and the whole ones of it.
@@ -119,7 +149,7 @@ __global__ __launch_bounds__(512) void few_kernel(GemmArgs a) {
             part[((wave * NW + q) * MT + t) * kWave + lane_id()] = acc[q][t];
     __syncthreads();
     if (wave >= MT) return;
-    const int64_t m = wave * 16 + i, n = n0 + g * 4, left = a.N - n, at = m * a.N + n;
+    const int64_t m = wave * 16 + i, n = n0 + g * 4, left = a.N - n, at = (group_row + m) * a.N + n;
     f32x4 sum[NW] = {};
     for (int v = 0; v < waves; ++v)
 #pragma unroll
@@ -133,7 +163,7 @@ __global__ __launch_bounds__(512) void few_kernel(GemmArgs a) {
     float v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = sum[0][j];
-    if constexpr (KIND == kGemmUp) {
+    if constexpr (kUp) {
         float u[4], h[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) u[j] = sum[NW - 1][j];
@@ -143,8 +173,8 @@ __global__ __launch_bounds__(512) void few_kernel(GemmArgs a) {
             put(a.dg, v);
             put(a.du, u);
         }
-    } else if (gridDim.y > 1) {
-        float* const to = a.part + int64_t(blockIdx.y) * a.M * a.N + at;
+    } else if (kGroups || gridDim.y > 1) {
+        float* const to = a.part + int64_t(blockIdx.y) * all_rows<KIND>(a) * a.N + at;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (j < left) to[j] = v[j];

@@ -23,7 +23,7 @@
 // of that forward: 1.94 and 0.95 ms, 141 and 144 TFLOP/s (the library 153).
 #pragma once
 
-#include "ffn.h"
+#include "groups.h"
 #include "mma.h"
 
 namespace iabn_impl {
@@ -44,7 +44,10 @@ constexpr int kSpan = 64;
 // the row, so that the 16 rows that one read takes fall on all 64 banks.  k
 // strided: a line is one k; 32-byte pairs of chunks (fp32: 64-byte fours) are
 // permuted so that the k that one read takes fall on different banks.
-template <int DT, bool KS, int ROWS, int THREADS, bool DUAL>
+//
+// GATHER: the operand's rows (k strided: its k) are tokens, in the order of a plan
+// (groups.h).
+template <int DT, bool KS, int ROWS, int THREADS, bool DUAL, bool GATHER = false>
 struct Stage {
     using T = typename Elem<DT>::T;
     static constexpr int E = 16 / sizeof(T);
@@ -85,12 +88,18 @@ struct Stage {
     // row0 on.
     u32x4 r[kLoads];
     __device__ __forceinline__ void load(const Operand& o, int seg, int64_t row0, int64_t rows,
-                                         int64_t k0, int64_t K) {
+                                         int64_t k0, int64_t K, const Tokens& tokens = {}) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int line = first_line() + i * kLineStep, c = chunk(i) * E;
             const T* p = static_cast<const T*>(o.p[KS ? seg : matrix_of(line, seg)]);
-            if constexpr (KS)
+            if constexpr (KS && GATHER)
+                r[i] = load16_first<DT>(p + tokens(min(k0 + line, K - 1)) * o.ld + row0 + c,
+                                        k0 + line < K ? rows - c : 0);
+            else if constexpr (GATHER)
+                r[i] = load16_first<DT>(p + tokens(row0 + min(int64_t(row_of(line)), rows - 1)) * o.ld + k0 + c,
+                                        row_of(line) < rows ? K - k0 - c : 0);
+            else if constexpr (KS)
                 r[i] = load16_first<DT>(p + (k0 + line) * o.ld + row0 + c, k0 + line < K ? rows - c : 0);
             else
                 r[i] = load16_first<DT>(p + (row0 + row_of(line)) * o.ld + k0 + c,
@@ -107,29 +116,45 @@ struct Stage {
     // last ones (the results that they go into are not stored).
     uint64_t base[2];      // the tile's first element of each matrix
     uint32_t off[kLoads];  // bytes from the step's first element
-    __device__ __forceinline__ void prepare(const Operand& o, int64_t row0, int64_t rows) {
+    // (k strided, GATHER: the next step's entries of the plan.)
+    uint32_t entry[KS && GATHER ? kLoads : 1];
+    __device__ __forceinline__ void prepare(const Operand& o, int64_t row0, int64_t rows, const Tokens& tokens = {}) {
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
             // (Kept in scalar registers, not loaded from the arguments at each step.)
-            const uint64_t p = reinterpret_cast<uint64_t>(static_cast<const T*>(o.p[q]) + row0 * (KS ? 1 : o.ld));
+            const uint64_t p = reinterpret_cast<uint64_t>(static_cast<const T*>(o.p[q]) +
+                                                          (KS ? row0 : GATHER ? 0 : row0 * o.ld));
             base[q] = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(p))) |
                       uint64_t(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(p >> 32)))) << 32;
         }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int line = first_line() + i * kLineStep, c = chunk(i) * E;
-            if constexpr (KS) {
+            if constexpr (KS && GATHER) {
+                off[i] = static_cast<uint32_t>((c < rows ? c : 0) * sizeof(T));
+            } else if constexpr (KS) {
                 off[i] = static_cast<uint32_t>((line * o.ld + (c < rows ? c : 0)) * sizeof(T));
+            } else if constexpr (GATHER) {
+                const int64_t row = min(static_cast<int64_t>(row_of(line)), rows - 1);
+                off[i] = static_cast<uint32_t>((tokens(row0 + row) * o.ld + c) * sizeof(T));
             } else {
                 const int64_t row = min(static_cast<int64_t>(row_of(line)), rows - 1);
                 off[i] = static_cast<uint32_t>((row * o.ld + c) * sizeof(T));
             }
         }
     }
-    __device__ __forceinline__ void fetch(const Operand& o, int seg, int64_t k0, char* lds) const {
+    // GATHER with k strided: the entries that the step at k0 takes, a step ahead of its fetch.
+    __device__ __forceinline__ void look_up(int64_t k0, int64_t K, const Tokens& tokens) {
+        if constexpr (KS && GATHER)
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                entry[i] = tokens.order[min(k0 + first_line() + i * kLineStep, K - 1)];
+    }
+    __device__ __forceinline__ void fetch(const Operand& o, int seg, int64_t k0, char* lds,
+                                          const Tokens& tokens = {}) const {
 #if defined(__HIP_DEVICE_COMPILE__)  // (the host's pass does not know the buffer types)
         typedef __attribute__((address_space(3))) void lds_t;
-        const uint64_t at = (KS ? k0 * o.ld : k0) * sizeof(T);
+        const uint64_t at = KS && GATHER ? 0 : (KS ? k0 * o.ld : k0) * sizeof(T);
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -138,8 +163,11 @@ struct Stage {
                 DUAL ? __builtin_amdgcn_readfirstlane(matrix_of(first_line() + i * kLineStep, seg)) : seg;
             const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
                 reinterpret_cast<void*>((which ? base[1] : base[0]) + at), 0, 0xffffffff, 0x00027000);
+            uint32_t from = off[i];
+            if constexpr (KS && GATHER)
+                from += tokens.of(entry[i]) * static_cast<uint32_t>(o.ld * static_cast<int64_t>(sizeof(T)));
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                rsrc, (lds_t*)(lds + (wave * kWave + i * THREADS) * 16), 16, off[i], 0, 0, 0);
+                rsrc, (lds_t*)(lds + (wave * kWave + i * THREADS) * 16), 16, from, 0, 0, 0);
         }
 #endif
     }
@@ -180,10 +208,16 @@ struct Stage {
 
 template <int KIND>
 struct KindOf {
-    static constexpr bool kDual = KIND == kGemmUp;
-    static constexpr bool kXStrided = KIND == kGemmDw;
-    static constexpr bool kYStrided = KIND == kGemmDh || KIND == kGemmDx || KIND == kGemmDw;
-    static constexpr int kSegs = KIND == kGemmDx ? 2 : 1;  // products that add up
+    static constexpr bool kGroups = KIND >= kOverGroups;
+    static constexpr GemmKind kBase = static_cast<GemmKind>(
+        !kGroups ? KIND : KIND == kGroupDwTokensY ? static_cast<int>(kGemmDw) : KIND - kOverGroups);
+    static constexpr bool kDual = kBase == kGemmUp;
+    static constexpr bool kXStrided = kBase == kGemmDw;
+    static constexpr bool kYStrided = kBase == kGemmDh || kBase == kGemmDx || kBase == kGemmDw;
+    static constexpr int kSegs = kBase == kGemmDx ? 2 : 1;  // products that add up
+    // The operand whose rows (strided: k) are tokens.
+    static constexpr bool kGatherY = KIND == kGroupDwTokensY;
+    static constexpr bool kGatherX = kGroups && !kGatherY && kBase != kGemmDown && kBase != kGemmDx;
 };
 
 // The tile of a block.  The hardware hands consecutive blocks to the XCDs in
@@ -200,15 +234,18 @@ __device__ __forceinline__ void tile_of(int tiles_m, int tiles_n, int& tm, int& 
     tm = static_cast<int>(strip * kStrip + in % height);
 }
 
+// KIND: a GemmKind, or one of the kinds over groups of rows (groups.h).
 template <int DT, int KIND, int TM, int TN, int WAVES_M, int WAVES_N, bool DMA>
-__global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs a, int tiles_m,
+__global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KIND> a, int tiles_m,
                                                                         int tiles_n) {
     using Kind = KindOf<KIND>;
+    constexpr bool kGroups = Kind::kGroups;
+    constexpr GemmKind kBase = Kind::kBase;
     constexpr int kT = WAVES_M * WAVES_N * kWave;
     constexpr int WM = TM / WAVES_M, WN = TN / WAVES_N, NM = WM / 16, NN = WN / 16;
     static_assert(!Kind::kDual || WN == kSpan, "a wave holds both projections of its columns");
-    using SX = Stage<DT, Kind::kXStrided, TM, kT, false>;
-    using SY = Stage<DT, Kind::kYStrided, TN, kT, Kind::kDual>;
+    using SX = Stage<DT, Kind::kXStrided, TM, kT, false, Kind::kGatherX>;
+    using SY = Stage<DT, Kind::kYStrided, TN, kT, Kind::kDual, Kind::kGatherY>;
     constexpr int BK = SX::BK;
     // Two buffers, of which one is multiplied while the other fills.
     constexpr int kBuffer = SX::kBytes + SY::kBytes;
@@ -216,7 +253,13 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
     char *const lds0 = lds, *const lds1 = lds + kBuffer;
 
     int tm, tn;
-    tile_of(tiles_m, tiles_n, tm, tn);
+    int64_t group_row = 0;  // the rows of the group's outputs begin there
+    Tokens tokens = {};
+    if constexpr (kGroups) {
+        if (!enter_group<DT, KIND, TM>(a, tiles_m, tiles_n, tm, tn, group_row, tokens)) return;
+    } else {
+        tile_of(tiles_m, tiles_n, tm, tn);
+    }
     const int64_t m0 = int64_t(tm) * TM;
     constexpr int kCols = Kind::kDual ? TN / 2 : TN;  // columns of the output
     const int64_t n0 = int64_t(tn) * kCols;
@@ -265,8 +308,10 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
         const auto fetch = [&](int kt, char* buf) __attribute__((always_inline)) {
             const int seg = Kind::kSegs > 1 ? (kt >= whole ? 1 : 0) : z;
             const int64_t k0 = int64_t(Kind::kSegs > 1 && seg ? kt - whole : kt) * BK;
-            sx.fetch(a.x, seg, k0, buf);
-            sy.fetch(a.y, seg, k0, buf + SX::kBytes);
+            sx.fetch(a.x, seg, k0, buf, tokens);
+            sy.fetch(a.y, seg, k0, buf + SX::kBytes, tokens);
+            sx.look_up(k0 + BK, a.K, tokens);
+            sy.look_up(k0 + BK, a.K, tokens);
         };
         // At `meet` what was fetched has arrived (each wave has waited for its
         // own) and the reads of the buffer to be filled next have ended.  The
@@ -315,8 +360,12 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
             turn(kt, b0, b1);
             if (kt + 1 < hi) turn(kt + 1, b1, b0);
         };
-        sx.prepare(a.x, m0, a.M - m0);
-        sy.prepare(a.y, n0, a.N - n0);
+        sx.prepare(a.x, m0, a.M - m0, tokens);
+        sy.prepare(a.y, n0, a.N - n0, tokens);
+        if (kGroups && lo < hi) {
+            sx.look_up(int64_t(lo) * BK, a.K, tokens);
+            sy.look_up(int64_t(lo) * BK, a.K, tokens);
+        }
         if (lo < hi) fetch(lo, lds0);
         if (kAhead && lo < hi) {
             meet();
@@ -330,8 +379,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
         const auto load = [&](int kt) __attribute__((always_inline)) {
             const int seg = Kind::kSegs > 1 ? (kt >= per_seg ? 1 : 0) : z;
             const int64_t k0 = int64_t(whole + (Kind::kSegs > 1 && seg ? kt - per_seg : kt)) * BK;
-            sx.load(a.x, seg, m0, a.M - m0, k0, a.K);
-            sy.load(a.y, seg, n0, a.N - n0, k0, a.K);
+            sx.load(a.x, seg, m0, a.M - m0, k0, a.K, tokens);
+            sy.load(a.y, seg, n0, a.N - n0, k0, a.K, tokens);
         };
         const auto store = [&](char* buf) __attribute__((always_inline)) {
             sx.store(buf);
@@ -372,7 +421,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
     // A lane's c-th chunk of the rows of pass p.
     constexpr int kCh = (Kind::kDual ? WN / 2 : WN) / kChunk;  // chunks of a row
     constexpr int kTurns = kPass * 16 * kCh / kWave;
-    static_assert(kTurns * kWave == kPass * 16 * kCh && (KIND != kGemmDh || kTurns % 2 == 0), "");
+    static_assert(kTurns * kWave == kPass * 16 * kCh && (kBase != kGemmDh || kTurns % 2 == 0), "");
     struct Place {
         int row, col, inside;
         int64_t out;
@@ -383,7 +432,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
         r.row = at_c / kCh, r.col = at_c % kCh * kChunk;
         const int64_t m = m0 + wm + p * 16 + r.row, n = n0 + (Kind::kDual ? wn / 2 : wn) + r.col;
         r.inside = m < a.M ? static_cast<int>(max(min(a.N - n, int64_t(kChunk)), int64_t(0))) : 0;
-        r.out = m * a.N + n;
+        r.out = kGroups ? (group_row + m) * a.N + n : m * a.N + n;
         return r;
     };
     // kGemmDh: g and u of the next chunks are on their way while one is finished.
@@ -396,7 +445,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
 #pragma unroll
     for (int p = 0; p < NM; p += kPass) {
         chunk_t gu[2][2];
-        if constexpr (KIND == kGemmDh) {
+        if constexpr (kBase == kGemmDh) {
             load_gu(p, 0, gu[0]);
             load_gu(p, 1, gu[1]);
         }
@@ -414,7 +463,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] = lo[q], v[q + 4] = hi[q];
         };
-        if constexpr (KIND == kGemmDh) {
+        if constexpr (kBase == kGemmDh) {
 #pragma unroll 1
             for (int c = 0; c < kTurns; c += 2)
 #pragma unroll
@@ -422,12 +471,31 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
                     const auto raw_g = gu[q][0], raw_u = gu[q][1];
                     const Place at_c = place(p, c + q);
                     if (c + q + 2 < kTurns) load_gu(p, c + q + 2, gu[q]);
-                    if (at_c.inside <= 0) continue;
+                    if (!kGroups && at_c.inside <= 0) continue;
                     float v[kChunk], g[kChunk], u[kChunk], dg[kChunk], du[kChunk], h[kChunk];
                     read(at_c.row, at_c.col, v);
                     widen<DT>(raw_g, g);
                     widen<DT>(raw_u, u);
-                    gate_backward<DT>(a.act, a.slope, v, g, u, dg, du, h);
+                    if constexpr (kGroups) {
+                        // The gradients of a pair's weight (the sum over the row of h and
+                        // dy Wd, of which this is 64 columns') and of its projections.
+                        const float w = pair_weight(a, tokens, m0 + wm + p * 16 + at_c.row, a.M);
+                        float dot = 0.0f;
+                        gate_backward<DT>(a.act, a.slope, v, g, u, dg, du, h);
+#pragma unroll
+                        for (int j = 0; j < kChunk; ++j) {
+                            if (j < at_c.inside) dot = fmaf(h[j], v[j], dot);
+                            dg[j] *= w, du[j] *= w, h[j] *= w;
+                        }
+                        dot += dpp_f32<0xB1, 0xF>(dot);
+                        dot += dpp_f32<0x4E, 0xF>(dot);
+                        dot += dpp_f32<0x141, 0xF>(dot);
+                        if (at_c.inside <= 0) continue;
+                        if (at_c.col == 0)
+                            a.dots[(group_row + m0 + wm + p * 16 + at_c.row) * ((a.N + WN - 1) / WN) + (n0 + wn) / WN] = dot;
+                    } else {
+                        gate_backward<DT>(a.act, a.slope, v, g, u, dg, du, h);
+                    }
                     store_chunk<DT, kCached>(a.dg, at_c.out, at_c.inside, dg);
                     store_chunk<DT, kCached>(a.du, at_c.out, at_c.inside, du);
                     store_chunk<DT, kCached>(a.out[0], at_c.out, at_c.inside, h);
@@ -439,7 +507,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
                 if (at_c.inside <= 0) continue;
                 float v[kChunk];
                 read(at_c.row, at_c.col, v);
-                if constexpr (KIND == kGemmUp) {
+                if constexpr (kBase == kGemmUp) {
                     float u[kChunk], h[kChunk];
                     read(at_c.row, at_c.col + WN / 2, u);
                     gate_forward<DT>(a.act, a.slope, v, u, h);
@@ -448,10 +516,17 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(GemmArgs 
                         store_chunk<DT, kStream>(a.dg, at_c.out, at_c.inside, v);
                         store_chunk<DT, kStream>(a.du, at_c.out, at_c.inside, u);
                     }
-                } else if (gridDim.y > 1) {
+                } else if (!kGroups && gridDim.y > 1) {
                     store_chunk<IABN_F32, kCached>(
                         a.part, (int64_t(blockIdx.y) * gridDim.z + z) * a.M * a.N + at_c.out, at_c.inside, v);
                 } else {
+                    if constexpr (kGroups && kBase == kGemmDown) {
+                        // (Weighted before it is rounded: an intermediate value overflows
+                        // only where a term of the tokens' sum does.)
+                        const float w = pair_weight(a, tokens, m0 + wm + p * 16 + at_c.row, a.M);
+#pragma unroll
+                        for (int j = 0; j < kChunk; ++j) v[j] *= w;
+                    }
                     store_chunk<DT, kCached>(z ? a.out[1] : a.out[0], at_c.out, at_c.inside, v);
                 }
             }

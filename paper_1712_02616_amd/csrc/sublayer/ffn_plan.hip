@@ -1,6 +1,6 @@
 // How the gated feed-forward block's products are cut (the tiles and the split
 // of the sum over k), and the kernel that joins a split sum.
-#include "ffn.h"
+#include "groups.h"
 
 namespace iabn_impl {
 namespace {
@@ -78,6 +78,35 @@ GemmPlan plan_gemm(int dtype, GemmKind kind, bool direct, int64_t M, int64_t N, 
                 best_us = us;
                 best = {t, s};
             }
+        }
+    }
+    return best;
+}
+
+// The same costs for products over groups of rows, without a split.  Where the rows
+// are the groups', half a tile of each expert's is empty on average; where k is, its
+// mean counts.
+TileSize plan_grouped(int dtype, GemmKind kind, bool direct, int64_t P, int64_t E, int64_t M, int64_t N, int64_t K,
+                      int products) {
+    const int64_t step = dtype == IABN_F32 ? 32 : 64, busy = E < P ? E : P;
+    const int64_t steps = kind == kGemmDw ? div_up(P / E, step) + 1 : div_up(K, step) * (kind == kGemmDx ? 2 : 1);
+    TileSize best = kTile64;
+    float best_us = 0.0f;
+    for (TileSize t : {kTile256, kTile128, kTile64, kTile32}) {
+        const TileCost& cost = kCost[dtype == IABN_F32][direct][t];
+        if (cost.ends == 0.0f) continue;
+        const int64_t tm = t == kTile256 ? 256 : t == kTile128 ? 128 : t == kTile64 ? 64 : 32;
+        const int64_t tn = (t == kTile256 ? 256 : 128) / (kind == kGemmUp ? 2 : 1);
+        const int64_t tiles = (kind == kGemmDw ? div_up(M, tm) * E : P / tm + (busy + 1) / 2) * div_up(N, tn) * products;
+        const int64_t on_cu = div_up(tiles, kCUs);
+        const float full = static_cast<float>((on_cu - 1) / 4);
+        const float slow = dtype != IABN_F32 && !direct && kind >= kGemmDh ? kStridedLoads : 1.0f;
+        const float per_step = slow * (full * cost.step[3] + cost.step[(on_cu - 1) % 4]);
+        const float us = static_cast<float>(steps) * per_step +
+                         static_cast<float>(on_cu) * cost.ends * (kind == kGemmDh ? kGatingEnds : 1.0f);
+        if (best_us == 0.0f || us < best_us) {
+            best_us = us;
+            best = t;
         }
     }
     return best;

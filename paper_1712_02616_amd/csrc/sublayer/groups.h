@@ -1,0 +1,196 @@
+// Products over groups of rows: those of routed experts.  The pairs (token, slot) are
+// sorted by expert (a plan: routed.h); expert e has the sorted rows
+// offsets[e] .. offsets[e + 1], and weights of its own.
+//
+//   up, dh:   X's rows are tokens, gathered by the plan's order; down, dx: X's rows are
+//             sorted ones.  Y is the expert's weights.
+//   dW:       the sum over k is over the expert's rows; one operand's are tokens.
+//
+// A block finds its expert from the offsets (which only the GPU knows): a wave
+// adds up how many tiles each expert has.  The numbers of a plan are held to their
+// ranges where they are used, so that a wrong one reads a wrong row of the right
+// matrix.
+#pragma once
+
+#include <type_traits>
+
+#include "ffn.h"
+#include "routed.h"
+
+namespace iabn_impl {
+
+// The kinds of products over groups: kOverGroups + a GemmKind, where dW's x is the
+// tokens' operand, or its y.
+constexpr int kOverGroups = 10, kGroupDwTokensY = kOverGroups + kGemmDw + 1;
+
+struct GroupArgs : GemmArgs {
+    const int32_t *offsets, *order;
+    const float* weights;    // [M, k]: down, dh
+    float* dots;             // dh: [P][ceil(F/64)], sums of h*(dy Wd) over 64 columns
+    iabn_divmagic_t top;     // k
+    int32_t E, P;
+    int64_t expert_stride;   // elements from one expert's matrix to the next one's
+};
+template <int KIND>
+using ArgsOf = std::conditional_t<(KIND < kOverGroups), GemmArgs, GroupArgs>;
+
+// The tokens of a group's rows.
+struct Tokens {
+    const int32_t* order;  // from the group's first row
+    uint32_t pairs;
+    iabn_divmagic_t top;
+    __device__ __forceinline__ uint32_t pair(uint32_t entry) const { return min(entry, pairs - 1); }
+    __device__ __forceinline__ uint32_t of(uint32_t entry) const { return iabn_divmagic_div(pair(entry), top); }
+    __device__ __forceinline__ int64_t operator()(int64_t row) const { return of(order[row]); }
+};
+
+__device__ __forceinline__ float pair_weight(const GroupArgs& a, const Tokens& tokens, int64_t m, int64_t M) {
+    return m < M ? a.weights[tokens.pair(tokens.order[m])] : 0.0f;
+}
+
+__device__ __forceinline__ void rows_of(const int32_t* offsets, int e, int P, int& first, int& rows) {
+    first = min(max(offsets[e], 0), P);
+    rows = max(min(offsets[e + 1], P) - first, 0);
+}
+
+// A tile's number for a block's: runs of `run` consecutive tiles stay on one XCD
+// (its L2 holds what they share), the runs go round the XCDs (experts differ in how
+// many rows they have).
+__device__ __forceinline__ uint32_t spread(uint32_t block, uint32_t n, uint32_t run) {
+    const uint32_t round = run * kXcds, whole = n / round * round;
+    if (block < whole) {
+        const uint32_t x = block % kXcds, j = block / kXcds;
+        return j / run * round + x * run + j % run;
+    }
+    const uint32_t left = n - whole, b = block - whole, x = b % kXcds, j = b / kXcds;
+    return whole + x * (left / kXcds) + min(x, left % kXcds) + j;
+}
+
+// Tile `t` of tiles_m x tiles_n, in strips of a few tiles of m.
+__device__ __forceinline__ void strip_of(uint32_t t, int tiles_m, int tiles_n, int strip_height, int& tm, int& tn) {
+    const uint32_t strip = t / (strip_height * tiles_n), in = t - strip * (strip_height * tiles_n);
+    const uint32_t height = min(static_cast<uint32_t>(strip_height), tiles_m - strip * strip_height);
+    tn = static_cast<int>(in / height);
+    tm = static_cast<int>(strip * strip_height + in % height);
+}
+
+// The expert that tile number t of the launch (tiles_n tiles for every TM of an
+// expert's rows) belongs to, and the tile's number in it; false past the last.
+struct Group {
+    int expert, first, rows;
+    uint32_t tile;
+};
+template <int TM>
+__device__ __forceinline__ bool find_group(const int32_t* offsets, int E, int P, uint32_t tiles_n, uint32_t run,
+                                           Group& g) {
+    const int each = (E + kWave - 1) / kWave, e0 = static_cast<int>(lane_id()) * each, e1 = min(e0 + each, E);
+    int tiles = 0;
+    for (int e = e0; e < e1; ++e) {
+        int first, rows;
+        rows_of(offsets, e, P, first, rows);
+        tiles += (rows + TM - 1) / TM;
+    }
+    int upto = tiles;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const int o = __shfl_up(upto, d);
+        if (static_cast<int>(lane_id()) >= d) upto += o;
+    }
+    const uint32_t total = static_cast<uint32_t>(__builtin_amdgcn_readlane(upto, kWave - 1)) * tiles_n;
+    if (blockIdx.x >= total) return false;
+    const uint32_t t = run ? spread(blockIdx.x, total, run) : blockIdx.x;
+    const int m = static_cast<int>(t / tiles_n);
+    const uint64_t has = __ballot(upto - tiles <= m && m < upto);
+    const int lane = __builtin_ctzll(has);
+    int before = upto - tiles, expert = e0, first = 0, rows = 0;
+    for (int e = e0; e < e1; ++e) {
+        rows_of(offsets, e, P, first, rows);
+        const int n = (rows + TM - 1) / TM;
+        expert = e;
+        if (m < before + n) break;
+        before += n;
+    }
+    g.expert = __builtin_amdgcn_readlane(expert, lane);
+    g.first = __builtin_amdgcn_readlane(first, lane);
+    g.rows = __builtin_amdgcn_readlane(rows, lane);
+    g.tile = t - static_cast<uint32_t>(__builtin_amdgcn_readlane(before, lane)) * tiles_n;
+    return true;
+}
+
+// Turns the launch's arguments into those of this block's group: its rows or its
+// part of k, its weights, its outputs.
+constexpr int kGroupStrip = 8;
+template <int DT, int KIND, int TM>
+__device__ __forceinline__ bool enter_group(GroupArgs& a, int tiles_m, int tiles_n, int& tm, int& tn,
+                                            int64_t& group_row, Tokens& tokens) {
+    using T = typename Elem<DT>::T;
+    constexpr uint32_t kRun = TM == 256 ? 32 : 64;
+    const auto move = [](Operand& o, int64_t by) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) o.p[q] = static_cast<const T*>(o.p[q]) + by;
+    };
+    int first;
+    if constexpr (KIND == kOverGroups + kGemmDw || KIND == kGroupDwTokensY) {
+        const uint32_t t = spread(blockIdx.x, gridDim.x, kRun), per = tiles_m * tiles_n, e = t / per;
+        strip_of(t - e * per, tiles_m, tiles_n, kGroupStrip, tm, tn);
+        int rows;
+        rows_of(a.offsets, static_cast<int>(e), a.P, first, rows);
+        first = __builtin_amdgcn_readfirstlane(first), rows = __builtin_amdgcn_readfirstlane(rows);
+        a.K = rows;
+        if constexpr (KIND != kGroupDwTokensY) move(a.y, first * a.y.ld);
+        else move(a.x, first * a.x.ld);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) a.out[q] = static_cast<T*>(a.out[q]) + e * a.expert_stride;
+    } else {
+        Group g;
+        if (!find_group<TM>(a.offsets, a.E, a.P, tiles_n, kRun, g)) return false;
+        first = g.first;
+        a.M = g.rows;
+        strip_of(g.tile, (g.rows + TM - 1) / TM, tiles_n, kGroupStrip, tm, tn);
+        if constexpr (KIND == kOverGroups + kGemmDown || KIND == kOverGroups + kGemmDx) move(a.x, first * a.x.ld);
+        move(a.y, g.expert * a.expert_stride);
+        group_row = first;
+    }
+    tokens = {a.order + first, static_cast<uint32_t>(a.P), a.top};
+    return true;
+}
+
+// The products of routed experts (`kind`: one over groups).  Of a few tokens, the
+// second one goes to `part`, [splits][P][N] fp32, not weighted.
+template <int DT>
+void launch_grouped(int kind, const GroupArgs& a, int products, hipStream_t st);
+template <int DT>
+void launch_grouped_few(int kind, const GroupArgs& a, hipStream_t st);
+
+extern template void launch_grouped<IABN_F32>(int, const GroupArgs&, int, hipStream_t);
+extern template void launch_grouped<IABN_F16>(int, const GroupArgs&, int, hipStream_t);
+extern template void launch_grouped<IABN_BF16>(int, const GroupArgs&, int, hipStream_t);
+extern template void launch_grouped_few<IABN_F32>(int, const GroupArgs&, hipStream_t);
+extern template void launch_grouped_few<IABN_F16>(int, const GroupArgs&, hipStream_t);
+extern template void launch_grouped_few<IABN_BF16>(int, const GroupArgs&, hipStream_t);
+
+// The tile of a grouped product.
+TileSize plan_grouped(int dtype, GemmKind kind, bool direct, int64_t P, int64_t E, int64_t M, int64_t N, int64_t K,
+                      int products);
+
+// Whether the forward takes the few tokens' kernels, over how many blocks their
+// second product's sum is split.
+bool few_pairs(int64_t M, int64_t P, int64_t E);
+int plan_grouped_few(int64_t P, int64_t E, int64_t N, int64_t K, int dtype);
+
+// y_t = sum over the slots s of the terms of its pairs' rows (place[t*k + s]),
+// weighted where `weights` is not null: [splits][P][C] of fp32 then, else [P][C].
+struct CombineArgs {
+    const void* terms;
+    const int32_t* place;
+    const float* weights;
+    void* y;
+    int64_t M, C;
+    int32_t k, P, splits;
+};
+void launch_combine(int dtype, const CombineArgs& a, hipStream_t st);
+
+// dweights[i] = sum of the n dots of pair i's row, 0 where it has none.
+void launch_dots(const float* dots, const int32_t* place, float* dweights, int64_t P, int64_t n, hipStream_t st);
+
+}  // namespace iabn_impl

@@ -1,0 +1,264 @@
+"""Python binding of libiabn's routed experts and of the clipping of gradients.
+Marshalling only, as the rest of the package (``__init__``).
+
+Tensors: rows are contiguous [..., C] in float32, float16 or bfloat16 on a HIP
+device, the experts' weights contiguous [E, F, C] (and [E, C, F]) of the same type;
+choices and plans are contiguous int32, weights of choices and biases contiguous
+float32 on the same device.  Calls are asynchronous on ``stream`` (default: torch's
+current stream for the tensors' device).
+"""
+
+from __future__ import annotations
+
+import ctypes
+import math
+
+import torch
+
+import paper_1712_02616_amd as _iabn
+
+from .sublayer import ACTIVATIONS, _code, _fast, _Rows
+
+# (All of them are names of the package too; its own list is that of the layer's and
+# the feed-forward sublayer's.)
+__all__ = ["SCORES", "iabn_route_forward", "iabn_route_backward", "iabn_experts_plan_size", "iabn_experts_plan",
+           "iabn_experts_workspace_size", "iabn_experts_forward", "iabn_experts_backward",
+           "iabn_grad_norm_workspace_size", "iabn_grad_norm", "iabn_grad_clip"]
+
+# iabn_score_t.
+SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def _choices(rows, t, dtype, what, k=None):
+    """(pointer, k) of a contiguous [rows, k] tensor of choices or their weights."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % what)
+    if t.dtype != dtype or t.dim() < 1 or not t.is_contiguous() or t.device != rows.device:
+        raise ValueError("%s must be a contiguous %s tensor on %s" % (what, dtype, rows.device))
+    n = t.shape[-1]
+    if t.numel() != rows.R * n or (k is not None and n != k):
+        raise ValueError("%s must be [%d, %s]" % (what, rows.R, "k" if k is None else k))
+    return _iabn._ptr(t), n
+
+
+def iabn_route_forward(logits, experts, weights, bias=None, score="softmax", groups=1, groups_kept=None,
+                       group_top=1, renormalise=False, scale=1.0, stream=None):
+    """The k experts of each row of ``logits`` [..., E] and their weights; returns
+    ``(experts, weights)``.
+
+    ``experts``: [..., k] int32, ``weights``: [..., k] float32, both written.
+    ``score``: "softmax" or "sigmoid".  ``bias``: [E] float32, for the choice alone.
+    ``groups_kept`` of ``groups`` (None: all) are chosen from, by the sum of their
+    ``group_top`` highest."""
+    code = _code(SCORES, score, "score")
+    kept = groups if groups_kept is None else groups_kept
+    if stream is None and _fast("route_forward", logits, experts, weights, bias, code, groups, kept,
+                                group_top, int(bool(renormalise)), scale):
+        return experts, weights
+    rows = _Rows()
+    lp = rows(logits, "logits")
+    ep, k = _choices(rows, experts, torch.int32, "experts")
+    wp, _ = _choices(rows, weights, torch.float32, "weights", k)
+    _iabn._enqueue("iabn_route_forward", rows.device, stream, lp, rows.code, rows.floats(bias, rows.C, "bias"),
+                   ep, wp, code, int(groups), int(kept), int(group_top), int(bool(renormalise)), float(scale),
+                   rows.R, rows.C, k)
+    return experts, weights
+
+
+def iabn_route_backward(dweights, logits, experts, dlogits, score="softmax", renormalise=False, scale=1.0,
+                        stream=None):
+    """The gradient of ``logits`` from that of iabn_route_forward's weights, for the
+    ``experts`` that it chose; ``dlogits`` may be ``logits``.  Returns ``dlogits``."""
+    code = _code(SCORES, score, "score")
+    if stream is None and _fast("route_backward", dweights, logits, experts, dlogits, code,
+                                int(bool(renormalise)), scale):
+        return dlogits
+    rows = _Rows()
+    lp, dp = rows(logits, "logits"), rows(dlogits, "dlogits")
+    ep, k = _choices(rows, experts, torch.int32, "experts")
+    wp, _ = _choices(rows, dweights, torch.float32, "dweights", k)
+    _iabn._enqueue("iabn_route_backward", rows.device, stream, wp, lp, ep, dp, rows.code, code,
+                   int(bool(renormalise)), float(scale), rows.R, rows.C, k)
+    return dlogits
+
+
+def iabn_experts_plan_size(M: int, k: int, E: int) -> int:
+    """The int32 values of a plan for M tokens with k of E experts each."""
+    return int((_iabn._lib or _iabn.load()).iabn_experts_plan_size(int(M), int(k), int(E)))
+
+
+def _plan(plan, M, k, E, device):
+    if not isinstance(plan, torch.Tensor):
+        raise TypeError("plan must be a torch.Tensor")
+    if plan.dtype != torch.int32 or not plan.is_contiguous() or plan.device != device:
+        raise ValueError("plan must be a contiguous int32 tensor on %s" % device)
+    need = iabn_experts_plan_size(M, k, E)
+    if plan.numel() < need or need == 0:
+        raise ValueError("plan must hold the %d values of M=%d, k=%d, E=%d" % (need, M, k, E))
+    return _iabn._ptr(plan)
+
+
+def iabn_experts_plan(experts, plan, E, stream=None):
+    """Sorts the pairs (token, slot) of ``experts`` [..., k] int32 by expert into
+    ``plan``, iabn_experts_plan_size int32 values: offsets [E + 1], order [M*k], place
+    [M*k] and what the kernels need.  Returns ``plan``."""
+    if stream is None and _fast("experts_plan", experts, plan, E):
+        return plan
+    if not isinstance(experts, torch.Tensor):
+        raise TypeError("experts must be a torch.Tensor")
+    if experts.dtype != torch.int32 or experts.dim() < 1 or not experts.is_contiguous():
+        raise ValueError("experts must be a contiguous int32 tensor of [..., k]")
+    if experts.device.type != "cuda":
+        raise ValueError("experts must be on a HIP device")
+    k, M, dev = experts.shape[-1], math.prod(experts.shape[:-1]), experts.device
+    _iabn._enqueue("iabn_experts_plan", dev, stream, _iabn._ptr(experts), _plan(plan, M, k, E, dev), M, k,
+                   int(E))
+    return plan
+
+
+def iabn_experts_workspace_size(M: int, k: int, E: int, C: int, F: int, dtype) -> int:
+    """Workspace bytes of iabn_experts_forward and iabn_experts_backward; ``dtype``
+    is a torch dtype or a dtype code."""
+    code = _iabn.DTYPE_CODES[dtype] if isinstance(dtype, torch.dtype) else int(dtype)
+    return int(_iabn.load().iabn_experts_workspace_size(int(M), int(k), int(E), int(C), int(F), code))
+
+
+def _expert_weight(rows, t, shape, what):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % what)
+    if tuple(t.shape) != shape or t.dtype != rows.dtype or not t.is_contiguous() or t.device != rows.device:
+        raise ValueError("%s must be contiguous %s of %s on %s" % (what, list(shape), rows.dtype, rows.device))
+    return _iabn._ptr(t)
+
+
+def _sizes(rows, w_gate):
+    if not isinstance(w_gate, torch.Tensor):
+        raise TypeError("w_gate must be a torch.Tensor")
+    if w_gate.dim() != 3:
+        raise ValueError("w_gate must be [E, F, C]")
+    return w_gate.shape[0], w_gate.shape[1], rows.C
+
+
+def iabn_experts_forward(x, plan, weights, w_gate, w_up, w_down, y, g=None, u=None, act="silu", slope=0.01,
+                         workspace=None, stream=None):
+    """y_t = sum over t's pairs of weight * (act(x_t w_gate[e]^T) * (x_t w_up[e]^T))
+    w_down[e]^T, for the pairs of ``plan``; returns ``y``.
+
+    ``weights``: [..., k] float32.  ``w_gate``, ``w_up``: [E, F, C], ``w_down``: [E, C,
+    F].  ``g``, ``u``: [..., F] of rows*k rows, the projections in the plan's order,
+    written for the backward where given.  ``act``: "silu", "gelu" or "leaky"
+    (``slope``)."""
+    code = _code(ACTIVATIONS, act, "act")
+    if stream is None and _fast("experts_forward", x, plan, weights, w_gate, w_up, w_down, y, g, u, code, slope,
+                                workspace):
+        return y
+    rows = _Rows()
+    xp, yp = rows(x, "x"), rows(y, "y")
+    E, F, C = _sizes(rows, w_gate)
+    wp, k = _choices(rows, weights, torch.float32, "weights")
+    pp = _plan(plan, rows.R, k, E, rows.device)
+    ws = [_expert_weight(rows, t, s, n) for t, s, n in (
+        (w_gate, (E, F, C), "w_gate"), (w_up, (E, F, C), "w_up"), (w_down, (E, C, F), "w_down"))]
+    gp, up = rows.matrix(g, rows.R * k, F, "g", True), rows.matrix(u, rows.R * k, F, "u", True)
+    space, sp, sb = _iabn._take(iabn_experts_workspace_size(rows.R, k, E, C, F, rows.code), rows.device,
+                                workspace, stream)
+    _iabn._enqueue("iabn_experts_forward", rows.device, stream, xp, pp, wp, *ws, yp, gp, up, rows.code, code,
+                   float(slope), rows.R, k, E, C, F, sp, sb)
+    return y
+
+
+def iabn_experts_backward(dy, x, plan, weights, g, u, w_gate, w_up, w_down, dx, dweights, dg, du, dw_gate,
+                          dw_up, dw_down, act="silu", slope=0.01, workspace=None, stream=None):
+    """The gradients of iabn_experts_forward from ``dy`` and the ``g``, ``u`` that it
+    gave; ``dg`` may be ``g`` and ``du`` may be ``u``.  Returns ``dx``."""
+    code = _code(ACTIVATIONS, act, "act")
+    if stream is None and _fast("experts_backward", dy, x, plan, weights, g, u, w_gate, w_up, w_down, dx,
+                                dweights, dg, du, dw_gate, dw_up, dw_down, code, slope, workspace):
+        return dx
+    rows = _Rows()
+    dyp, xp = rows(dy, "dy"), rows(x, "x")
+    E, F, C = _sizes(rows, w_gate)
+    wp, k = _choices(rows, weights, torch.float32, "weights")
+    pp = _plan(plan, rows.R, k, E, rows.device)
+    P = rows.R * k
+    kept = [rows.matrix(t, P, F, n) for t, n in ((g, "g"), (u, "u"))]
+    shapes = {"gate": (E, F, C), "up": (E, F, C), "down": (E, C, F)}
+    ws = [_expert_weight(rows, t, shapes[n], "w_" + n) for t, n in ((w_gate, "gate"), (w_up, "up"),
+                                                                    (w_down, "down"))]
+    outs = [rows(dx, "dx"), _choices(rows, dweights, torch.float32, "dweights", k)[0],
+            rows.matrix(dg, P, F, "dg"), rows.matrix(du, P, F, "du")]
+    outs += [_expert_weight(rows, t, shapes[n], "dw_" + n) for t, n in ((dw_gate, "gate"), (dw_up, "up"),
+                                                                       (dw_down, "down"))]
+    space, sp, sb = _iabn._take(iabn_experts_workspace_size(rows.R, k, E, C, F, rows.code), rows.device,
+                                workspace, stream)
+    _iabn._enqueue("iabn_experts_backward", rows.device, stream, dyp, xp, pp, wp, *kept, *ws, *outs, rows.code,
+                   code, float(slope), rows.R, k, E, C, F, sp, sb)
+    return dx
+
+
+class _List:
+    """A list of tensors as the host arrays of the entry points."""
+
+    def __init__(self, tensors, what):
+        self.tensors = list(tensors)
+        for t in self.tensors:
+            if not isinstance(t, torch.Tensor):
+                raise TypeError("%s must be torch.Tensors" % what)
+            if t.dtype not in _iabn.DTYPE_CODES or not t.is_contiguous() or t.device.type != "cuda":
+                raise ValueError("%s must be contiguous float32, float16 or bfloat16 tensors on a HIP device" % what)
+            if t.device != self.tensors[0].device:
+                raise ValueError("%s must be on one device" % what)
+        n = len(self.tensors)
+        self.count = n
+        self.pointers = (ctypes.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
+        self.dtypes = (ctypes.c_int * n)(*[_iabn.DTYPE_CODES[t.dtype] for t in self.tensors])
+        self.sizes = (ctypes.c_int64 * n)(*[t.numel() for t in self.tensors])
+
+
+def _norm_value(norm, device):
+    if not isinstance(norm, torch.Tensor):
+        raise TypeError("norm must be a torch.Tensor")
+    if norm.dtype != torch.float32 or norm.numel() != 1 or norm.device.type != "cuda" or \
+            (device is not None and norm.device != device):
+        raise ValueError("norm must be one float32 value on the gradients' HIP device")
+    return _iabn._ptr(norm)
+
+
+def iabn_grad_norm_workspace_size(sizes) -> int:
+    """Workspace bytes of iabn_grad_norm for tensors of these numbers of elements."""
+    sizes = list(sizes)
+    return int(_iabn.load().iabn_grad_norm_workspace_size((ctypes.c_int64 * len(sizes))(*sizes), len(sizes)))
+
+
+def iabn_grad_norm(grads, norm, workspace=None, stream=None):
+    """norm[0] = sqrt of the sum of the squares of all ``grads`` (a list of tensors
+    of any shapes and types); returns ``norm``, one float32 value."""
+    if not isinstance(grads, (list, tuple)):
+        grads = list(grads)
+    if stream is None and _fast("grad_norm", grads, norm, workspace):
+        return norm
+    of = _List(grads, "grads")
+    np_ = _norm_value(norm, of.tensors[0].device if of.count else None)
+    ws, wp, wb = _iabn._take(int(_iabn.load().iabn_grad_norm_workspace_size(of.sizes, of.count)), norm.device,
+                             workspace, stream)
+    _iabn._enqueue("iabn_grad_norm", norm.device, stream, of.pointers, of.dtypes, of.sizes, of.count, np_, wp, wb)
+    return norm
+
+
+def iabn_grad_clip(grads, outs, norm, max_norm, stream=None):
+    """outs = grads * min(1, max_norm/(norm[0] + 1e-6)), tensor by tensor; ``outs`` may
+    be ``grads``.  Returns ``outs``."""
+    if not isinstance(grads, (list, tuple)):
+        grads = list(grads)
+    if not isinstance(outs, (list, tuple)):
+        outs = list(outs)
+    if stream is None and _fast("grad_clip", grads, outs, norm, max_norm):
+        return outs
+    of, to = _List(grads, "grads"), _List(outs, "outs")
+    if of.count != to.count or any(a.numel() != b.numel() or a.dtype != b.dtype or a.device != b.device
+                                   for a, b in zip(of.tensors, to.tensors)):
+        raise ValueError("outs must match grads in number, sizes, dtypes and device")
+    np_ = _norm_value(norm, of.tensors[0].device if of.count else None)
+    _iabn._enqueue("iabn_grad_clip", norm.device, stream, of.pointers, to.pointers, of.dtypes, of.sizes, of.count,
+                   np_, float(max_norm))
+    return outs
