@@ -48,7 +48,7 @@ __global__ __launch_bounds__(512) void few_kernel(ArgsOf<KIND> a) {
     const int waves = blockDim.x / kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int i = lane_id() & 15, g = lane_id() >> 4;
     int64_t n0 = int64_t(blockIdx.x) * 16;
-    int64_t group_row = 0;
+    int64_t group_row = 0, expert = 0;
     Tokens tokens = {};
     if constexpr (kGroups) {
         // A block has 16 columns for up to MT*16 rows of one expert.
@@ -60,13 +60,12 @@ __global__ __launch_bounds__(512) void few_kernel(ArgsOf<KIND> a) {
         a.M = min(group.rows - tile * MT * 16, MT * 16);
         group_row = group.first + tile * MT * 16;
         tokens = {a.order + group_row, static_cast<uint32_t>(a.P), a.top};
-#pragma unroll
-        for (int q = 0; q < NW; ++q) a.y.p[q] = static_cast<const T*>(a.y.p[q]) + group.expert * a.expert_stride;
+        expert = group.expert * a.expert_stride;
     }
     const T *w[NW], *x[MT];
 #pragma unroll
     for (int q = 0; q < NW; ++q)
-        w[q] = static_cast<const T*>(a.y.p[q]) + min(n0 + i, a.N - 1) * a.y.ld + g * E;
+        w[q] = static_cast<const T*>(a.y.p[q]) + (kGroups ? expert : 0) + min(n0 + i, a.N - 1) * a.y.ld + g * E;
 #pragma unroll
     for (int t = 0; t < MT; ++t)
         x[t] = static_cast<const T*>(a.x.p[0]) + few_row<KIND>(a, tokens, group_row, t * 16 + i) * a.x.ld + g * E;

@@ -87,12 +87,13 @@ struct Stage {
     // Through registers.  rows: how many of the operand's rows there are from
     // row0 on.
     u32x4 r[kLoads];
-    __device__ __forceinline__ void load(const Operand& o, int seg, int64_t row0, int64_t rows,
+    template <typename Op>
+    __device__ __forceinline__ void load(const Op& o, int seg, int64_t row0, int64_t rows,
                                          int64_t k0, int64_t K, const Tokens& tokens = {}) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int line = first_line() + i * kLineStep, c = chunk(i) * E;
-            const T* p = static_cast<const T*>(o.p[KS ? seg : matrix_of(line, seg)]);
+            const T* p = static_cast<const T*>(matrix(o, KS ? seg : matrix_of(line, seg)));
             if constexpr (KS && GATHER)
                 r[i] = load16_first<DT>(p + tokens(min(k0 + line, K - 1)) * o.ld + row0 + c,
                                         k0 + line < K ? rows - c : 0);
@@ -118,11 +119,12 @@ struct Stage {
     uint32_t off[kLoads];  // bytes from the step's first element
     // (k strided, GATHER: the next step's entries of the plan.)
     uint32_t entry[KS && GATHER ? kLoads : 1];
-    __device__ __forceinline__ void prepare(const Operand& o, int64_t row0, int64_t rows, const Tokens& tokens = {}) {
+    template <typename Op>
+    __device__ __forceinline__ void prepare(const Op& o, int64_t row0, int64_t rows, const Tokens& tokens = {}) {
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
             // (Kept in scalar registers, not loaded from the arguments at each step.)
-            const uint64_t p = reinterpret_cast<uint64_t>(static_cast<const T*>(o.p[q]) +
+            const uint64_t p = reinterpret_cast<uint64_t>(static_cast<const T*>(matrix(o, q)) +
                                                           (KS ? row0 : GATHER ? 0 : row0 * o.ld));
             base[q] = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(p))) |
                       uint64_t(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(p >> 32)))) << 32;
@@ -150,7 +152,8 @@ struct Stage {
             for (int i = 0; i < kLoads; ++i)
                 entry[i] = tokens.order[min(k0 + first_line() + i * kLineStep, K - 1)];
     }
-    __device__ __forceinline__ void fetch(const Operand& o, int seg, int64_t k0, char* lds,
+    template <typename Op>
+    __device__ __forceinline__ void fetch(const Op& o, int seg, int64_t k0, char* lds,
                                           const Tokens& tokens = {}) const {
 #if defined(__HIP_DEVICE_COMPILE__)  // (the host's pass does not know the buffer types)
         typedef __attribute__((address_space(3))) void lds_t;
@@ -253,13 +256,19 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
     char *const lds0 = lds, *const lds1 = lds + kBuffer;
 
     int tm, tn;
-    int64_t group_row = 0;  // the rows of the group's outputs begin there
     Tokens tokens = {};
+    Entered group = {};
     if constexpr (kGroups) {
-        if (!enter_group<DT, KIND, TM>(a, tiles_m, tiles_n, tm, tn, group_row, tokens)) return;
+        if (!enter_group<DT, KIND, TM>(a, tiles_m, tiles_n, tm, tn, group, tokens)) return;
+        (kBase == kGemmDw ? a.K : a.M) = group.rows;
     } else {
         tile_of(tiles_m, tiles_n, tm, tn);
     }
+    const auto operand = [](const auto& whole, const auto& own) -> const auto& {
+        if constexpr (kGroups) return own;
+        else return whole;
+    };
+    const auto &x = operand(a.x, group.x), &y = operand(a.y, group.y);
     const int64_t m0 = int64_t(tm) * TM;
     constexpr int kCols = Kind::kDual ? TN / 2 : TN;  // columns of the output
     const int64_t n0 = int64_t(tn) * kCols;
@@ -308,8 +317,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
         const auto fetch = [&](int kt, char* buf) __attribute__((always_inline)) {
             const int seg = Kind::kSegs > 1 ? (kt >= whole ? 1 : 0) : z;
             const int64_t k0 = int64_t(Kind::kSegs > 1 && seg ? kt - whole : kt) * BK;
-            sx.fetch(a.x, seg, k0, buf, tokens);
-            sy.fetch(a.y, seg, k0, buf + SX::kBytes, tokens);
+            sx.fetch(x, seg, k0, buf, tokens);
+            sy.fetch(y, seg, k0, buf + SX::kBytes, tokens);
             sx.look_up(k0 + BK, a.K, tokens);
             sy.look_up(k0 + BK, a.K, tokens);
         };
@@ -360,8 +369,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
             turn(kt, b0, b1);
             if (kt + 1 < hi) turn(kt + 1, b1, b0);
         };
-        sx.prepare(a.x, m0, a.M - m0, tokens);
-        sy.prepare(a.y, n0, a.N - n0, tokens);
+        sx.prepare(x, m0, a.M - m0, tokens);
+        sy.prepare(y, n0, a.N - n0, tokens);
         if (kGroups && lo < hi) {
             sx.look_up(int64_t(lo) * BK, a.K, tokens);
             sy.look_up(int64_t(lo) * BK, a.K, tokens);
@@ -379,8 +388,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
         const auto load = [&](int kt) __attribute__((always_inline)) {
             const int seg = Kind::kSegs > 1 ? (kt >= per_seg ? 1 : 0) : z;
             const int64_t k0 = int64_t(whole + (Kind::kSegs > 1 && seg ? kt - per_seg : kt)) * BK;
-            sx.load(a.x, seg, m0, a.M - m0, k0, a.K, tokens);
-            sy.load(a.y, seg, n0, a.N - n0, k0, a.K, tokens);
+            sx.load(x, seg, m0, a.M - m0, k0, a.K, tokens);
+            sy.load(y, seg, n0, a.N - n0, k0, a.K, tokens);
         };
         const auto store = [&](char* buf) __attribute__((always_inline)) {
             sx.store(buf);
@@ -432,7 +441,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
         r.row = at_c / kCh, r.col = at_c % kCh * kChunk;
         const int64_t m = m0 + wm + p * 16 + r.row, n = n0 + (Kind::kDual ? wn / 2 : wn) + r.col;
         r.inside = m < a.M ? static_cast<int>(max(min(a.N - n, int64_t(kChunk)), int64_t(0))) : 0;
-        r.out = kGroups ? (group_row + m) * a.N + n : m * a.N + n;
+        r.out = kGroups ? (kBase == kGemmDw ? group.out : group.row0 * a.N) + m * a.N + n : m * a.N + n;
         return r;
     };
     // kGemmDh: g and u of the next chunks are on their way while one is finished.
@@ -492,7 +501,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
                         dot += dpp_f32<0x141, 0xF>(dot);
                         if (at_c.inside <= 0) continue;
                         if (at_c.col == 0)
-                            a.dots[(group_row + m0 + wm + p * 16 + at_c.row) * ((a.N + WN - 1) / WN) + (n0 + wn) / WN] = dot;
+                            a.dots[(group.row0 + m0 + wm + p * 16 + at_c.row) * ((a.N + WN - 1) / WN) + (n0 + wn) / WN] = dot;
                     } else {
                         gate_backward<DT>(a.act, a.slope, v, g, u, dg, du, h);
                     }

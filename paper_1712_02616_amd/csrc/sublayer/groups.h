@@ -117,40 +117,54 @@ __device__ __forceinline__ bool find_group(const int32_t* offsets, int E, int P,
     return true;
 }
 
-// Turns the launch's arguments into those of this block's group: its rows or its
-// part of k, its weights, its outputs.
+// A group's operand: its two matrices in registers (an array that is indexed by a
+// register would go through scratch memory).
+struct GroupOperand {
+    const void *p0, *p1;
+    int64_t ld;
+};
+__device__ __forceinline__ const void* matrix(const Operand& o, int q) { return o.p[q]; }
+__device__ __forceinline__ const void* matrix(const GroupOperand& o, int q) {
+    const uint64_t a = reinterpret_cast<uint64_t>(o.p0), b = reinterpret_cast<uint64_t>(o.p1);
+    return reinterpret_cast<const void*>(q ? b : a);
+}
+
+// What a block's group is: its rows or its part of k, its weights, its outputs.
+struct Entered {
+    GroupOperand x, y;
+    int64_t rows;  // of the group: M, or K of dW
+    int64_t row0;  // the group's first sorted row
+    int64_t out;   // elements from the outputs' first one (dW)
+};
 constexpr int kGroupStrip = 8;
 template <int DT, int KIND, int TM>
-__device__ __forceinline__ bool enter_group(GroupArgs& a, int tiles_m, int tiles_n, int& tm, int& tn,
-                                            int64_t& group_row, Tokens& tokens) {
+__device__ __forceinline__ bool enter_group(const GroupArgs& a, int tiles_m, int tiles_n, int& tm, int& tn,
+                                            Entered& in, Tokens& tokens) {
     using T = typename Elem<DT>::T;
     constexpr uint32_t kRun = TM == 256 ? 32 : 64;
-    const auto move = [](Operand& o, int64_t by) {
-#pragma unroll
-        for (int q = 0; q < 2; ++q) o.p[q] = static_cast<const T*>(o.p[q]) + by;
+    const auto from = [](const Operand& o, int64_t by) -> GroupOperand {
+        return {static_cast<const T*>(o.p[0]) + by, static_cast<const T*>(o.p[1]) + by, o.ld};
     };
-    int first;
+    int first, rows;
     if constexpr (KIND == kOverGroups + kGemmDw || KIND == kGroupDwTokensY) {
         const uint32_t t = spread(blockIdx.x, gridDim.x, kRun), per = tiles_m * tiles_n, e = t / per;
         strip_of(t - e * per, tiles_m, tiles_n, kGroupStrip, tm, tn);
-        int rows;
         rows_of(a.offsets, static_cast<int>(e), a.P, first, rows);
         first = __builtin_amdgcn_readfirstlane(first), rows = __builtin_amdgcn_readfirstlane(rows);
-        a.K = rows;
-        if constexpr (KIND != kGroupDwTokensY) move(a.y, first * a.y.ld);
-        else move(a.x, first * a.x.ld);
-#pragma unroll
-        for (int q = 0; q < 2; ++q) a.out[q] = static_cast<T*>(a.out[q]) + e * a.expert_stride;
+        in.x = from(a.x, KIND == kGroupDwTokensY ? first * a.x.ld : 0);
+        in.y = from(a.y, KIND == kGroupDwTokensY ? 0 : first * a.y.ld);
+        in.out = e * a.expert_stride;
     } else {
         Group g;
         if (!find_group<TM>(a.offsets, a.E, a.P, tiles_n, kRun, g)) return false;
-        first = g.first;
-        a.M = g.rows;
-        strip_of(g.tile, (g.rows + TM - 1) / TM, tiles_n, kGroupStrip, tm, tn);
-        if constexpr (KIND == kOverGroups + kGemmDown || KIND == kOverGroups + kGemmDx) move(a.x, first * a.x.ld);
-        move(a.y, g.expert * a.expert_stride);
-        group_row = first;
+        first = g.first, rows = g.rows;
+        strip_of(g.tile, (rows + TM - 1) / TM, tiles_n, kGroupStrip, tm, tn);
+        constexpr bool kSorted = KIND == kOverGroups + kGemmDown || KIND == kOverGroups + kGemmDx;
+        in.x = from(a.x, kSorted ? first * a.x.ld : 0);
+        in.y = from(a.y, g.expert * a.expert_stride);
+        in.out = 0;
     }
+    in.rows = rows, in.row0 = first;
     tokens = {a.order + first, static_cast<uint32_t>(a.P), a.top};
     return true;
 }
