@@ -46,7 +46,7 @@ template <int DT>
 bool group_fetchable(const Operand& o, int64_t row, bool strided, int64_t tokens) {
     constexpr int64_t es = sizeof(typename Elem<DT>::T), E = 16 / es;
     if (!fetchable<DT>(o, row)) return false;
-    return tokens == 0 || (tokens * o.ld * es < int64_t(1) << 32 && (!strided || row % E == 0));
+    return tokens == 0 || (tokens * o.ld * es <= 0xfffff000 && (!strided || row % E == 0));
 }
 
 template <int DT, int KIND>

@@ -152,23 +152,33 @@ struct Stage {
             for (int i = 0; i < kLoads; ++i)
                 entry[i] = tokens.order[min(k0 + first_line() + i * kLineStep, K - 1)];
     }
-    template <typename Op>
-    __device__ __forceinline__ void fetch(const Op& o, int seg, int64_t k0, char* lds,
-                                          const Tokens& tokens = {}) const {
+    // K >= 0: lines of k from there on (strided) are fetched as zeros, by offsets that
+    // lie outside of the buffer (row0: the tile's first column).
+    static constexpr uint32_t kOutside = 0xfffff000;
+    template <int LOADS, typename Op>
+    __device__ __forceinline__ void fetch(const Op& o, int seg, int64_t k0, char* lds, const Tokens& tokens,
+                                          int64_t K, int64_t row0) const {
 #if defined(__HIP_DEVICE_COMPILE__)  // (the host's pass does not know the buffer types)
         typedef __attribute__((address_space(3))) void lds_t;
         const uint64_t at = KS && GATHER ? 0 : (KS ? k0 * o.ld : k0) * sizeof(T);
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        uint32_t bytes = 0xffffffff;
+        if (KS && K >= 0) {
+            const uint64_t left = static_cast<uint64_t>(((K - k0) * o.ld - row0) * static_cast<int64_t>(sizeof(T)));
+            bytes = GATHER || left > kOutside ? kOutside : static_cast<uint32_t>(left);
+        }
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
+        for (int i = 0; i < LOADS; ++i) {
             // (A wave's lines are of one matrix: a wave covers 8 lines or fewer.)
             const int which =
                 DUAL ? __builtin_amdgcn_readfirstlane(matrix_of(first_line() + i * kLineStep, seg)) : seg;
             const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
-                reinterpret_cast<void*>((which ? base[1] : base[0]) + at), 0, 0xffffffff, 0x00027000);
+                reinterpret_cast<void*>((which ? base[1] : base[0]) + at), 0, static_cast<int>(bytes), 0x00027000);
             uint32_t from = off[i];
-            if constexpr (KS && GATHER)
+            if constexpr (KS && GATHER) {
                 from += tokens.of(entry[i]) * static_cast<uint32_t>(o.ld * static_cast<int64_t>(sizeof(T)));
+                if (K >= 0 && k0 + first_line() + i * kLineStep >= K) from = kOutside;
+            }
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 rsrc, (lds_t*)(lds + (wave * kWave + i * THREADS) * 16), 16, from, 0, 0, 0);
         }
@@ -282,22 +292,31 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
     // half of a wave's rows of x: its fragments, and their products.
     constexpr bool kAhead = NM * NN > 16;
     constexpr int kHalves = kAhead ? 2 : 1, kPhases = kSteps * kHalves, NH = NM / kHalves;
+    // The largest tile over groups: the last one of an expert's rows often holds no
+    // more than half of them.  Every wave then has rows of both halves of the tile,
+    // so that the phases of the empty half are left out ((32768 pairs of 64 experts,
+    // kShort).
+    constexpr bool kShort = kGroups && kBase != kGemmDw && kAhead;
+    const auto acc_row = [&](int g) __attribute__((always_inline)) {  // of accumulators g
+        return kShort ? g / NH * (TM / 2) + wave / WAVES_N * (WM / 2) + g % NH * 16 : wm + g * 16;
+    };
     u32x4 fy[kSteps][NN], fx[2][NH];
-    const auto read = [&](const char* __restrict__ buf, int phase) __attribute__((always_inline)) {
+    // (slot: where the fragments go, of two.)
+    const auto read = [&](const char* __restrict__ buf, int phase, int slot) __attribute__((always_inline)) {
         const int s = phase / kHalves, h = phase % kHalves;
         if (h == 0)
 #pragma unroll
             for (int j = 0; j < NN; ++j) fy[s][j] = SY::frag(buf + SX::kBytes, wn + j * 16, s);
 #pragma unroll
-        for (int i = 0; i < NH; ++i) fx[phase & 1][i] = SX::frag(buf, wm + (h * NH + i) * 16, s);
+        for (int i = 0; i < NH; ++i) fx[slot][i] = SX::frag(buf, acc_row(h * NH + i), s);
     };
-    const auto products = [&](int phase) __attribute__((always_inline)) {
+    const auto products = [&](int phase, int slot) __attribute__((always_inline)) {
         const int s = phase / kHalves, h = phase % kHalves;
 #pragma unroll
         for (int i = 0; i < NH; ++i)
 #pragma unroll
             for (int j = 0; j < NN; ++j)
-                acc[h * NH + i][j] = Mma<DT>::run(fy[s][j], fx[phase & 1][i], acc[h * NH + i][j]);
+                acc[h * NH + i][j] = Mma<DT>::run(fy[s][j], fx[slot][i], acc[h * NH + i][j]);
     };
     // Steps of K: whole ones that go straight to LDS, those of the first
     // product and then those of the second, and the others, through
@@ -306,7 +325,10 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
     // not fetch its last row.)
     constexpr int E = SX::E;
     const bool reaches = (Kind::kXStrided && a.M % E != 0) || (Kind::kYStrided && a.N % E != 0);
-    const int whole = DMA ? static_cast<int>((a.K - (reaches ? 1 : 0)) / BK) : 0, steps = whole * Kind::kSegs;
+    // (dW over groups: its sums end anywhere.  Where nothing reaches, the last step is
+    // fetched too, and its lines past the sum's end as zeros.)
+    constexpr bool kFill = kGroups && kBase == kGemmDw;
+    const int whole = !DMA ? 0 : static_cast<int>(kFill && !reaches ? (a.K + BK - 1) / BK : (a.K - (reaches ? 1 : 0)) / BK), steps = whole * Kind::kSegs;
     const int per_seg = static_cast<int>((a.K + BK - 1) / BK) - whole, rest = per_seg * Kind::kSegs;
     const int64_t all = steps + rest;
     const int begin = static_cast<int>(all * blockIdx.y / gridDim.y);
@@ -314,11 +336,11 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
     const int lo = min(begin, steps), hi = min(end, steps);
     const int from = max(begin - steps, 0), to = max(end - steps, 0);
     if constexpr (DMA) {
-        const auto fetch = [&](int kt, char* buf) __attribute__((always_inline)) {
+        const auto fetch = [&](int kt, char* buf, auto tall) __attribute__((always_inline)) {
             const int seg = Kind::kSegs > 1 ? (kt >= whole ? 1 : 0) : z;
             const int64_t k0 = int64_t(Kind::kSegs > 1 && seg ? kt - whole : kt) * BK;
-            sx.fetch(x, seg, k0, buf, tokens);
-            sy.fetch(y, seg, k0, buf + SX::kBytes, tokens);
+            sx.template fetch<tall ? SX::kLoads : SX::kLoads / 2>(x, seg, k0, buf, tokens, kFill ? a.K : -1, m0);
+            sy.template fetch<SY::kLoads>(y, seg, k0, buf + SX::kBytes, tokens, kFill ? a.K : -1, n0);
             sx.look_up(k0 + BK, a.K, tokens);
             sy.look_up(k0 + BK, a.K, tokens);
         };
@@ -340,34 +362,35 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         };
-        const auto turn = [&](int kt, char* __restrict__ cur, char* __restrict__ next) __attribute__((always_inline)) {
+        const auto turn = [&](int kt, char* __restrict__ cur, char* __restrict__ next, auto tall) __attribute__((always_inline)) {
             if constexpr (kAhead) {
+                constexpr int kStep = tall ? 1 : kHalves;  // of the phases that there are
 #pragma unroll
-                for (int p = 0; p + 1 < kPhases; ++p) {
-                    read(cur, p + 1);
-                    products(p);
+                for (int p = 0; p + kStep < kPhases; p += kStep) {
+                    read(cur, p + kStep, (p / kStep + 1) & 1);
+                    products(p, p / kStep & 1);
                     __builtin_amdgcn_sched_barrier(0);  // (products stay on their side)
                 }
                 meet();
-                if (kt + 2 < hi) fetch(kt + 2, cur);
-                if (kt + 1 < hi) read(next, 0);
-                products(kPhases - 1);
+                if (kt + 2 < hi) fetch(kt + 2, cur, tall);
+                if (kt + 1 < hi) read(next, 0, 0);
+                products(kPhases - kStep, kPhases / kStep - 1 & 1);
                 __builtin_amdgcn_sched_barrier(0);
             } else {
                 meet();
-                if (kt + 1 < hi) fetch(kt + 1, next);
+                if (kt + 1 < hi) fetch(kt + 1, next, tall);
 #pragma unroll
-                for (int p = 0; p < kPhases; ++p) read(cur, p);
+                for (int p = 0; p < kPhases; ++p) read(cur, p, p & 1);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int p = 0; p < kPhases; ++p) products(p);
+                for (int p = 0; p < kPhases; ++p) products(p, p & 1);
             }
         };
         // (The buffers are told apart, restrict, so that the compiler does not
         // make the reads of one wait for what arrives in the other.)
-        const auto round = [&](int kt, char* __restrict__ b0, char* __restrict__ b1) __attribute__((always_inline)) {
-            turn(kt, b0, b1);
-            if (kt + 1 < hi) turn(kt + 1, b1, b0);
+        const auto round = [&](int kt, char* __restrict__ b0, char* __restrict__ b1, auto tall) __attribute__((always_inline)) {
+            turn(kt, b0, b1, tall);
+            if (kt + 1 < hi) turn(kt + 1, b1, b0, tall);
         };
         sx.prepare(x, m0, a.M - m0, tokens);
         sy.prepare(y, n0, a.N - n0, tokens);
@@ -375,13 +398,21 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
             sx.look_up(int64_t(lo) * BK, a.K, tokens);
             sy.look_up(int64_t(lo) * BK, a.K, tokens);
         }
-        if (lo < hi) fetch(lo, lds0);
-        if (kAhead && lo < hi) {
-            meet();
-            if (lo + 1 < hi) fetch(lo + 1, lds1);
-            read(lds0, 0);
+        const auto run = [&](auto tall) __attribute__((always_inline)) {
+            if (lo < hi) fetch(lo, lds0, tall);
+            if (kAhead && lo < hi) {
+                meet();
+                if (lo + 1 < hi) fetch(lo + 1, lds1, tall);
+                read(lds0, 0, 0);
+            }
+            for (int kt = lo; kt < hi; kt += 2) round(kt, lds0, lds1, tall);
+        };
+        if constexpr (kShort) {
+            if (a.M - m0 > TM / 2) run(std::true_type());
+            else run(std::false_type());
+        } else {
+            run(std::true_type());
         }
-        for (int kt = lo; kt < hi; kt += 2) round(kt, lds0, lds1);
         __syncthreads();
     }
     if (from < to) {
@@ -399,8 +430,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
         const auto multiply = [&](const char* buf) __attribute__((always_inline)) {
 #pragma unroll
             for (int p = 0; p < kPhases; ++p) {
-                read(buf, p);
-                products(p);
+                read(buf, p, p & 1);
+                products(p, p & 1);
             }
         };
         load(from);
@@ -433,13 +464,14 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
     static_assert(kTurns * kWave == kPass * 16 * kCh && (kBase != kGemmDh || kTurns % 2 == 0), "");
     struct Place {
         int row, col, inside;
-        int64_t out;
+        int64_t out, m;
     };
     const auto place = [&](int p, int c) {
         const int at_c = c * kWave + static_cast<int>(lane_id());
         Place r;
         r.row = at_c / kCh, r.col = at_c % kCh * kChunk;
-        const int64_t m = m0 + wm + p * 16 + r.row, n = n0 + (Kind::kDual ? wn / 2 : wn) + r.col;
+        const int64_t m = m0 + (kShort ? acc_row(p + r.row / 16) + r.row % 16 : wm + p * 16 + r.row), n = n0 + (Kind::kDual ? wn / 2 : wn) + r.col;
+        r.m = m;
         r.inside = m < a.M ? static_cast<int>(max(min(a.N - n, int64_t(kChunk)), int64_t(0))) : 0;
         r.out = kGroups ? (kBase == kGemmDw ? group.out : group.row0 * a.N) + m * a.N + n : m * a.N + n;
         return r;
@@ -453,6 +485,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
     };
 #pragma unroll
     for (int p = 0; p < NM; p += kPass) {
+        if (kShort && m0 + acc_row(p) - acc_row(0) >= a.M) break;  // (a half that is empty)
         chunk_t gu[2][2];
         if constexpr (kBase == kGemmDh) {
             load_gu(p, 0, gu[0]);
@@ -488,7 +521,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
                     if constexpr (kGroups) {
                         // The gradients of a pair's weight (the sum over the row of h and
                         // dy Wd, of which this is 64 columns') and of its projections.
-                        const float w = pair_weight(a, tokens, m0 + wm + p * 16 + at_c.row, a.M);
+                        const float w = pair_weight(a, tokens, at_c.m, a.M);
                         float dot = 0.0f;
                         gate_backward<DT>(a.act, a.slope, v, g, u, dg, du, h);
 #pragma unroll
@@ -501,7 +534,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
                         dot += dpp_f32<0x141, 0xF>(dot);
                         if (at_c.inside <= 0) continue;
                         if (at_c.col == 0)
-                            a.dots[(group.row0 + m0 + wm + p * 16 + at_c.row) * ((a.N + WN - 1) / WN) + (n0 + wn) / WN] = dot;
+                            a.dots[(group.row0 + at_c.m) * ((a.N + WN - 1) / WN) + (n0 + wn) / WN] = dot;
                     } else {
                         gate_backward<DT>(a.act, a.slope, v, g, u, dg, du, h);
                     }
@@ -532,7 +565,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
                     if constexpr (kGroups && kBase == kGemmDown) {
                         // (Weighted before it is rounded: an intermediate value overflows
                         // only where a term of the tokens' sum does.)
-                        const float w = pair_weight(a, tokens, m0 + wm + p * 16 + at_c.row, a.M);
+                        const float w = pair_weight(a, tokens, at_c.m, a.M);
 #pragma unroll
                         for (int j = 0; j < kChunk; ++j) v[j] *= w;
                     }

@@ -97,7 +97,9 @@ TileSize plan_grouped(int dtype, GemmKind kind, bool direct, int64_t P, int64_t 
         if (cost.ends == 0.0f) continue;
         const int64_t tm = t == kTile256 ? 256 : t == kTile128 ? 128 : t == kTile64 ? 64 : 32;
         const int64_t tn = (t == kTile256 ? 256 : 128) / (kind == kGemmUp ? 2 : 1);
-        const int64_t tiles = (kind == kGemmDw ? div_up(M, tm) * E : P / tm + (busy + 1) / 2) * div_up(N, tn) * products;
+        // (The largest tile's empty half costs nothing.)
+        const int64_t empty = t == kTile256 ? (busy + 3) / 4 : (busy + 1) / 2;
+        const int64_t tiles = (kind == kGemmDw ? div_up(M, tm) * E : P / tm + empty) * div_up(N, tn) * products;
         const int64_t on_cu = div_up(tiles, kCUs);
         const float full = static_cast<float>((on_cu - 1) / 4);
         const float slow = dtype != IABN_F32 && !direct && kind >= kGemmDh ? kStridedLoads : 1.0f;
