@@ -117,8 +117,10 @@ struct Stage {
     // last ones (the results that they go into are not stored).
     uint64_t base[2];      // the tile's first element of each matrix
     uint32_t off[kLoads];  // bytes from the step's first element
-    // (k strided, GATHER: the next step's entries of the plan.)
-    uint32_t entry[KS && GATHER ? kLoads : 1];
+    // (k strided, GATHER: the next step's entries of the plan, of the lines that a
+    // wave brings at a time: two, or as many as lanes may each look up their own.)
+    static constexpr bool kPairs = kWave / kPerLine == 2;
+    uint32_t entry[KS && GATHER ? kLoads : 1][kPairs ? 2 : 1];
     template <typename Op>
     __device__ __forceinline__ void prepare(const Op& o, int64_t row0, int64_t rows, const Tokens& tokens = {}) {
 #pragma unroll
@@ -146,16 +148,36 @@ struct Stage {
         }
     }
     // GATHER with k strided: the entries that the step at k0 takes, a step ahead of its fetch.
+    template <int FROM = 0, int TO = kLoads>
     __device__ __forceinline__ void look_up(int64_t k0, int64_t K, const Tokens& tokens) {
-        if constexpr (KS && GATHER)
+        if constexpr (KS && GATHER && kPairs) {
+            // (Scalar loads: a vector load would be waited for with the fetches before it.)
+            typedef const __attribute__((address_space(4))) int32_t* scalar_t;
+            const scalar_t order = (scalar_t)(reinterpret_cast<uint64_t>(tokens.order));
+            const int first = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * 2;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i)
-                entry[i] = tokens.order[min(k0 + first_line() + i * kLineStep, K - 1)];
+            for (int i = FROM; i < TO; ++i)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) entry[i][q] = order[min(k0 + first + i * kLineStep + q, K - 1)];
+        } else if constexpr (KS && GATHER) {
+#pragma unroll
+            for (int i = FROM; i < TO; ++i)
+                entry[i][0] = tokens.order[min(k0 + first_line() + i * kLineStep, K - 1)];
+        }
+    }
+    // Bytes from the matrix to the row of a thread's i-th line.
+    __device__ __forceinline__ uint32_t gathered(int i, uint32_t row_bytes, const Tokens& tokens) const {
+        if constexpr (kPairs) {
+            const uint32_t a = tokens.of(entry[i][0]) * row_bytes, b = tokens.of(entry[i][1]) * row_bytes;
+            return lane_id() < kWave / 2 ? a : b;
+        } else {
+            return tokens.of(entry[i][0]) * row_bytes;
+        }
     }
     // K >= 0: lines of k from there on (strided) are fetched as zeros, by offsets that
     // lie outside of the buffer (row0: the tile's first column).
     static constexpr uint32_t kOutside = 0xfffff000;
-    template <int LOADS, typename Op>
+    template <int FROM, int TO, typename Op>
     __device__ __forceinline__ void fetch(const Op& o, int seg, int64_t k0, char* lds, const Tokens& tokens,
                                           int64_t K, int64_t row0) const {
 #if defined(__HIP_DEVICE_COMPILE__)  // (the host's pass does not know the buffer types)
@@ -168,7 +190,7 @@ struct Stage {
             bytes = GATHER || left > kOutside ? kOutside : static_cast<uint32_t>(left);
         }
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
+        for (int i = FROM; i < TO; ++i) {
             // (A wave's lines are of one matrix: a wave covers 8 lines or fewer.)
             const int which =
                 DUAL ? __builtin_amdgcn_readfirstlane(matrix_of(first_line() + i * kLineStep, seg)) : seg;
@@ -176,11 +198,11 @@ struct Stage {
                 reinterpret_cast<void*>((which ? base[1] : base[0]) + at), 0, static_cast<int>(bytes), 0x00027000);
             uint32_t from = off[i];
             if constexpr (KS && GATHER) {
-                from += tokens.of(entry[i]) * static_cast<uint32_t>(o.ld * static_cast<int64_t>(sizeof(T)));
+                from += gathered(i, static_cast<uint32_t>(o.ld * static_cast<int64_t>(sizeof(T))), tokens);
                 if (K >= 0 && k0 + first_line() + i * kLineStep >= K) from = kOutside;
             }
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                rsrc, (lds_t*)(lds + (wave * kWave + i * THREADS) * 16), 16, from, 0, 0, 0);
+                rsrc, (lds_t*)(lds + (wave * kWave + (i - FROM) * THREADS) * 16), 16, from, 0, 0, 0);
         }
 #endif
     }
@@ -301,22 +323,21 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
         return kShort ? g / NH * (TM / 2) + wave / WAVES_N * (WM / 2) + g % NH * 16 : wm + g * 16;
     };
     u32x4 fy[kSteps][NN], fx[2][NH];
-    // (slot: where the fragments go, of two.)
-    const auto read = [&](const char* __restrict__ buf, int phase, int slot) __attribute__((always_inline)) {
+    const auto read = [&](const char* __restrict__ buf, int phase) __attribute__((always_inline)) {
         const int s = phase / kHalves, h = phase % kHalves;
         if (h == 0)
 #pragma unroll
             for (int j = 0; j < NN; ++j) fy[s][j] = SY::frag(buf + SX::kBytes, wn + j * 16, s);
 #pragma unroll
-        for (int i = 0; i < NH; ++i) fx[slot][i] = SX::frag(buf, acc_row(h * NH + i), s);
+        for (int i = 0; i < NH; ++i) fx[phase & 1][i] = SX::frag(buf, acc_row(h * NH + i), s);
     };
-    const auto products = [&](int phase, int slot) __attribute__((always_inline)) {
+    const auto products = [&](int phase) __attribute__((always_inline)) {
         const int s = phase / kHalves, h = phase % kHalves;
 #pragma unroll
         for (int i = 0; i < NH; ++i)
 #pragma unroll
             for (int j = 0; j < NN; ++j)
-                acc[h * NH + i][j] = Mma<DT>::run(fy[s][j], fx[slot][i], acc[h * NH + i][j]);
+                acc[h * NH + i][j] = Mma<DT>::run(fy[s][j], fx[phase & 1][i], acc[h * NH + i][j]);
     };
     // Steps of K: whole ones that go straight to LDS, those of the first
     // product and then those of the second, and the others, through
@@ -336,11 +357,13 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
     const int lo = min(begin, steps), hi = min(end, steps);
     const int from = max(begin - steps, 0), to = max(end - steps, 0);
     if constexpr (DMA) {
-        const auto fetch = [&](int kt, char* buf, auto tall) __attribute__((always_inline)) {
-            const int seg = Kind::kSegs > 1 ? (kt >= whole ? 1 : 0) : z;
-            const int64_t k0 = int64_t(Kind::kSegs > 1 && seg ? kt - whole : kt) * BK;
-            sx.template fetch<tall ? SX::kLoads : SX::kLoads / 2>(x, seg, k0, buf, tokens, kFill ? a.K : -1, m0);
-            sy.template fetch<SY::kLoads>(y, seg, k0, buf + SX::kBytes, tokens, kFill ? a.K : -1, n0);
+        const auto seg_of = [&](int kt) { return Kind::kSegs > 1 ? (kt >= whole ? 1 : 0) : z; };
+        const auto k_of = [&](int kt) { return int64_t(Kind::kSegs > 1 && kt >= whole ? kt - whole : kt) * BK; };
+        const auto fetch = [&](int kt, char* buf) __attribute__((always_inline)) {
+            const int seg = seg_of(kt);
+            const int64_t k0 = k_of(kt);
+            sx.template fetch<0, SX::kLoads>(x, seg, k0, buf, tokens, kFill ? a.K : -1, m0);
+            sy.template fetch<0, SY::kLoads>(y, seg, k0, buf + SX::kBytes, tokens, kFill ? a.K : -1, n0);
             sx.look_up(k0 + BK, a.K, tokens);
             sy.look_up(k0 + BK, a.K, tokens);
         };
@@ -362,35 +385,34 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         };
-        const auto turn = [&](int kt, char* __restrict__ cur, char* __restrict__ next, auto tall) __attribute__((always_inline)) {
+        const auto turn = [&](int kt, char* __restrict__ cur, char* __restrict__ next) __attribute__((always_inline)) {
             if constexpr (kAhead) {
-                constexpr int kStep = tall ? 1 : kHalves;  // of the phases that there are
 #pragma unroll
-                for (int p = 0; p + kStep < kPhases; p += kStep) {
-                    read(cur, p + kStep, (p / kStep + 1) & 1);
-                    products(p, p / kStep & 1);
+                for (int p = 0; p + 1 < kPhases; ++p) {
+                    read(cur, p + 1);
+                    products(p);
                     __builtin_amdgcn_sched_barrier(0);  // (products stay on their side)
                 }
                 meet();
-                if (kt + 2 < hi) fetch(kt + 2, cur, tall);
-                if (kt + 1 < hi) read(next, 0, 0);
-                products(kPhases - kStep, kPhases / kStep - 1 & 1);
+                if (kt + 2 < hi) fetch(kt + 2, cur);
+                if (kt + 1 < hi) read(next, 0);
+                products(kPhases - 1);
                 __builtin_amdgcn_sched_barrier(0);
             } else {
                 meet();
-                if (kt + 1 < hi) fetch(kt + 1, next, tall);
+                if (kt + 1 < hi) fetch(kt + 1, next);
 #pragma unroll
-                for (int p = 0; p < kPhases; ++p) read(cur, p, p & 1);
+                for (int p = 0; p < kPhases; ++p) read(cur, p);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int p = 0; p < kPhases; ++p) products(p, p & 1);
+                for (int p = 0; p < kPhases; ++p) products(p);
             }
         };
         // (The buffers are told apart, restrict, so that the compiler does not
         // make the reads of one wait for what arrives in the other.)
-        const auto round = [&](int kt, char* __restrict__ b0, char* __restrict__ b1, auto tall) __attribute__((always_inline)) {
-            turn(kt, b0, b1, tall);
-            if (kt + 1 < hi) turn(kt + 1, b1, b0, tall);
+        const auto round = [&](int kt, char* __restrict__ b0, char* __restrict__ b1) __attribute__((always_inline)) {
+            turn(kt, b0, b1);
+            if (kt + 1 < hi) turn(kt + 1, b1, b0);
         };
         sx.prepare(x, m0, a.M - m0, tokens);
         sy.prepare(y, n0, a.N - n0, tokens);
@@ -398,20 +420,132 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
             sx.look_up(int64_t(lo) * BK, a.K, tokens);
             sy.look_up(int64_t(lo) * BK, a.K, tokens);
         }
-        const auto run = [&](auto tall) __attribute__((always_inline)) {
-            if (lo < hi) fetch(lo, lds0, tall);
+        if constexpr (kGroups && kAhead) {
+            // Over groups a step's tiles come from farther away (an expert's weights
+            // serve few rows): its fetch is cut in two, and the first part of the
+            // next but one starts as soon as the buffer's first part has been read,
+            // in the middle of a step.  The parts: X's first half of rows and all of Y
+            // (whose fragments are held for the second half), or where k is strided
+            // in both, the first half of k.
+            constexpr bool kByK = kBase == kGemmDw;
+            constexpr int kXPart = SX::kLoads / 2, kYPart = kByK ? SY::kLoads / 2 : SY::kLoads;
+            constexpr int kXHalf = SX::kBytes / 2, kYHalf = SY::kBytes / 2;
+            const auto first_part = [&](int kt, char* x0, char* y0) __attribute__((always_inline)) {
+                sx.template fetch<0, kXPart>(x, seg_of(kt), k_of(kt), x0, tokens, kFill ? a.K : -1, m0);
+                sy.template fetch<0, kYPart>(y, seg_of(kt), k_of(kt), y0, tokens, kFill ? a.K : -1, n0);
+            };
+            const auto second_part = [&](int kt, char* x1, char* y1) __attribute__((always_inline)) {
+                sx.template fetch<kXPart, SX::kLoads>(x, seg_of(kt), k_of(kt), x1, tokens, kFill ? a.K : -1, m0);
+                if constexpr (kByK)
+                    sy.template fetch<kYPart, SY::kLoads>(y, seg_of(kt), k_of(kt), y1, tokens, kFill ? a.K : -1, n0);
+            };
+            const auto look_up_first = [&](int kt) __attribute__((always_inline)) {
+                sx.template look_up<0, kXPart>(k_of(kt), a.K, tokens);
+                sy.template look_up<0, kYPart>(k_of(kt), a.K, tokens);
+            };
+            const auto look_up_second = [&](int kt) __attribute__((always_inline)) {
+                sx.template look_up<kXPart, SX::kLoads>(k_of(kt), a.K, tokens);
+                sy.template look_up<kYPart, SY::kLoads>(k_of(kt), a.K, tokens);
+            };
+            // Phase p: of k half s, X rows' half h; xr, yr: the parts that hold them.
+            const auto take = [&](const char* __restrict__ xr, const char* __restrict__ yr, int p) __attribute__((always_inline)) {
+                const int h = kByK ? p % 2 : p / 2, s = kByK ? p / 2 : p % 2;
+                if (h == 0)
+#pragma unroll
+                    for (int j = 0; j < NN; ++j) fy[s][j] = SY::frag(yr, wn + j * 16, kByK ? 0 : s);
+#pragma unroll
+                for (int i = 0; i < NH; ++i) fx[p & 1][i] = SX::frag(xr, acc_row(kByK ? h * NH + i : i), kByK ? 0 : s);
+            };
+            const auto multiply = [&](int p) __attribute__((always_inline)) {
+                const int h = kByK ? p % 2 : p / 2, s = kByK ? p / 2 : p % 2;
+#pragma unroll
+                for (int i = 0; i < NH; ++i)
+#pragma unroll
+                    for (int j = 0; j < NN; ++j)
+                        acc[h * NH + i][j] = Mma<DT>::run(fy[s][j], fx[p & 1][i], acc[h * NH + i][j]);
+                __builtin_amdgcn_sched_barrier(0);  // (products stay on their side)
+            };
+            // All waves: their reads of LDS have ended, and all but the last `left`
+            // fetches have arrived.
+            const auto meet_but = [](auto left) __attribute__((always_inline)) {
+                __builtin_amdgcn_s_waitcnt(0x0070 | (left & 15) | (left >> 4 << 14));
+                asm volatile("" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+            };
+            using std::integral_constant;
+            constexpr integral_constant<int, 63> kAny;
+            constexpr integral_constant<int, kXPart + kYPart> kFirst;
+            constexpr integral_constant<int, SX::kLoads + SY::kLoads> kStepLoads;
+            constexpr integral_constant<int, 0> kNone;
+            const auto split_turn = [&](int kt, char* __restrict__ x0, char* __restrict__ x1, char* __restrict__ y0,
+                                        char* __restrict__ y1, char* __restrict__ next_x, char* __restrict__ next_y,
+                                        auto tall) __attribute__((always_inline)) {
+                const bool more = kt + 2 < hi;
+                take(x0, y0, 1);
+                multiply(0);
+                if constexpr (tall) {
+                    meet_but(kAny);
+                    if (more) {
+                        first_part(kt + 2, x0, y0);
+                        // (Here, so that the wait at the next barrier is theirs too.)
+                        look_up_second(kt + 2);
+                        look_up_first(kt + 3);
+                    }
+                    take(x1, y1, 2);
+                    multiply(1);
+                    take(x1, y1, 3);
+                    multiply(2);
+                    if (more) meet_but(kFirst);
+                    else meet_but(kNone);
+                    if (more) second_part(kt + 2, x1, y1);
+                } else {
+                    meet_but(kNone);
+                    if (more) first_part(kt + 2, x0, y0);
+                }
+                if (kt + 1 < hi) take(next_x, next_y, 0);
+                multiply(tall ? 3 : 1);
+            };
+            const auto split_round = [&](int kt, char* __restrict__ x0, char* __restrict__ x1, char* __restrict__ y0,
+                                         char* __restrict__ y1, char* __restrict__ x2, char* __restrict__ x3,
+                                         char* __restrict__ y2, char* __restrict__ y3, auto tall) __attribute__((always_inline)) {
+                split_turn(kt, x0, x1, y0, y1, x2, y2, tall);
+                if (kt + 1 < hi) split_turn(kt + 1, x2, x3, y2, y3, x0, y0, tall);
+            };
+            const auto run = [&](auto tall) __attribute__((always_inline)) {
+                char *const y0 = lds0 + SX::kBytes, *const y1 = lds1 + SX::kBytes;
+                if (lo >= hi) return;
+                first_part(lo, lds0, y0);
+                if (tall) second_part(lo, lds0 + kXHalf, y0 + kYHalf);
+                if (lo + 1 < hi) {
+                    look_up_first(lo + 1);
+                    look_up_second(lo + 1);
+                    first_part(lo + 1, lds1, y1);
+                    if (tall) second_part(lo + 1, lds1 + kXHalf, y1 + kYHalf);
+                    look_up_first(lo + 2);
+                    if (tall) meet_but(kStepLoads);
+                    else meet_but(kFirst);
+                } else {
+                    meet_but(kNone);
+                }
+                take(lds0, y0, 0);
+                for (int kt = lo; kt < hi; kt += 2)
+                    split_round(kt, lds0, lds0 + kXHalf, y0, y0 + kYHalf, lds1, lds1 + kXHalf, y1, y1 + kYHalf, tall);
+            };
+            if constexpr (kShort) {
+                if (a.M - m0 > TM / 2) run(std::true_type());
+                else run(std::false_type());
+            } else {
+                run(std::true_type());
+            }
+        } else {
+            if (lo < hi) fetch(lo, lds0);
             if (kAhead && lo < hi) {
                 meet();
-                if (lo + 1 < hi) fetch(lo + 1, lds1, tall);
-                read(lds0, 0, 0);
+                if (lo + 1 < hi) fetch(lo + 1, lds1);
+                read(lds0, 0);
             }
-            for (int kt = lo; kt < hi; kt += 2) round(kt, lds0, lds1, tall);
-        };
-        if constexpr (kShort) {
-            if (a.M - m0 > TM / 2) run(std::true_type());
-            else run(std::false_type());
-        } else {
-            run(std::true_type());
+            for (int kt = lo; kt < hi; kt += 2) round(kt, lds0, lds1);
         }
         __syncthreads();
     }
@@ -430,8 +564,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
         const auto multiply = [&](const char* buf) __attribute__((always_inline)) {
 #pragma unroll
             for (int p = 0; p < kPhases; ++p) {
-                read(buf, p, p & 1);
-                products(p, p & 1);
+                read(buf, p);
+                products(p);
             }
         };
         load(from);
