@@ -13,30 +13,34 @@ uint32_t blocks_for(int64_t want) { return static_cast<uint32_t>(want < 1 << 22 
 // by the terms' traffic.
 template <int DT, bool FEW>
 __global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a, int chunks) {
-    constexpr int TERM = FEW ? IABN_F32 : DT;
+    constexpr int TERM = FEW ? IABN_F32 : DT, kSlots = 4;
     for (int64_t c = int64_t(blockIdx.x) * kThreads + threadIdx.x; c < a.M * chunks; c += int64_t(gridDim.x) * kThreads) {
         const int64_t t = c / chunks, col = (c - t * chunks) * kChunk;
         const int n = static_cast<int>(min(a.C - col, int64_t(kChunk)));
         float sum[kChunk] = {};
-        for (int s = 0; s < a.k; ++s) {
-            const uint32_t p = static_cast<uint32_t>(a.place[t * a.k + s]);
-            if (p >= static_cast<uint32_t>(a.P)) continue;
-            if constexpr (FEW) {
-                const float w = a.weights[t * a.k + s];
-                float term[kChunk] = {};
-                for (int q = 0; q < a.splits; ++q) {
+        for (int s0 = 0; s0 < a.k; s0 += kSlots) {
+            // The places, then the terms of several slots on their way together.
+            uint32_t p[kSlots];
+            float w[kSlots];
+            typename ChunkOf<TERM>::vec term[kSlots];
+#pragma unroll
+            for (int q = 0; q < kSlots; ++q) {
+                p[q] = s0 + q < a.k ? static_cast<uint32_t>(a.place[t * a.k + s0 + q]) : 0xFFFFFFFFu;
+                w[q] = FEW && s0 + q < a.k ? a.weights[t * a.k + s0 + q] : 1.0f;
+            }
+            for (int split = 0; split < (FEW ? a.splits : 1); ++split) {
+#pragma unroll
+                for (int q = 0; q < kSlots; ++q)
+                    term[q] = load_chunk<TERM, FEW ? kCached : kStream>(
+                        a.terms, (int64_t(split) * a.P + p[q]) * a.C + col, p[q] < static_cast<uint32_t>(a.P) ? n : 0);
+#pragma unroll
+                for (int q = 0; q < kSlots; ++q) {
                     float v[kChunk];
-                    widen<TERM>(load_chunk<TERM, kCached>(a.terms, (int64_t(q) * a.P + p) * a.C + col, n), v);
+                    widen<TERM>(term[q], v);
 #pragma unroll
-                    for (int j = 0; j < kChunk; ++j) term[j] += v[j];
+                    for (int j = 0; j < kChunk; ++j)
+                        sum[j] = p[q] < static_cast<uint32_t>(a.P) ? FEW ? fmaf(w[q], v[j], sum[j]) : sum[j] + v[j] : sum[j];
                 }
-#pragma unroll
-                for (int j = 0; j < kChunk; ++j) sum[j] = fmaf(w, term[j], sum[j]);
-            } else {
-                float v[kChunk];
-                widen<TERM>(load_chunk<TERM, kStream>(a.terms, p * a.C + col, n), v);
-#pragma unroll
-                for (int j = 0; j < kChunk; ++j) sum[j] += v[j];
             }
         }
         store_chunk<DT, kCached>(a.y, t * a.C + col, n, sum);

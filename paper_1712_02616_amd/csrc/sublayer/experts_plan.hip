@@ -29,16 +29,28 @@ __device__ __forceinline__ void span_of(const PlanArgs& a, int wave, int& from, 
     to = static_cast<int>(min(begin + (wave + 1) * per, end));
 }
 
+// Counts the experts of a wave's pairs in LDS; a lane has eight on their way.
+__device__ __forceinline__ void count_span(const PlanArgs& a, int32_t* counts, int from, int to) {
+    for (int base = from; base < to; base += 8 * kWave) {
+        int e[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int i = base + q * kWave + static_cast<int>(lane_id());
+            e[q] = i < to ? a.experts[i] : -1;
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (routed(e[q], a.E)) atomicAdd(&counts[e[q]], 1);
+    }
+}
+
 __global__ __launch_bounds__(kPlanThreads) void plan_count_kernel(PlanArgs a) {
     extern __shared__ int32_t counts[];  // [E]
     for (int e = threadIdx.x; e < a.E; e += kPlanThreads) counts[e] = 0;
     __syncthreads();
     int from, to;
     span_of(a, threadIdx.x / kWave, from, to);
-    for (int i = from + static_cast<int>(lane_id()); i < to; i += kWave) {
-        const int e = a.experts[i];
-        if (routed(e, a.E)) atomicAdd(&counts[e], 1);
-    }
+    count_span(a, counts, from, to);
     __syncthreads();
     for (int e = threadIdx.x; e < a.E; e += kPlanThreads)
         a.counts[int64_t(blockIdx.x) * a.E + e] = counts[e];
@@ -65,10 +77,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     __syncthreads();
     int from, to;
     span_of(a, wave, from, to);
-    for (int i = from + static_cast<int>(lane_id()); i < to; i += kWave) {
-        const int e = a.experts[i];
-        if (routed(e, a.E)) atomicAdd(&own[e], 1);
-    }
+    count_span(a, own, from, to);
     __syncthreads();
     // Each thread has `each` consecutive experts.
     constexpr int kEach = kMaxExperts / kPlanThreads;
@@ -82,10 +91,16 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
         if (a.blocks == 1) {
             for (int w = 0; w < kPlanWaves; ++w) all[j] += next[w * a.E + e];
         } else {
-            for (int b = 0; b < a.blocks; ++b) {
-                const int n = a.counts[int64_t(b) * a.E + e];
-                before[j] += b < static_cast<int>(blockIdx.x) ? n : 0;
-                all[j] += n;
+            // (Sixteen loads on their way at a time.)
+            for (int b0 = 0; b0 < a.blocks; b0 += 16) {
+                int n[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) n[i] = b0 + i < a.blocks ? a.counts[int64_t(b0 + i) * a.E + e] : 0;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    before[j] += b0 + i < static_cast<int>(blockIdx.x) ? n[i] : 0;
+                    all[j] += n[i];
+                }
             }
         }
         sum += all[j];
@@ -110,9 +125,11 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
         if (blockIdx.x == 0 && e == a.E - 1) a.offsets[a.E] = at;
     }
     __syncthreads();
+    int ahead = from + static_cast<int>(lane_id()) < to ? a.experts[from + static_cast<int>(lane_id())] : -1;
     for (int base = from; base < to; base += kWave) {  // (uniform over the wave)
         const int i = base + static_cast<int>(lane_id());
-        int e = i < to ? a.experts[i] : -1;
+        const int e = ahead;
+        ahead = i + kWave < to ? a.experts[i + kWave] : -1;
         const bool is = routed(e, a.E);
         uint64_t same = __ballot(is);
         for (int bit = 1; bit < a.E; bit *= 2) {

@@ -9,8 +9,11 @@
 // ordered as unsigned integers (the float's bits, those of negative ones turned
 // over), 0 for what may not be chosen, the largest for a NaN.  Without a bias the
 // order of the scores is that of the logits, which is exact in 32 bits.  With one
-// (or with groups), scores next to each other decide, so they are formed and
-// compared in 64 bits.
+// (or with groups), scores next to each other decide: they are formed in 32 bits
+// with a bound of their error, and where two that decide are closer than that, the
+// wave forms and compares them in 64 bits.
+#include <type_traits>
+
 #include "routed.h"
 
 namespace iabn_impl {
@@ -140,115 +143,81 @@ __device__ __forceinline__ void wave_fence() {
 }
 
 // The groups that a row keeps, a bit each.  t: the scores in LDS, -inf for what
-// may not be chosen; gs: a place for the groups' scores.
-template <int L>
-__device__ __forceinline__ uint64_t kept_groups(const RouteArgs& a, const double* t, double* gs, int lane) {
+// may not be chosen; gs: a place for the groups' scores.  The scores are off by at
+// most `tol`, and sums of two by 2^-22 of themselves besides: `sure` turns false
+// where that could change which groups are kept.
+template <int L, typename S>
+__device__ __forceinline__ uint64_t kept_groups(const RouteArgs& a, const S* t, S* gs, int lane, S tol, bool& sure) {
     // A group belongs to `per_group` lanes, which look through it in turn.
     const int per_group = L / a.groups, g = lane / per_group, part = lane - g * per_group;
-    double top1 = -kInf, top2 = -kInf;
+    const S none = -kInf;
+    S top1 = none, top2 = none;
+    const auto larger = [](S x, S y) { return x > y ? x : y; };
+    const auto smaller = [](S x, S y) { return x < y ? x : y; };
     if (g < a.groups)
         for (int i = part; i < a.per; i += per_group) {
-            double v = t[g * a.per + i];
+            S v = t[g * a.per + i];
             if (v != v) v = kInf;
-            top2 = fmax(top2, fmin(top1, v));
-            top1 = fmax(top1, v);
+            top2 = larger(top2, smaller(top1, v));
+            top1 = larger(top1, v);
         }
     for (int d = 1; d < per_group; d *= 2) {
-        const double o1 = __shfl_down(top1, d, L), o2 = __shfl_down(top2, d, L);
+        const S o1 = __shfl_down(top1, d, L), o2 = __shfl_down(top2, d, L);
         if (part + d < per_group) {
-            top2 = fmax(fmin(top1, o1), fmax(top2, o2));
-            top1 = fmax(top1, o1);
+            top2 = larger(smaller(top1, o1), larger(top2, o2));
+            top1 = larger(top1, o1);
         }
     }
-    if (a.group_top == 2 && top2 > -kInf) top1 += top2;
+    if (a.group_top == 2 && top2 > none) top1 += top2;
     if (g < a.groups && part == 0) gs[g] = top1;
     wave_fence();
-    bool keep = false;
+    bool keep = false, clear = true;
     if (lane < a.groups) {
-        const double mine = gs[lane];
-        int above = 0;
-        for (int i = 0; i < a.groups; ++i) above += gs[i] > mine || (gs[i] == mine && i < lane);
-        keep = above < a.kept && mine > -kInf;
+        const S mine = gs[lane];
+        // How many are above, and how many surely are, and may be.
+        int above = 0, surely = 0, maybe = 0;
+        for (int i = 0; i < a.groups; ++i) {
+            const S other = gs[i];
+            const bool same = i == lane;
+            above += other > mine || (other == mine && i < lane);
+            if constexpr (sizeof(S) == 4) {
+                const S far = 2.0f * tol + 2.4e-7f * (fabsf(mine) + fabsf(other));
+                surely += !same && other - mine > far;
+                maybe += !same && other - mine > -far;
+            }
+        }
+        keep = above < a.kept && mine > none;
+        if constexpr (sizeof(S) == 4) clear = mine == none || maybe < a.kept || surely >= a.kept;
     }
+    sure = sure && __ballot(!clear) == 0;
     const uint64_t all = __ballot(keep);
     if constexpr (L == 64) return all;
     return all >> (lane_id() / L * L) & ((uint64_t(1) << L) - 1);
 }
 
-template <int DT, int L, int V, bool WIDE>
-__global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
-    const int lane = threadIdx.x % L, first = lane * V;
-    const int64_t own = int64_t(blockIdx.x) * (kThreads / L) + threadIdx.x / L;
-    const bool there = own < a.M;
-    const int64_t row = there ? own : a.M - 1;  // (every lane stays for the maxima)
-
-    float v[V];
-    load_logits<DT, V>(a.logits, row, a.E, first, v);
-    const float high = a.sigmoid ? 0.0f : row_maxf<L>(largest(v));
-
-    // What is ordered: `key`, or with WIDE its upper half and `low`.
-    uint32_t key[V], low[WIDE ? V : 1];
-    float total = 0.0f;  // of the softmax
-    if constexpr (WIDE) {
-        double s[V], sum = 0.0;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const double l = v[j];
-            s[j] = a.sigmoid ? 1.0 / (1.0 + exp(-l)) : exp(l - static_cast<double>(high));
-            sum += s[j];
-        }
-        if (!a.sigmoid) {
-            sum = row_add64<L>(sum);
-#pragma unroll
-            for (int j = 0; j < V; ++j) s[j] /= sum;
-            total = static_cast<float>(sum);
-        }
-        uint64_t groups = ~uint64_t(0);
-        bool may[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            may[j] = v[j] != -kInf;
-            if (a.bias && may[j]) {
-                const float b = a.bias[first + j];
-                may[j] = b != -kInf;
-                s[j] += b;
-            }
-        }
-        if (a.kept < a.groups) {
-            extern __shared__ double scores[];  // [rows][E], [rows][groups]
-            double* const t = scores + threadIdx.x / L * a.E;
-            double* const gs = scores + kThreads / L * a.E + threadIdx.x / L * a.groups;
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (first + j < a.E) t[first + j] = may[j] ? s[j] : -kInf;
-            wave_fence();
-            groups = kept_groups<L>(a, t, gs, lane);
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int g = static_cast<int>(static_cast<uint32_t>(first + j) * a.per_magic >> 20);
-            const uint64_t o = may[j] && (a.kept >= a.groups || (groups >> g & 1)) ? order64(a.bias ? s[j] : v[j]) : 0;
-            key[j] = static_cast<uint32_t>(o >> 32);
-            low[j] = static_cast<uint32_t>(o);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) key[j] = v[j] == -kInf ? 0 : order32(v[j]);
-        if (!a.sigmoid && !a.renormalise) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) total += exp_from(v[j], high);
-            total = row_add<L>(total);
-        }
-    }
-
-    // The choices, one after the other; lane i keeps the i-th.
-    int mine = -1;
+// What a row chose: lane i has the i-th expert (-1: none) and its logit.
+struct Choice {
+    int expert = -1;
     float logit = 0.0f;
-    for (int i = 0; i < a.k; ++i) {
-        uint32_t best = key[0], best_low = WIDE ? low[0] : 0;
+};
+
+// The k highest keys, one after the other (64-bit ones: `low` is their lower half).
+// SCORES: the keys are scores, off by tol + 2^-23 of themselves; one choice more is
+// looked at, and `sure` turns false where two that follow each other are too close.
+// LOGITS: the keys are the logits.
+enum KeyKind { kLogitKeys, kScoreKeys, kWideKeys };
+template <int L, int V, KeyKind KEYS>
+__device__ __forceinline__ Choice choose(uint32_t (&key)[V], uint32_t (&low)[KEYS == kWideKeys ? V : 1], int k, int lane,
+                                         float tol, bool& sure) {
+    constexpr bool kWide = KEYS == kWideKeys;
+    const int first = lane * V;
+    Choice c;
+    float before = kInf;
+    for (int i = 0; i < (KEYS == kScoreKeys ? k + 1 : k); ++i) {
+        uint32_t best = key[0], best_low = kWide ? low[0] : 0;
 #pragma unroll
         for (int j = 1; j < V; ++j) {
-            if constexpr (WIDE) {
+            if constexpr (kWide) {
                 const bool more = key[j] > best || (key[j] == best && low[j] > best_low);
                 best = more ? key[j] : best;
                 best_low = more ? low[j] : best_low;
@@ -257,28 +226,137 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
             }
         }
         const uint32_t top = row_max<L>(best);
-        const uint32_t top_low = WIDE ? row_max<L>(best == top ? best_low : 0) : 0;
-        uint32_t at = 0xFFFFFFFFu;
-        float l = 0.0f;
-#pragma unroll
-        for (int j = V - 1; j >= 0; --j) {
-            const bool is = key[j] == top && (!WIDE || low[j] == top_low);
-            at = is ? first + j : at;
-            l = is ? v[j] : l;
+        const uint32_t top_low = kWide ? row_max<L>(best == top ? best_low : 0) : 0;
+        const float value = __builtin_bit_cast(float, top >> 31 ? top & 0x7FFFFFFFu : ~top);
+        if constexpr (KEYS == kScoreKeys) {
+            // (A NaN is never far from another.)
+            sure = sure && (top == 0 || before - value > 2.0f * tol + 2.4e-7f * fabsf(value));
+            before = value;
+            if (i == k) break;
         }
+        uint32_t at = 0xFFFFFFFFu;
+#pragma unroll
+        for (int j = V - 1; j >= 0; --j)
+            at = key[j] == top && (!kWide || low[j] == top_low) ? first + j : at;
         const uint32_t e = row_min<L>(at);
-        // (One lane has it.)
-        l = __builtin_bit_cast(float, row_max<L>(at == e ? __builtin_bit_cast(uint32_t, l) : 0));
+        const uint32_t mine = e - first;
 #pragma unroll
-        for (int j = 0; j < V; ++j) key[j] = static_cast<uint32_t>(first + j) == e ? 0 : key[j];
-        if constexpr (WIDE)
+        for (int j = 0; j < V; ++j) key[j] = mine == static_cast<uint32_t>(j) ? 0 : key[j];
+        if constexpr (kWide)
 #pragma unroll
-            for (int j = 0; j < V; ++j) low[j] = static_cast<uint32_t>(first + j) == e ? 0 : low[j];
+            for (int j = 0; j < V; ++j) low[j] = mine == static_cast<uint32_t>(j) ? 0 : low[j];
         if (lane == i && top != 0) {
-            mine = static_cast<int>(e);
-            logit = l;
+            c.expert = static_cast<int>(e);
+            if constexpr (KEYS == kLogitKeys) c.logit = top == 0xFFFFFFFFu ? __builtin_nanf("") : value;
         }
     }
+    return c;
+}
+
+template <int DT, int L, int V, bool SCORED>
+__global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
+    using T = typename Elem<DT>::T;
+    const int lane = threadIdx.x % L, first = lane * V;
+    const int64_t own = int64_t(blockIdx.x) * (kThreads / L) + threadIdx.x / L;
+    const bool there = own < a.M;
+    const int64_t row = there ? own : a.M - 1;  // (every lane stays for the maxima)
+
+    float v[V];
+    load_logits<DT, V>(a.logits, row, a.E, first, v);
+    const float high = a.sigmoid ? 0.0f : row_maxf<L>(largest(v));
+    float total = 0.0f;  // of the softmax
+    if (!a.sigmoid && !a.renormalise) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) total += exp_from(v[j], high);
+        total = row_add<L>(total);
+    }
+
+    Choice c;
+    bool sure = true;
+    if constexpr (SCORED) {
+        extern __shared__ double scores[];  // [rows][E], [rows][groups], of either type
+        const bool grouped = a.kept < a.groups;
+        float bias[V];
+        bool may[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            bias[j] = a.bias && first + j < a.E ? a.bias[first + j] : 0.0f;
+            may[j] = v[j] != -kInf && bias[j] != -kInf;
+        }
+        // The keys of scores s, of what may be chosen and is in a kept group.
+        const auto in_groups = [&](const auto& s, auto tol) {
+            using S = std::remove_cv_t<decltype(tol)>;
+            if (!grouped) return ~uint64_t(0);
+            // (A row's place is the same for both types: other waves have theirs in use.)
+            S* const t = reinterpret_cast<S*>(scores + threadIdx.x / L * a.E);
+            S* const gs = reinterpret_cast<S*>(scores + kThreads / L * a.E + threadIdx.x / L * a.groups);
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (first + j < a.E) t[first + j] = may[j] ? s[j] : static_cast<S>(-kInf);
+            wave_fence();
+            return kept_groups<L, S>(a, t, gs, lane, tol, sure);
+        };
+        const auto in_kept = [&](uint64_t groups, int j) {
+            const int g = static_cast<int>(static_cast<uint32_t>(first + j) * a.per_magic >> 20);
+            return may[j] && (!grouped || (groups >> g & 1));
+        };
+        uint32_t key[V];
+        {
+            // In 32 bits.  A sigmoid is off by less than 2^-22, a term of the softmax by
+            // less than 2^-18 of the largest (its sum by 22 roundings).
+            float s[V], sum = 0.0f, tol = 0x1p-21f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                s[j] = __expf(a.sigmoid ? -v[j] : v[j] - high);
+                if (a.sigmoid) s[j] = __builtin_amdgcn_rcpf(1.0f + s[j]);
+                sum += s[j];
+            }
+            if (!a.sigmoid) {
+                const float scale = 1.0f / row_add<L>(sum);
+                tol = scale * 0x1p-18f;
+#pragma unroll
+                for (int j = 0; j < V; ++j) s[j] *= scale;
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) s[j] += bias[j];
+            const uint64_t groups = in_groups(s, tol);
+#pragma unroll
+            for (int j = 0; j < V; ++j) key[j] = in_kept(groups, j) ? order32(a.bias ? s[j] : v[j]) : 0;
+            uint32_t none[1];
+            if (a.bias) c = choose<L, V, kScoreKeys>(key, none, a.k, lane, tol, sure);
+            else c = choose<L, V, kLogitKeys>(key, none, a.k, lane, tol, sure);
+        }
+        if (__ballot(!sure) != 0) {
+            double s[V], sum = 0.0;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const double l = v[j];
+                s[j] = a.sigmoid ? 1.0 / (1.0 + exp(-l)) : exp(l - static_cast<double>(high));
+                sum += s[j];
+            }
+            if (!a.sigmoid) sum = row_add64<L>(sum);
+#pragma unroll
+            for (int j = 0; j < V; ++j) s[j] = (a.sigmoid ? s[j] : s[j] / sum) + bias[j];
+            wave_fence();
+            const uint64_t groups = in_groups(s, 0.0);
+            uint32_t low[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const uint64_t o = in_kept(groups, j) ? order64(a.bias ? s[j] : v[j]) : 0;
+                key[j] = static_cast<uint32_t>(o >> 32);
+                low[j] = static_cast<uint32_t>(o);
+            }
+            c = choose<L, V, kWideKeys>(key, low, a.k, lane, 0.0f, sure);
+        }
+        if (c.expert >= 0) c.logit = static_cast<float>(static_cast<const T*>(a.logits)[row * a.E + c.expert]);
+    } else {
+        uint32_t key[V], none[1];
+#pragma unroll
+        for (int j = 0; j < V; ++j) key[j] = v[j] == -kInf ? 0 : order32(v[j]);
+        c = choose<L, V, kLogitKeys>(key, none, a.k, lane, 0.0f, sure);
+    }
+    const int mine = c.expert;
+    const float logit = c.logit;
 
     float w = 0.0f;
     if (a.renormalise) {
