@@ -10,9 +10,11 @@
 // over), 0 for what may not be chosen, the largest for a NaN.  Without a bias the
 // order of the scores is that of the logits, which is exact in 32 bits.  With one
 // (or with groups), scores next to each other decide: they are formed in 32 bits
-// with a bound of their error, and where two that decide are closer than that, the
-// wave forms and compares them in 64 bits.
+// with a bound of their error, and where two that decide are closer than that, those
+// few are formed and compared in 64 bits.  (That is what one wave in a hundred does;
+// all scores in 64 bits for it (16384, 256) bf16, 8 of 256: 29 us instead of PATH.)
 #include <type_traits>
+#include <utility>
 
 #include "routed.h"
 
@@ -83,6 +85,23 @@ __device__ __forceinline__ double row_add64(double v) {
     return v;
 }
 
+// A value of the row's lane I, in all of its lanes (of 64: the wave's).
+constexpr int kRowLanes = 16;
+template <int L, int I>
+__device__ __forceinline__ uint32_t from_lane(uint32_t v) {
+    if constexpr (L == 16) return dpp_u32<0x150 + I>(v);
+    else return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), I));
+}
+// fn(i) for the choices i < k, the first 16 of them, i a constant.
+template <int L, typename Fn, int... I>
+__device__ __forceinline__ void each_choice(int k, Fn fn, std::integer_sequence<int, I...>) {
+    ((I < k ? fn(std::integral_constant<int, I>()) : void()), ...);
+}
+template <int L, typename Fn>
+__device__ __forceinline__ void each_choice(int k, Fn fn) {
+    each_choice<L>(k, fn, std::make_integer_sequence<int, kRowLanes>());
+}
+
 // ---------------------------------------------------------------- scores
 
 // Bits that are ordered as the value (-0 as 0, a NaN above all); 0 is below all.
@@ -107,11 +126,11 @@ __device__ __forceinline__ float exp_from(float v, float m) {
 // 1/(1 + exp(-v)).
 __device__ __forceinline__ float sigmoid(float v) { return 1.0f / (1.0f + expf(-v)); }
 
-// The row's logits, V of each lane; -inf past the last expert.
+// A row's values of E experts, V of each lane; -inf past the last one.
 template <int DT, int V>
-__device__ __forceinline__ void load_logits(const void* logits, int64_t row, int E, int first, float (&v)[V]) {
+__device__ __forceinline__ void load_row(const void* rows, int64_t row, int E, int first, float (&v)[V]) {
     using T = typename Elem<DT>::T;
-    const T* p = static_cast<const T*>(logits) + row * E + first;
+    const T* p = static_cast<const T*>(rows) + row * E + first;
     typedef T vec __attribute__((ext_vector_type(V)));
     typedef T mem __attribute__((ext_vector_type(V), aligned(sizeof(T))));
     if (first + V <= E) {
@@ -143,9 +162,9 @@ __device__ __forceinline__ void wave_fence() {
 }
 
 // The groups that a row keeps, a bit each.  t: the scores in LDS, -inf for what
-// may not be chosen; gs: a place for the groups' scores.  The scores are off by at
-// most `tol`, and sums of two by 2^-22 of themselves besides: `sure` turns false
-// where that could change which groups are kept.
+// may not be chosen; gs: a place for the groups' scores.  32-bit scores are off by
+// at most `tol` and their own roundings, a group's by twice that: `sure` turns false
+// where it could change which groups are kept.
 template <int L, typename S>
 __device__ __forceinline__ uint64_t kept_groups(const RouteArgs& a, const S* t, S* gs, int lane, S tol, bool& sure) {
     // A group belongs to `per_group` lanes, which look through it in turn.
@@ -154,12 +173,19 @@ __device__ __forceinline__ uint64_t kept_groups(const RouteArgs& a, const S* t, 
     S top1 = none, top2 = none;
     const auto larger = [](S x, S y) { return x > y ? x : y; };
     const auto smaller = [](S x, S y) { return x < y ? x : y; };
+    // (Eight reads on their way at a time; past the group's end, its last one again.)
+    constexpr int kReads = 8;
     if (g < a.groups)
-        for (int i = part; i < a.per; i += per_group) {
-            S v = t[g * a.per + i];
-            if (v != v) v = kInf;
-            top2 = larger(top2, smaller(top1, v));
-            top1 = larger(top1, v);
+        for (int i = part; i < a.per; i += kReads * per_group) {
+            S v[kReads];
+#pragma unroll
+            for (int q = 0; q < kReads; ++q) v[q] = t[g * a.per + min(i + q * per_group, a.per - 1)];
+#pragma unroll
+            for (int q = 0; q < kReads; ++q) {
+                const S x = i + q * per_group >= a.per ? none : v[q] != v[q] ? static_cast<S>(kInf) : v[q];
+                top2 = larger(top2, smaller(top1, x));
+                top1 = larger(top1, x);
+            }
         }
     for (int d = 1; d < per_group; d *= 2) {
         const S o1 = __shfl_down(top1, d, L), o2 = __shfl_down(top2, d, L);
@@ -176,14 +202,21 @@ __device__ __forceinline__ uint64_t kept_groups(const RouteArgs& a, const S* t, 
         const S mine = gs[lane];
         // How many are above, and how many surely are, and may be.
         int above = 0, surely = 0, maybe = 0;
-        for (int i = 0; i < a.groups; ++i) {
-            const S other = gs[i];
-            const bool same = i == lane;
-            above += other > mine || (other == mine && i < lane);
-            if constexpr (sizeof(S) == 4) {
-                const S far = 2.0f * tol + 2.4e-7f * (fabsf(mine) + fabsf(other));
-                surely += !same && other - mine > far;
-                maybe += !same && other - mine > -far;
+        for (int i0 = 0; i0 < a.groups; i0 += kReads) {
+            S others[kReads];
+#pragma unroll
+            for (int q = 0; q < kReads; ++q) others[q] = gs[min(i0 + q, a.groups - 1)];
+#pragma unroll
+            for (int q = 0; q < kReads; ++q) {
+                const int i = i0 + q;
+                const S other = others[q];
+                const bool is = i < a.groups && i != lane;
+                above += is && (other > mine || (other == mine && i < lane));
+                if constexpr (sizeof(S) == 4) {
+                    const S far = 4.0f * tol + 0x1p-22f * (fabsf(mine) + fabsf(other));
+                    surely += is && other - mine > far;
+                    maybe += is && other - mine > -far;
+                }
             }
         }
         keep = above < a.kept && mine > none;
@@ -202,18 +235,23 @@ struct Choice {
 };
 
 // The k highest keys, one after the other (64-bit ones: `low` is their lower half).
-// SCORES: the keys are scores, off by tol + 2^-23 of themselves; one choice more is
-// looked at, and `sure` turns false where two that follow each other are too close.
-// LOGITS: the keys are the logits.
+// kScoreKeys: they are scores off by at most tol.  Then more are taken until the
+// next one is surely below the k-th, and `close` says how it went: kApart, no two that
+// follow each other too close; kClose, the right ones are among the first
+// `taken`; kLost, there are more than lanes.  kLogitKeys: the keys are the logits.
 enum KeyKind { kLogitKeys, kScoreKeys, kWideKeys };
+enum Closeness { kApart, kClose, kLost };
 template <int L, int V, KeyKind KEYS>
 __device__ __forceinline__ Choice choose(uint32_t (&key)[V], uint32_t (&low)[KEYS == kWideKeys ? V : 1], int k, int lane,
-                                         float tol, bool& sure) {
+                                         float tol, int& taken, Closeness& close) {
     constexpr bool kWide = KEYS == kWideKeys;
     const int first = lane * V;
     Choice c;
     float before = kInf;
-    for (int i = 0; i < (KEYS == kScoreKeys ? k + 1 : k); ++i) {
+    bool apart = true, closed = false;
+    close = kApart;
+    for (taken = 0; KEYS == kScoreKeys || taken < k; ++taken) {
+        const int i = taken;
         uint32_t best = key[0], best_low = kWide ? low[0] : 0;
 #pragma unroll
         for (int j = 1; j < V; ++j) {
@@ -229,10 +267,19 @@ __device__ __forceinline__ Choice choose(uint32_t (&key)[V], uint32_t (&low)[KEY
         const uint32_t top_low = kWide ? row_max<L>(best == top ? best_low : 0) : 0;
         const float value = __builtin_bit_cast(float, top >> 31 ? top & 0x7FFFFFFFu : ~top);
         if constexpr (KEYS == kScoreKeys) {
-            // (A NaN is never far from another.)
-            sure = sure && (top == 0 || before - value > 2.0f * tol + 2.4e-7f * fabsf(value));
+            // (The scores' own roundings: 2^-24 of them.  A NaN is never far from another.)
+            const bool far = top == 0 || before - value > 2.0f * tol + 0x1p-24f * (fabsf(before) + fabsf(value)) || i == 0;
             before = value;
-            if (i == k) break;
+            apart = apart && (far || closed);
+            closed = closed || (i >= k && far);
+            if (i >= k && __ballot(!closed) == 0) {
+                close = __ballot(!apart) == 0 ? kApart : kClose;
+                break;
+            }
+            if (i == L) {
+                close = kLost;
+                break;
+            }
         }
         uint32_t at = 0xFFFFFFFFu;
 #pragma unroll
@@ -253,6 +300,24 @@ __device__ __forceinline__ Choice choose(uint32_t (&key)[V], uint32_t (&low)[KEY
     return c;
 }
 
+// Lane i's choice of `taken`, with its 64-bit key, goes to the lane of its rank.
+template <int L>
+__device__ __forceinline__ int by_rank(int expert, uint64_t key, int taken, int lane) {
+    int rank = 0;
+    for (int j = 0; j < taken; ++j) {
+        const uint64_t other = uint64_t(__shfl(static_cast<uint32_t>(key >> 32), j, L)) << 32 |
+                               __shfl(static_cast<uint32_t>(key), j, L);
+        const int e = __shfl(expert, j, L);
+        rank += other > key || (other == key && e < expert);
+    }
+    int out = -1;
+    for (int j = 0; j < taken; ++j) {
+        const int r = __shfl(rank, j, L), e = __shfl(expert, j, L);
+        out = r == lane && e >= 0 ? e : out;
+    }
+    return out;
+}
+
 template <int DT, int L, int V, bool SCORED>
 __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
     using T = typename Elem<DT>::T;
@@ -262,7 +327,7 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
     const int64_t row = there ? own : a.M - 1;  // (every lane stays for the maxima)
 
     float v[V];
-    load_logits<DT, V>(a.logits, row, a.E, first, v);
+    load_row<DT, V>(a.logits, row, a.E, first, v);
     const float high = a.sigmoid ? 0.0f : row_maxf<L>(largest(v));
     float total = 0.0f;  // of the softmax
     if (!a.sigmoid && !a.renormalise) {
@@ -274,13 +339,14 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
     Choice c;
     bool sure = true;
     if constexpr (SCORED) {
-        extern __shared__ double scores[];  // [rows][E], [rows][groups], of either type
+        extern __shared__ double scores[];  // [rows][V*L], [rows][groups], of either type
         const bool grouped = a.kept < a.groups;
         float bias[V];
         bool may[V];
+        if (a.bias) load_row<IABN_F32, V>(a.bias, 0, a.E, first, bias);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            bias[j] = a.bias && first + j < a.E ? a.bias[first + j] : 0.0f;
+            bias[j] = a.bias ? bias[j] : 0.0f;
             may[j] = v[j] != -kInf && bias[j] != -kInf;
         }
         // The keys of scores s, of what may be chosen and is in a kept group.
@@ -288,11 +354,10 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
             using S = std::remove_cv_t<decltype(tol)>;
             if (!grouped) return ~uint64_t(0);
             // (A row's place is the same for both types: other waves have theirs in use.)
-            S* const t = reinterpret_cast<S*>(scores + threadIdx.x / L * a.E);
-            S* const gs = reinterpret_cast<S*>(scores + kThreads / L * a.E + threadIdx.x / L * a.groups);
+            S* const t = reinterpret_cast<S*>(scores + threadIdx.x / L * (V * L));
+            S* const gs = reinterpret_cast<S*>(scores + kThreads * V + threadIdx.x / L * a.groups);
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (first + j < a.E) t[first + j] = may[j] ? s[j] : static_cast<S>(-kInf);
+            for (int j = 0; j < V; ++j) t[first + j] = may[j] ? s[j] : static_cast<S>(-kInf);
             wave_fence();
             return kept_groups<L, S>(a, t, gs, lane, tol, sure);
         };
@@ -300,60 +365,84 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
             const int g = static_cast<int>(static_cast<uint32_t>(first + j) * a.per_magic >> 20);
             return may[j] && (!grouped || (groups >> g & 1));
         };
-        uint32_t key[V];
-        {
-            // In 32 bits.  A sigmoid is off by less than 2^-22, a term of the softmax by
-            // less than 2^-18 of the largest (its sum by 22 roundings).
-            float s[V], sum = 0.0f, tol = 0x1p-21f;
+        // In 32 bits.  A sigmoid is off by less than 2^-22, a term of the softmax by less
+        // than 2^-18 of the largest (its sum by 22 roundings).
+        float s[V], sum = 0.0f, tol = 0x1p-22f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                s[j] = __expf(a.sigmoid ? -v[j] : v[j] - high);
-                if (a.sigmoid) s[j] = __builtin_amdgcn_rcpf(1.0f + s[j]);
-                sum += s[j];
-            }
-            if (!a.sigmoid) {
-                const float scale = 1.0f / row_add<L>(sum);
-                tol = scale * 0x1p-18f;
-#pragma unroll
-                for (int j = 0; j < V; ++j) s[j] *= scale;
-            }
-#pragma unroll
-            for (int j = 0; j < V; ++j) s[j] += bias[j];
-            const uint64_t groups = in_groups(s, tol);
-#pragma unroll
-            for (int j = 0; j < V; ++j) key[j] = in_kept(groups, j) ? order32(a.bias ? s[j] : v[j]) : 0;
-            uint32_t none[1];
-            if (a.bias) c = choose<L, V, kScoreKeys>(key, none, a.k, lane, tol, sure);
-            else c = choose<L, V, kLogitKeys>(key, none, a.k, lane, tol, sure);
+        for (int j = 0; j < V; ++j) {
+            s[j] = __expf(a.sigmoid ? -v[j] : v[j] - high);
+            if (a.sigmoid) s[j] = __builtin_amdgcn_rcpf(1.0f + s[j]);
+            sum += s[j];
         }
+        if (!a.sigmoid) {
+            const float scale = 1.0f / row_add<L>(sum);
+            tol = scale * 0x1p-18f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) s[j] *= scale;
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[j] += bias[j];
+        // And in 64, where they are asked for.
+        double sum64 = 0.0;
+        const auto score64 = [&](float l) {
+            return a.sigmoid ? 1.0 / (1.0 + exp(-static_cast<double>(l)))
+                             : exp(static_cast<double>(l) - static_cast<double>(high)) / sum64;
+        };
+        const auto sum_in_64 = [&]() {
+            if (a.sigmoid || sum64 != 0.0) return;
+            double t = 0.0;
+#pragma unroll
+            for (int j = 0; j < V; ++j) t += exp(static_cast<double>(v[j]) - static_cast<double>(high));
+            sum64 = row_add64<L>(t);
+        };
+        const auto all_in_64 = [&](double (&s64)[V]) {
+            sum_in_64();
+#pragma unroll
+            for (int j = 0; j < V; ++j) s64[j] = score64(v[j]) + bias[j];
+        };
+        uint64_t groups = in_groups(s, tol);
         if (__ballot(!sure) != 0) {
-            double s[V], sum = 0.0;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const double l = v[j];
-                s[j] = a.sigmoid ? 1.0 / (1.0 + exp(-l)) : exp(l - static_cast<double>(high));
-                sum += s[j];
-            }
-            if (!a.sigmoid) sum = row_add64<L>(sum);
-#pragma unroll
-            for (int j = 0; j < V; ++j) s[j] = (a.sigmoid ? s[j] : s[j] / sum) + bias[j];
+            double s64[V];
+            all_in_64(s64);
             wave_fence();
-            const uint64_t groups = in_groups(s, 0.0);
+            groups = in_groups(s64, 0.0);
+        }
+        uint32_t key[V], none[1];
+#pragma unroll
+        for (int j = 0; j < V; ++j) key[j] = in_kept(groups, j) ? order32(a.bias ? s[j] : v[j]) : 0;
+        int taken;
+        Closeness close;
+        if (a.bias) c = choose<L, V, kScoreKeys>(key, none, a.k, lane, tol, taken, close);
+        else c = choose<L, V, kLogitKeys>(key, none, a.k, lane, tol, taken, close);
+        if (close == kClose) {
+            sum_in_64();
+            const bool is = c.expert >= 0;
+            const float l = is ? static_cast<float>(static_cast<const T*>(a.logits)[row * a.E + c.expert]) : 0.0f;
+            const uint64_t key64 = is ? order64(score64(l) + a.bias[c.expert]) : 0;
+            c.expert = by_rank<L>(c.expert, key64, taken, lane);
+            if (lane >= a.k) c.expert = -1;
+        } else if (close == kLost) {
+            double s64[V];
+            all_in_64(s64);
             uint32_t low[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const uint64_t o = in_kept(groups, j) ? order64(a.bias ? s[j] : v[j]) : 0;
+                const uint64_t o = in_kept(groups, j) ? order64(s64[j]) : 0;
                 key[j] = static_cast<uint32_t>(o >> 32);
                 low[j] = static_cast<uint32_t>(o);
             }
-            c = choose<L, V, kWideKeys>(key, low, a.k, lane, 0.0f, sure);
+            c = choose<L, V, kWideKeys>(key, low, a.k, lane, 0.0f, taken, close);
+        } else if (lane >= a.k) {
+            c.expert = -1;
         }
         if (c.expert >= 0) c.logit = static_cast<float>(static_cast<const T*>(a.logits)[row * a.E + c.expert]);
     } else {
         uint32_t key[V], none[1];
 #pragma unroll
         for (int j = 0; j < V; ++j) key[j] = v[j] == -kInf ? 0 : order32(v[j]);
-        c = choose<L, V, kLogitKeys>(key, none, a.k, lane, 0.0f, sure);
+        int taken;
+        Closeness close;
+        c = choose<L, V, kLogitKeys>(key, none, a.k, lane, 0.0f, taken, close);
     }
     const int mine = c.expert;
     const float logit = c.logit;
@@ -391,7 +480,7 @@ __global__ __launch_bounds__(kThreads) void route_bwd_kernel(RouteBwdArgs a) {
     const int64_t row = there ? own : a.M - 1;
 
     float v[V];
-    load_logits<DT, V>(a.logits, row, a.E, first, v);
+    load_row<DT, V>(a.logits, row, a.E, first, v);
     // Lane i: the i-th choice.
     int mine = lane < a.k ? a.experts[row * a.k + lane] : -1;
     if (mine < 0 || mine >= a.E) mine = -1;
@@ -422,18 +511,36 @@ __global__ __launch_bounds__(kThreads) void route_bwd_kernel(RouteBwdArgs a) {
         dot = row_add<L>(mine >= 0 ? exp_from(logit, high) / total * d : 0.0f);
     }
 
-    float sum[V] = {};
-    for (int i = 0; i < a.k; ++i) {
-        const int e = __shfl(mine, i, L);
-        const float di = __shfl(d, i, L);
+    // The choices' parts to the lanes that have their experts, through LDS; those of
+    // an expert that a token has twice are added up by both.
+    __shared__ __align__(16) float parts[kThreads * V];
+    float* const own_parts = parts + threadIdx.x / L * (L * V);
+    float sum[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum[j] += e == first + j ? di : 0.0f;
-    }
+    for (int j = 0; j < V; ++j) own_parts[first + j] = 0.0f;
+    float mine_sum = 0.0f;
+    each_choice<L>(a.k, [&](auto i) {
+        const int e = static_cast<int>(from_lane<L, i>(static_cast<uint32_t>(mine)));
+        const float di = __builtin_bit_cast(float, from_lane<L, i>(__builtin_bit_cast(uint32_t, d)));
+        mine_sum += e == mine ? di : 0.0f;
+    });
+    if constexpr (L == 64)
+        for (int i = kRowLanes; i < a.k; ++i) {
+            const int e = __shfl(mine, i);
+            const float di = __shfl(d, i);
+            mine_sum += e == mine ? di : 0.0f;
+        }
+    wave_fence();
+    if (mine >= 0) own_parts[mine] = mine_sum;
+    wave_fence();
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[j] = own_parts[first + j];
+    const float scale = 1.0f / total;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         if (a.renormalise) v[j] = sum[j];
         else if (a.sigmoid) v[j] = sum[j] == 0.0f ? 0.0f : sum[j] * sigmoid(v[j]) * sigmoid(-v[j]);
-        else v[j] = v[j] == 0.0f ? 0.0f : v[j] / total * (sum[j] - dot);
+        else v[j] = v[j] == 0.0f ? 0.0f : v[j] * scale * (sum[j] - dot);
     }
     if (!there) return;
     T* const p = static_cast<T*>(a.dlogits) + row * a.E + first;
@@ -466,7 +573,7 @@ void launch_fwd_as(const RouteArgs& a, hipStream_t st) {
     const int rows = kThreads / L;
     const dim3 grid(static_cast<uint32_t>((a.M + rows - 1) / rows));
     const bool grouped = a.kept < a.groups;
-    const size_t lds = grouped ? static_cast<size_t>(rows) * (a.E + a.groups) * sizeof(double) : 0;
+    const size_t lds = grouped ? static_cast<size_t>(rows) * (V * L + a.groups) * sizeof(double) : 0;
     if (a.bias || grouped) route_kernel<DT, L, V, true><<<grid, kThreads, lds, st>>>(a);
     else route_kernel<DT, L, V, false><<<grid, kThreads, 0, st>>>(a);
 }
