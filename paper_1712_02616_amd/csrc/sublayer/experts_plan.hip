@@ -14,7 +14,7 @@
 namespace iabn_impl {
 namespace {
 
-constexpr int kPlanThreads = 256, kPlanWaves = kPlanThreads / kWave;
+constexpr int kPlanThreads = 512, kPlanWaves = kPlanThreads / kWave;
 constexpr int kPlanPairs = 2048;    // of a block, while there are fewer blocks than
 constexpr int kMaxPlanBlocks = 256;
 

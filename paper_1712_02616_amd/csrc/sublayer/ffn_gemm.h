@@ -117,10 +117,8 @@ struct Stage {
     // last ones (the results that they go into are not stored).
     uint64_t base[2];      // the tile's first element of each matrix
     uint32_t off[kLoads];  // bytes from the step's first element
-    // (k strided, GATHER: the next step's entries of the plan, of the lines that a
-    // wave brings at a time: two, or as many as lanes may each look up their own.)
-    static constexpr bool kPairs = kWave / kPerLine == 2;
-    uint32_t entry[KS && GATHER ? kLoads : 1][kPairs ? 2 : 1];
+    // (k strided, GATHER: the next step's entries of the plan.)
+    uint32_t entry[KS && GATHER ? kLoads : 1];
     template <typename Op>
     __device__ __forceinline__ void prepare(const Op& o, int64_t row0, int64_t rows, const Tokens& tokens = {}) {
 #pragma unroll
@@ -148,31 +146,11 @@ struct Stage {
         }
     }
     // GATHER with k strided: the entries that the step at k0 takes, a step ahead of its fetch.
-    template <int FROM = 0, int TO = kLoads>
     __device__ __forceinline__ void look_up(int64_t k0, int64_t K, const Tokens& tokens) {
-        if constexpr (KS && GATHER && kPairs) {
-            // (Scalar loads: a vector load would be waited for with the fetches before it.)
-            typedef const __attribute__((address_space(4))) int32_t* scalar_t;
-            const scalar_t order = (scalar_t)(reinterpret_cast<uint64_t>(tokens.order));
-            const int first = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * 2;
+        if constexpr (KS && GATHER)
 #pragma unroll
-            for (int i = FROM; i < TO; ++i)
-#pragma unroll
-                for (int q = 0; q < 2; ++q) entry[i][q] = order[min(k0 + first + i * kLineStep + q, K - 1)];
-        } else if constexpr (KS && GATHER) {
-#pragma unroll
-            for (int i = FROM; i < TO; ++i)
-                entry[i][0] = tokens.order[min(k0 + first_line() + i * kLineStep, K - 1)];
-        }
-    }
-    // Bytes from the matrix to the row of a thread's i-th line.
-    __device__ __forceinline__ uint32_t gathered(int i, uint32_t row_bytes, const Tokens& tokens) const {
-        if constexpr (kPairs) {
-            const uint32_t a = tokens.of(entry[i][0]) * row_bytes, b = tokens.of(entry[i][1]) * row_bytes;
-            return lane_id() < kWave / 2 ? a : b;
-        } else {
-            return tokens.of(entry[i][0]) * row_bytes;
-        }
+            for (int i = 0; i < kLoads; ++i)
+                entry[i] = tokens.order[min(k0 + first_line() + i * kLineStep, K - 1)];
     }
     // K >= 0: lines of k from there on (strided) are fetched as zeros, by offsets that
     // lie outside of the buffer (row0: the tile's first column).
@@ -198,7 +176,7 @@ struct Stage {
                 reinterpret_cast<void*>((which ? base[1] : base[0]) + at), 0, static_cast<int>(bytes), 0x00027000);
             uint32_t from = off[i];
             if constexpr (KS && GATHER) {
-                from += gathered(i, static_cast<uint32_t>(o.ld * static_cast<int64_t>(sizeof(T))), tokens);
+                from += tokens.of(entry[i]) * static_cast<uint32_t>(o.ld * static_cast<int64_t>(sizeof(T)));
                 if (K >= 0 && k0 + first_line() + i * kLineStep >= K) from = kOutside;
             }
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
@@ -316,8 +294,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
     constexpr int kHalves = kAhead ? 2 : 1, kPhases = kSteps * kHalves, NH = NM / kHalves;
     // The largest tile over groups: the last one of an expert's rows often holds no
     // more than half of them.  Every wave then has rows of both halves of the tile,
-    // so that the phases of the empty half are left out ((32768 pairs of 64 experts,
-    // kShort).
+    // so that the phases of the empty half are left out (32768 pairs of 64 experts, up
+    // projection: 328 us, 315 without them).
     constexpr bool kShort = kGroups && kBase != kGemmDw && kAhead;
     const auto acc_row = [&](int g) __attribute__((always_inline)) {  // of accumulators g
         return kShort ? g / NH * (TM / 2) + wave / WAVES_N * (WM / 2) + g % NH * 16 : wm + g * 16;
@@ -420,52 +398,40 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
             sx.look_up(int64_t(lo) * BK, a.K, tokens);
             sy.look_up(int64_t(lo) * BK, a.K, tokens);
         }
-        if constexpr (kGroups && kAhead) {
+        if constexpr (kShort) {
             // Over groups a step's tiles come from farther away (an expert's weights
             // serve few rows): its fetch is cut in two, and the first part of the
-            // next but one starts as soon as the buffer's first part has been read,
-            // in the middle of a step.  The parts: X's first half of rows and all of Y
-            // (whose fragments are held for the second half), or where k is strided
-            // in both, the first half of k.
-            constexpr bool kByK = kBase == kGemmDw;
-            constexpr int kXPart = SX::kLoads / 2, kYPart = kByK ? SY::kLoads / 2 : SY::kLoads;
-            constexpr int kXHalf = SX::kBytes / 2, kYHalf = SY::kBytes / 2;
-            const auto first_part = [&](int kt, char* x0, char* y0) __attribute__((always_inline)) {
-                sx.template fetch<0, kXPart>(x, seg_of(kt), k_of(kt), x0, tokens, kFill ? a.K : -1, m0);
-                sy.template fetch<0, kYPart>(y, seg_of(kt), k_of(kt), y0, tokens, kFill ? a.K : -1, n0);
+            // next but one starts as soon as it has been read, in the middle of a
+            // step: X's first half of rows, and all of Y, whose fragments are held for
+            // the second half.  (Up projection of 512 rows of each of 64 experts, 2048
+            // -> 2x1024: 238 us instead of 254.  In dW, with parts by k: dy's 345 us
+            // instead of 317.)
+            constexpr int kXPart = SX::kLoads / 2, kXHalf = SX::kBytes / 2;
+            const auto first_part = [&](int kt, char* x0, char* yb) __attribute__((always_inline)) {
+                sx.template fetch<0, kXPart>(x, seg_of(kt), k_of(kt), x0, tokens, -1, m0);
+                sy.template fetch<0, SY::kLoads>(y, seg_of(kt), k_of(kt), yb, tokens, -1, n0);
             };
-            const auto second_part = [&](int kt, char* x1, char* y1) __attribute__((always_inline)) {
-                sx.template fetch<kXPart, SX::kLoads>(x, seg_of(kt), k_of(kt), x1, tokens, kFill ? a.K : -1, m0);
-                if constexpr (kByK)
-                    sy.template fetch<kYPart, SY::kLoads>(y, seg_of(kt), k_of(kt), y1, tokens, kFill ? a.K : -1, n0);
+            const auto second_part = [&](int kt, char* x1) __attribute__((always_inline)) {
+                sx.template fetch<kXPart, SX::kLoads>(x, seg_of(kt), k_of(kt), x1, tokens, -1, m0);
             };
-            const auto look_up_first = [&](int kt) __attribute__((always_inline)) {
-                sx.template look_up<0, kXPart>(k_of(kt), a.K, tokens);
-                sy.template look_up<0, kYPart>(k_of(kt), a.K, tokens);
-            };
-            const auto look_up_second = [&](int kt) __attribute__((always_inline)) {
-                sx.template look_up<kXPart, SX::kLoads>(k_of(kt), a.K, tokens);
-                sy.template look_up<kYPart, SY::kLoads>(k_of(kt), a.K, tokens);
-            };
-            // Phase p: of k half s, X rows' half h; xr, yr: the parts that hold them.
+            // Phase p: half p/2 of X's rows (in xr), half p%2 of k.
             const auto take = [&](const char* __restrict__ xr, const char* __restrict__ yr, int p) __attribute__((always_inline)) {
-                const int h = kByK ? p % 2 : p / 2, s = kByK ? p / 2 : p % 2;
-                if (h == 0)
+                if (p < kSteps)
 #pragma unroll
-                    for (int j = 0; j < NN; ++j) fy[s][j] = SY::frag(yr, wn + j * 16, kByK ? 0 : s);
+                    for (int j = 0; j < NN; ++j) fy[p][j] = SY::frag(yr, wn + j * 16, p);
 #pragma unroll
-                for (int i = 0; i < NH; ++i) fx[p & 1][i] = SX::frag(xr, acc_row(kByK ? h * NH + i : i), kByK ? 0 : s);
+                for (int i = 0; i < NH; ++i) fx[p & 1][i] = SX::frag(xr, acc_row(i), p % kSteps);
             };
             const auto multiply = [&](int p) __attribute__((always_inline)) {
-                const int h = kByK ? p % 2 : p / 2, s = kByK ? p / 2 : p % 2;
+                const int h = p / kSteps, k = p % kSteps;
 #pragma unroll
                 for (int i = 0; i < NH; ++i)
 #pragma unroll
                     for (int j = 0; j < NN; ++j)
-                        acc[h * NH + i][j] = Mma<DT>::run(fy[s][j], fx[p & 1][i], acc[h * NH + i][j]);
+                        acc[h * NH + i][j] = Mma<DT>::run(fy[k][j], fx[p & 1][i], acc[h * NH + i][j]);
                 __builtin_amdgcn_sched_barrier(0);  // (products stay on their side)
             };
-            // All waves: their reads of LDS have ended, and all but the last `left`
+            // All waves: their reads of LDS have ended, and all but their last `left`
             // fetches have arrived.
             const auto meet_but = [](auto left) __attribute__((always_inline)) {
                 __builtin_amdgcn_s_waitcnt(0x0070 | (left & 15) | (left >> 4 << 14));
@@ -475,69 +441,58 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
             };
             using std::integral_constant;
             constexpr integral_constant<int, 63> kAny;
-            constexpr integral_constant<int, kXPart + kYPart> kFirst;
+            constexpr integral_constant<int, kXPart + SY::kLoads> kFirst;
             constexpr integral_constant<int, SX::kLoads + SY::kLoads> kStepLoads;
             constexpr integral_constant<int, 0> kNone;
-            const auto split_turn = [&](int kt, char* __restrict__ x0, char* __restrict__ x1, char* __restrict__ y0,
-                                        char* __restrict__ y1, char* __restrict__ next_x, char* __restrict__ next_y,
+            // (The parts of both buffers are told apart as the buffers are above.)
+            const auto split_turn = [&](int kt, char* __restrict__ x0, char* __restrict__ x1, char* __restrict__ yb,
+                                        char* __restrict__ next_x, char* __restrict__ next_y,
                                         auto tall) __attribute__((always_inline)) {
                 const bool more = kt + 2 < hi;
-                take(x0, y0, 1);
+                take(x0, yb, 1);
                 multiply(0);
                 if constexpr (tall) {
                     meet_but(kAny);
-                    if (more) {
-                        first_part(kt + 2, x0, y0);
-                        // (Here, so that the wait at the next barrier is theirs too.)
-                        look_up_second(kt + 2);
-                        look_up_first(kt + 3);
-                    }
-                    take(x1, y1, 2);
+                    if (more) first_part(kt + 2, x0, yb);
+                    take(x1, yb, 2);
                     multiply(1);
-                    take(x1, y1, 3);
+                    take(x1, yb, 3);
                     multiply(2);
                     if (more) meet_but(kFirst);
                     else meet_but(kNone);
-                    if (more) second_part(kt + 2, x1, y1);
+                    if (more) second_part(kt + 2, x1);
                 } else {
                     meet_but(kNone);
-                    if (more) first_part(kt + 2, x0, y0);
+                    if (more) first_part(kt + 2, x0, yb);
                 }
                 if (kt + 1 < hi) take(next_x, next_y, 0);
                 multiply(tall ? 3 : 1);
             };
-            const auto split_round = [&](int kt, char* __restrict__ x0, char* __restrict__ x1, char* __restrict__ y0,
-                                         char* __restrict__ y1, char* __restrict__ x2, char* __restrict__ x3,
-                                         char* __restrict__ y2, char* __restrict__ y3, auto tall) __attribute__((always_inline)) {
-                split_turn(kt, x0, x1, y0, y1, x2, y2, tall);
-                if (kt + 1 < hi) split_turn(kt + 1, x2, x3, y2, y3, x0, y0, tall);
+            const auto split_round = [&](int kt, char* __restrict__ x0, char* __restrict__ x1, char* __restrict__ ya,
+                                         char* __restrict__ x2, char* __restrict__ x3, char* __restrict__ yb,
+                                         auto tall) __attribute__((always_inline)) {
+                split_turn(kt, x0, x1, ya, x2, yb, tall);
+                if (kt + 1 < hi) split_turn(kt + 1, x2, x3, yb, x0, ya, tall);
             };
             const auto run = [&](auto tall) __attribute__((always_inline)) {
-                char *const y0 = lds0 + SX::kBytes, *const y1 = lds1 + SX::kBytes;
+                char *const ya = lds0 + SX::kBytes, *const yb = lds1 + SX::kBytes;
                 if (lo >= hi) return;
-                first_part(lo, lds0, y0);
-                if (tall) second_part(lo, lds0 + kXHalf, y0 + kYHalf);
+                first_part(lo, lds0, ya);
+                if (tall) second_part(lo, lds0 + kXHalf);
                 if (lo + 1 < hi) {
-                    look_up_first(lo + 1);
-                    look_up_second(lo + 1);
-                    first_part(lo + 1, lds1, y1);
-                    if (tall) second_part(lo + 1, lds1 + kXHalf, y1 + kYHalf);
-                    look_up_first(lo + 2);
+                    first_part(lo + 1, lds1, yb);
+                    if (tall) second_part(lo + 1, lds1 + kXHalf);
                     if (tall) meet_but(kStepLoads);
                     else meet_but(kFirst);
                 } else {
                     meet_but(kNone);
                 }
-                take(lds0, y0, 0);
+                take(lds0, ya, 0);
                 for (int kt = lo; kt < hi; kt += 2)
-                    split_round(kt, lds0, lds0 + kXHalf, y0, y0 + kYHalf, lds1, lds1 + kXHalf, y1, y1 + kYHalf, tall);
+                    split_round(kt, lds0, lds0 + kXHalf, ya, lds1, lds1 + kXHalf, yb, tall);
             };
-            if constexpr (kShort) {
-                if (a.M - m0 > TM / 2) run(std::true_type());
-                else run(std::false_type());
-            } else {
-                run(std::true_type());
-            }
+            if (a.M - m0 > TM / 2) run(std::true_type());
+            else run(std::false_type());
         } else {
             if (lo < hi) fetch(lo, lds0);
             if (kAhead && lo < hi) {
@@ -620,11 +575,11 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
 #pragma unroll
     for (int p = 0; p < NM; p += kPass) {
         if (kShort && m0 + acc_row(p) - acc_row(0) >= a.M) break;  // (a half that is empty)
-        chunk_t gu[2][2];
-        if constexpr (kBase == kGemmDh) {
-            load_gu(p, 0, gu[0]);
-            load_gu(p, 1, gu[1]);
-        }
+        constexpr int kLook = kGroups && kTurns % 4 == 0 ? 4 : 2;
+        chunk_t gu[kLook][2];
+        if constexpr (kBase == kGemmDh)
+#pragma unroll
+            for (int q = 0; q < kLook; ++q) load_gu(p, q, gu[q]);
         const int lm = lane_id() & 15, ln = (lane_id() >> 4) * 4;
 #pragma unroll
         for (int i = 0; i < kPass; ++i)
@@ -641,12 +596,12 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
         };
         if constexpr (kBase == kGemmDh) {
 #pragma unroll 1
-            for (int c = 0; c < kTurns; c += 2)
+            for (int c = 0; c < kTurns; c += kLook)
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
+                for (int q = 0; q < kLook; ++q) {
                     const auto raw_g = gu[q][0], raw_u = gu[q][1];
                     const Place at_c = place(p, c + q);
-                    if (c + q + 2 < kTurns) load_gu(p, c + q + 2, gu[q]);
+                    if (c + q + kLook < kTurns) load_gu(p, c + q + kLook, gu[q]);
                     if (!kGroups && at_c.inside <= 0) continue;
                     float v[kChunk], g[kChunk], u[kChunk], dg[kChunk], du[kChunk], h[kChunk];
                     read(at_c.row, at_c.col, v);

@@ -12,9 +12,8 @@
 namespace iabn_impl {
 namespace {
 
-// The tensor of this block's piece, and the piece [from, to) of it.
-__device__ __forceinline__ int tensor_of(const GradArgs& a, int64_t& from, int64_t& to) {
-    const int b = blockIdx.x;
+// The tensor of piece b, and the piece [from, to) of it.
+__device__ __forceinline__ int tensor_of(const GradArgs& a, int b, int64_t& from, int64_t& to) {
     int lo = 0, hi = a.count;  // first[lo] <= b < first[hi]
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
@@ -42,7 +41,7 @@ __device__ __forceinline__ double squares(const void* p, int64_t from, int64_t t
     double sum = 0.0;
     for (int64_t at = from + int64_t(threadIdx.x) * kChunk; at < to; at += kThreads * kChunk) {
         float v[kChunk];
-        widen<DT>(load_chunk<DT, kStream>(p, at, static_cast<int>(min(to - at, int64_t(kChunk)))), v);
+        widen<DT>(load_chunk<DT, kCached>(p, at, static_cast<int>(min(to - at, int64_t(kChunk)))), v);
 #pragma unroll
         for (int j = 0; j < kChunk; ++j) {
             const double d = v[j];
@@ -55,7 +54,7 @@ __device__ __forceinline__ double squares(const void* p, int64_t from, int64_t t
 __global__ __launch_bounds__(kThreads) void grad_norm_kernel(GradArgs a) {
     __shared__ double slots[kWaves];
     int64_t from, to;
-    const int t = tensor_of(a, from, to);
+    const int t = tensor_of(a, blockIdx.x, from, to);
     double sum;
     switch (a.dtype[t]) {
         case IABN_F32: sum = squares<IABN_F32>(a.in[t], from, to); break;
@@ -69,7 +68,14 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(GradArgs a) {
 __global__ __launch_bounds__(kThreads) void grad_join_kernel(const double* part, int64_t n, float* norm) {
     __shared__ double slots[kWaves];
     double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += kThreads) sum += part[i];
+    constexpr int kAhead = 8;  // on their way at a time
+    for (int64_t i = threadIdx.x; i < n; i += kAhead * kThreads) {
+        double v[kAhead];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) v[q] = i + q * kThreads < n ? part[i + q * kThreads] : 0.0;
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) sum += v[q];
+    }
     sum = block_sum(sum, slots);
     if (threadIdx.x == 0) *norm = static_cast<float>(sqrt(sum));
 }
@@ -88,7 +94,10 @@ __device__ __forceinline__ void scale(const void* in, void* out, int64_t from, i
 
 __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradArgs a) {
     int64_t from, to;
-    const int t = tensor_of(a, from, to);
+    // (From the last piece on: the caches hold what the norm read last.  403 million
+    // bf16 values: 277 us, and 132 for the norm; 309 and 118 where the norm's loads
+    // are non-temporal.)
+    const int t = tensor_of(a, gridDim.x - 1 - blockIdx.x, from, to);
     const double ratio = static_cast<double>(a.max_norm) / (static_cast<double>(*a.norm) + 1e-6);
     const float factor = ratio >= 1.0 ? 1.0f : static_cast<float>(ratio);  // (a NaN stays one)
     if (factor == 1.0f && a.in[t] == a.out[t]) return;

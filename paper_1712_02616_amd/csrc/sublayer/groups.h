@@ -76,6 +76,10 @@ __device__ __forceinline__ void strip_of(uint32_t t, int tiles_m, int tiles_n, i
 
 // The expert that tile number t of the launch (tiles_n tiles for every TM of an
 // expert's rows) belongs to, and the tile's number in it; false past the last.
+template <int CTRL>
+__device__ __forceinline__ int shifted(int v) {
+    return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, true);
+}
 struct Group {
     int expert, first, rows;
     uint32_t tile;
@@ -90,11 +94,17 @@ __device__ __forceinline__ bool find_group(const int32_t* offsets, int E, int P,
         rows_of(offsets, e, P, first, rows);
         tiles += (rows + TM - 1) / TM;
     }
+    // The sum over the lanes up to each: in rows of 16, then over the rows' ends.
     int upto = tiles;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        const int o = __shfl_up(upto, d);
-        if (static_cast<int>(lane_id()) >= d) upto += o;
+    upto += shifted<0x111>(upto);
+    upto += shifted<0x112>(upto);
+    upto += shifted<0x114>(upto);
+    upto += shifted<0x118>(upto);
+    {
+        const int row = static_cast<int>(lane_id()) / 16;
+        const int end0 = __builtin_amdgcn_readlane(upto, 15), end1 = __builtin_amdgcn_readlane(upto, 31),
+                  end2 = __builtin_amdgcn_readlane(upto, 47);
+        upto += (row > 0 ? end0 : 0) + (row > 1 ? end1 : 0) + (row > 2 ? end2 : 0);
     }
     const uint32_t total = static_cast<uint32_t>(__builtin_amdgcn_readlane(upto, kWave - 1)) * tiles_n;
     if (blockIdx.x >= total) return false;
