@@ -6,6 +6,9 @@
 namespace iabn_impl {
 namespace {
 
+constexpr int64_t kCUs = 256;
+constexpr int kMaxSplits = 16;
+
 // (A launch holds fewer than 2^32 threads.)
 uint32_t blocks_for(int64_t want) { return static_cast<uint32_t>(want < 1 << 22 ? want : 1 << 22); }
 
@@ -87,13 +90,22 @@ void launch_dots(const float* dots, const int32_t* place, float* dweights, int64
     dots_kernel<<<dim3(blocks_for(div_up(P, kThreads / 16))), kThreads, 0, st>>>(dots, place, dweights, P, n);
 }
 
-bool few_pairs(int64_t M, int64_t, int64_t) { return M <= kFewRows; }
+// By the tokens, which no expert has more rows than (where none has it twice).  Few
+// tokens' kernels and tiles take (us, forward, 16 / 40 / 56 / 64 tokens): bf16 8 of 64
+// experts (2048 -> 1024) 143 / 161 / 175 / 181 and 147 / 162 / 164 / 164; 2 of 8 (2048
+// -> 4096) 95 / 97 / 104 / 113 and 128 / 117 / 118 / 132; fp16 4 of 32 (1024 -> 2048) 81
+// / 85 / 91 / 95 and 86 / 90 / 91 / 91; fp32 2 of 7 (1000 -> 731) 30 / 39 / 40 / 69 and
+// 51 each.  One token of the first: 30 and 48.
+constexpr int64_t kFewTokens = 56;
+bool few_pairs(int64_t M) { return M <= kFewTokens; }
 
+// Blocks of 16 columns over K: split like those of one matrix (plan_few), where they
+// are fewer than three quarters of the CUs.
 int plan_grouped_few(int64_t P, int64_t E, int64_t N, int64_t K, int dtype) {
     const int64_t blocks = div_up(N, 16) * (E < P ? E : P), lines = div_up(K, dtype == IABN_F32 ? 32 : 64);
-    if (blocks >= 192) return 1;
-    int64_t s = 512 / blocks;
-    if (s > 16) s = 16;
+    if (blocks >= kCUs * 3 / 4) return 1;
+    int64_t s = kCUs * 2 / blocks;
+    if (s > kMaxSplits) s = kMaxSplits;
     if (s > lines / 16) s = lines / 16;
     return s < 2 ? 1 : static_cast<int>(s);
 }

@@ -199,7 +199,7 @@ TileSize plan_grouped(int dtype, GemmKind kind, bool direct, int64_t P, int64_t 
 
 // Whether the forward takes the few tokens' kernels, over how many blocks their
 // second product's sum is split.
-bool few_pairs(int64_t M, int64_t P, int64_t E);
+bool few_pairs(int64_t M);
 int plan_grouped_few(int64_t P, int64_t E, int64_t N, int64_t K, int dtype);
 
 // y_t = sum over the slots s of the terms of its pairs' rows (place[t*k + s]),

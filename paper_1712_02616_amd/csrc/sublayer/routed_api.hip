@@ -67,7 +67,7 @@ struct ExpertsSpace {
 ExpertsSpace experts_space(int64_t M, int64_t k, int64_t E, int64_t C, int64_t F, int dtype) {
     const size_t P = static_cast<size_t>(M) * k, eb = elem_bytes(dtype);
     ExpertsSpace s = {padded(P * F * eb), padded(P * C * eb), padded(P * div_up(F, 64) * sizeof(float))};
-    if (P > 0 && few_pairs(M, P, E)) {
+    if (P > 0 && few_pairs(M)) {
         const size_t few = padded(plan_grouped_few(P, E, C, F, dtype) * P * C * sizeof(float));
         s.terms = s.terms < few ? few : s.terms;
     }
@@ -263,7 +263,7 @@ int iabn_experts_forward(const void* x, const int32_t* plan, const float* weight
     if ((rc = check_workspace(workspace, workspace_bytes, space.all()))) return rc;
     const PlanArgs sorted = plan_of(P, E, const_cast<int32_t*>(plan));
     void* const terms = static_cast<char*>(workspace) + space.h;
-    const bool few = few_pairs(M, P, E);
+    const bool few = few_pairs(M);
     GroupArgs up = group_args(sorted, weights, k, C, F, act, slope);
     up.x = {{x, x}, C}, up.y = {{w_gate, w_up}, C};
     up.M = P, up.N = F, up.K = C;
