@@ -559,8 +559,9 @@ int iabn_experts_plan(const int32_t *experts, int32_t *plan, int64_t M, int64_t 
  *   act, slope     as in iabn_ffn_forward.
  *   C, F           at most 2^17; no tensor of more than 2^35 elements.  Where C or F
  *                  or k is 0, y (and g, u) are 0.
- * Products are summed in fp32 (matrix cores).  h and, for more than 56 tokens, each
- * pair's weighted term of y are rounded to the storage type between the kernels.
+ * Products are summed in fp32 (matrix cores).  Between the kernels h (and dg, du)
+ * are rounded to the storage type, and each pair's term of y and dx to no fewer than
+ * 16 digits of fp32's 24, with its range.
  * A token without experts has y = 0.  The workspace holds
  * iabn_experts_workspace_size(M, k, E, C, F, dtype) bytes, 16-byte aligned: enough
  * for either direction.

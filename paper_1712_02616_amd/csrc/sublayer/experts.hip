@@ -16,7 +16,7 @@ uint32_t blocks_for(int64_t want) { return static_cast<uint32_t>(want < 1 << 22 
 // by the terms' traffic.
 template <int DT, bool FEW>
 __global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a, int chunks) {
-    constexpr int TERM = FEW ? IABN_F32 : DT, kSlots = 4;
+    constexpr int kSlots = 4;
     for (int64_t c = int64_t(blockIdx.x) * kThreads + threadIdx.x; c < a.M * chunks; c += int64_t(gridDim.x) * kThreads) {
         const int64_t t = c / chunks, col = (c - t * chunks) * kChunk;
         const int n = static_cast<int>(min(a.C - col, int64_t(kChunk)));
@@ -25,7 +25,7 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a, int ch
             // The places, then the terms of several slots on their way together.
             uint32_t p[kSlots];
             float w[kSlots];
-            typename ChunkOf<TERM>::vec term[kSlots];
+            Terms<FEW ? IABN_F32 : DT> term[kSlots];
 #pragma unroll
             for (int q = 0; q < kSlots; ++q) {
                 p[q] = s0 + q < a.k ? static_cast<uint32_t>(a.place[t * a.k + s0 + q]) : 0xFFFFFFFFu;
@@ -34,12 +34,12 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a, int ch
             for (int split = 0; split < (FEW ? a.splits : 1); ++split) {
 #pragma unroll
                 for (int q = 0; q < kSlots; ++q)
-                    term[q] = load_chunk<TERM, FEW ? kCached : kStream>(
-                        a.terms, (int64_t(split) * a.P + p[q]) * a.C + col, p[q] < static_cast<uint32_t>(a.P) ? n : 0);
+                    term[q].load(a.terms, a.low, (int64_t(split) * a.P + p[q]) * a.C + col,
+                                 p[q] < static_cast<uint32_t>(a.P) ? n : 0);
 #pragma unroll
                 for (int q = 0; q < kSlots; ++q) {
                     float v[kChunk];
-                    widen<TERM>(term[q], v);
+                    term[q].get(v);
 #pragma unroll
                     for (int j = 0; j < kChunk; ++j)
                         sum[j] = p[q] < static_cast<uint32_t>(a.P) ? FEW ? fmaf(w[q], v[j], sum[j]) : sum[j] + v[j] : sum[j];

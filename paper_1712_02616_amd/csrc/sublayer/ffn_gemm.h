@@ -652,13 +652,14 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void gemm_kernel(ArgsOf<KI
                         a.part, (int64_t(blockIdx.y) * gridDim.z + z) * a.M * a.N + at_c.out, at_c.inside, v);
                 } else {
                     if constexpr (kGroups && kBase == kGemmDown) {
-                        // (Weighted before it is rounded: an intermediate value overflows
-                        // only where a term of the tokens' sum does.)
                         const float w = pair_weight(a, tokens, at_c.m, a.M);
 #pragma unroll
                         for (int j = 0; j < kChunk; ++j) v[j] *= w;
                     }
-                    store_chunk<DT, kCached>(z ? a.out[1] : a.out[0], at_c.out, at_c.inside, v);
+                    if constexpr (kGroups && (kBase == kGemmDown || kBase == kGemmDx))
+                        store_terms<DT>(a.out[0], a.out[1], at_c.out, at_c.inside, v);
+                    else
+                        store_chunk<DT, kCached>(z ? a.out[1] : a.out[0], at_c.out, at_c.inside, v);
                 }
             }
         }

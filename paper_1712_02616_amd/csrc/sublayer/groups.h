@@ -127,6 +127,81 @@ __device__ __forceinline__ bool find_group(const int32_t* offsets, int E, int P,
     return true;
 }
 
+// A pair's term of its token's sum (y, dx), between the product that forms it and the
+// kernel that adds the terms up.  fp32 for fp32; else the upper 24 bits of it, 16 in
+// `high` and 8 in `low`: with fp32's range, and so many digits that they do not show
+// beside the result's rounding.  (In the storage type y of (4096, 8 of 64 experts,
+// 2048 -> 1024) bf16 is off by 2.9e-3 in root mean square, with these by 2.3e-3,
+// which h's rounding leaves, at 24 us of 545 more.)
+template <int DT>
+__device__ __forceinline__ void store_terms(void* high, void* low, int64_t at, int n, const float (&v)[kChunk]) {
+    if constexpr (DT == IABN_F32) {
+        store_chunk<IABN_F32, kCached>(high, at, n, v);
+    } else {
+        typedef uint16_t high_t __attribute__((ext_vector_type(8)));
+        typedef uint16_t high_mem __attribute__((ext_vector_type(8), aligned(2)));
+        typedef uint8_t low_t __attribute__((ext_vector_type(8)));
+        typedef uint8_t low_mem __attribute__((ext_vector_type(8), aligned(1)));
+        high_t h;
+        low_t l;
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) {
+            const uint32_t bits = __builtin_bit_cast(uint32_t, v[j]) + (v[j] == v[j] ? 0x80u : 0u);
+            h[j] = static_cast<uint16_t>(bits >> 16);
+            l[j] = static_cast<uint8_t>(bits >> 8);
+        }
+        uint16_t* const ph = static_cast<uint16_t*>(high) + at;
+        uint8_t* const pl = static_cast<uint8_t*>(low) + at;
+        if (n >= kChunk) {
+            *reinterpret_cast<high_mem*>(ph) = h;
+            *reinterpret_cast<low_mem*>(pl) = l;
+        } else {
+#pragma unroll
+            for (int j = 0; j < kChunk; ++j)
+                if (j < n) ph[j] = h[j], pl[j] = l[j];
+        }
+    }
+}
+// The bits of kChunk terms as they are loaded, and the terms.
+template <int DT>
+struct Terms {
+    typename ChunkOf<IABN_F32>::vec v;
+    __device__ __forceinline__ void load(const void* high, const void*, int64_t at, int n) {
+        v = load_chunk<IABN_F32, kStream>(high, at, n);
+    }
+    __device__ __forceinline__ void get(float (&f)[kChunk]) const { widen<IABN_F32>(v, f); }
+};
+struct Terms24 {
+    typedef uint16_t high_t __attribute__((ext_vector_type(8)));
+    typedef uint8_t low_t __attribute__((ext_vector_type(8)));
+    high_t h;
+    low_t l;
+    __device__ __forceinline__ void load(const void* high, const void* low, int64_t at, int n) {
+        typedef uint16_t high_mem __attribute__((ext_vector_type(8), aligned(2)));
+        typedef uint8_t low_mem __attribute__((ext_vector_type(8), aligned(1)));
+        const uint16_t* const ph = static_cast<const uint16_t*>(high) + at;
+        const uint8_t* const pl = static_cast<const uint8_t*>(low) + at;
+        h = {}, l = {};
+        if (n >= kChunk) {
+            h = __builtin_nontemporal_load(reinterpret_cast<const high_mem*>(ph));
+            l = __builtin_nontemporal_load(reinterpret_cast<const low_mem*>(pl));
+        } else {
+#pragma unroll
+            for (int j = 0; j < kChunk; ++j)
+                if (j < n) h[j] = ph[j], l[j] = pl[j];
+        }
+    }
+    __device__ __forceinline__ void get(float (&f)[kChunk]) const {
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j)
+            f[j] = __builtin_bit_cast(float, static_cast<uint32_t>(h[j]) << 16 | static_cast<uint32_t>(l[j]) << 8);
+    }
+};
+template <>
+struct Terms<IABN_F16> : Terms24 {};
+template <>
+struct Terms<IABN_BF16> : Terms24 {};
+
 // A group's operand: its two matrices in registers (an array that is indexed by a
 // register would go through scratch memory).
 struct GroupOperand {
@@ -203,9 +278,10 @@ bool few_pairs(int64_t M);
 int plan_grouped_few(int64_t P, int64_t E, int64_t N, int64_t K, int dtype);
 
 // y_t = sum over the slots s of the terms of its pairs' rows (place[t*k + s]),
-// weighted where `weights` is not null: [splits][P][C] of fp32 then, else [P][C].
+// weighted where `weights` is not null: [splits][P][C] of fp32 then, else [P][C]
+// as store_terms leaves them.
 struct CombineArgs {
-    const void* terms;
+    const void *terms, *low;
     const int32_t* place;
     const float* weights;
     void* y;

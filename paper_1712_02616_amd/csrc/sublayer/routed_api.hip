@@ -58,15 +58,18 @@ int check_experts(int dtype, int act, float slope, int64_t M, int64_t k, int64_t
 
 size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// h (forward and backward), then the pairs' terms, [P][C] of the storage type or
-// of fp32 for few tokens; in the backward the dots, [P][ceil(F/64)], after them.
+// h (forward and backward), then the pairs' terms, [P][C] as store_terms leaves them
+// or of fp32 for few tokens; in the backward the dots, [P][ceil(F/64)], after them.
 struct ExpertsSpace {
     size_t h, terms, dots;
+    size_t low;  // of the terms, from their begin
     size_t all() const { return h + terms + dots; }
 };
 ExpertsSpace experts_space(int64_t M, int64_t k, int64_t E, int64_t C, int64_t F, int dtype) {
     const size_t P = static_cast<size_t>(M) * k, eb = elem_bytes(dtype);
-    ExpertsSpace s = {padded(P * F * eb), padded(P * C * eb), padded(P * div_up(F, 64) * sizeof(float))};
+    ExpertsSpace s = {padded(P * F * eb), padded(P * C * eb), padded(P * div_up(F, 64) * sizeof(float)), 0};
+    s.low = s.terms;
+    if (dtype != IABN_F32) s.terms += padded(P * C);
     if (P > 0 && few_pairs(M)) {
         const size_t few = padded(plan_grouped_few(P, E, C, F, dtype) * P * C * sizeof(float));
         s.terms = s.terms < few ? few : s.terms;
@@ -272,10 +275,10 @@ int iabn_experts_forward(const void* x, const int32_t* plan, const float* weight
     GroupArgs down = group_args(sorted, weights, k, C, F, act, slope);
     down.x = {{workspace, workspace}, F}, down.y = {{w_down, w_down}, F};
     down.M = P, down.N = C, down.K = F;
-    down.out[0] = terms, down.part = static_cast<float*>(terms);
+    down.out[0] = terms, down.out[1] = static_cast<char*>(terms) + space.low, down.part = static_cast<float*>(terms);
     few ? grouped_few(dtype, kOverGroups + kGemmDown, down, st) : grouped(dtype, kOverGroups + kGemmDown, down, 1, st);
     CombineArgs join = {};
-    join.terms = terms, join.place = sorted.place, join.weights = few ? weights : nullptr, join.y = y;
+    join.terms = terms, join.low = down.out[1], join.place = sorted.place, join.weights = few ? weights : nullptr, join.y = y;
     join.M = M, join.C = C, join.k = static_cast<int32_t>(k), join.P = sorted.P;
     join.splits = few ? plan_grouped_few(P, E, C, F, dtype) : 1;
     launch_combine(dtype, join, st);
@@ -334,10 +337,10 @@ int iabn_experts_backward(const void* dy, const void* x, const int32_t* plan, co
     GroupArgs dxp = base;
     dxp.x = {{dg, du}, F}, dxp.y = {{w_gate, w_up}, C};
     dxp.M = P, dxp.N = C, dxp.K = F;
-    dxp.out[0] = terms;
+    dxp.out[0] = terms, dxp.out[1] = static_cast<char*>(terms) + space.low;
     grouped(dtype, kOverGroups + kGemmDx, dxp, 1, st);
     CombineArgs join = {};
-    join.terms = terms, join.place = sorted.place, join.y = dx;
+    join.terms = terms, join.low = dxp.out[1], join.place = sorted.place, join.y = dx;
     join.M = M, join.C = C, join.k = static_cast<int32_t>(k), join.P = sorted.P, join.splits = 1;
     launch_combine(dtype, join, st);
     return launched("experts_backward");

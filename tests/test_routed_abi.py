@@ -111,8 +111,8 @@ def test_experts_workspace(lib):  # noqa: F811
     # h, the pairs' terms and the weights' partial gradients, and no more than padding.
     for M, k, E, C, F, dtype, b in ((4096, 8, 64, 2048, 1024, BF16, 2), (333, 2, 7, 1000, 731, F32, 4)):
         pairs = M * k
-        least = pairs * (F * b + C * b + -(-F // 64) * 4)
-        assert least <= size(M, k, E, C, F, dtype) <= least + 3 * 256
+        least = pairs * (F * b + C * (3 if b == 2 else 4) + -(-F // 64) * 4)
+        assert least <= size(M, k, E, C, F, dtype) <= least + 4 * 256
     # Few tokens: fp32 terms, of at most 16 splits.
     assert 8 * 2048 * 4 <= size(1, 8, 64, 2048, 1024, BF16) <= 8 * 2048 * 4 * 16 + 8 * 1024 * 8
 
