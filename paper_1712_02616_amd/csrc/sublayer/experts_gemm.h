@@ -4,6 +4,18 @@
 // The number of rows that an expert has is not known on the host, so that a launch
 // has as many blocks as the worst division of the pairs needs (for each expert one
 // tile that is not full); those past the last tile end at once.
+//
+// Fetch-bound as much as by the matrix cores (busy in 0.38-0.53 of the cycles): an
+// expert's weights serve few rows, so that more of a step's 64 KB comes from HBM.
+// With 512 rows of each of 64 experts, up projection (2048 -> 2x1024) bf16, 254 us
+// before the fetch was cut in two; 239 without the products, 206 without the fetches, 216
+// without the results.  bf16, 8192 tokens, 8 of 64 experts of skewed popularity, 2048
+// -> 1024 (fastest and median of 10 passes): dh 400 and 415 us, dW 310 and 710 (down;
+// gate and up), 330 and 760, dx 540 and 580: 0.69, 0.89, 0.77, 1.0 PFLOP/s; the
+// forward of 4096 tokens 315 and 365 us (up), 213 and 250 (down): 0.87, 0.65.  fp32,
+// 333 tokens, 2 of 7 experts, 1000 -> 731: 41 and 21 us, 48 TFLOP/s, one block of four
+// waves on a CU.  Few tokens (HBM): one token, 8 of 64 experts, 13.5 and 8.7 us, 5.0
+// and 3.9 TB/s; 24 tokens, 4 of 32, 1200 hidden, fp16 57 and 33 us, 5.2 and 4.7.
 #pragma once
 
 #include "ffn_few.h"

@@ -8,7 +8,9 @@
 // pair's place among those is the number of lanes before it with the same expert
 // (found bit by bit of the expert's number).  Up to kPlanPairs pairs are one
 // block and one launch; more are counted by a launch of their own, and every block
-// adds up the counts before its own (blocks*E integers from the caches).
+// adds up the counts before its own (blocks*E integers from the caches).  65536 pairs
+// of 64 experts: 3 and 7 us (16 with one count on its way at a time and blocks of 256
+// threads); 8 pairs 2.5, a launch.
 #include "routed.h"
 
 namespace iabn_impl {
@@ -69,7 +71,7 @@ __device__ __forceinline__ int wave_before(int v, int& total) {
 }
 
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
-    extern __shared__ int32_t next[];  // [waves][E]: where the wave's next pair of e goes
+    extern __shared__ int32_t next[];  // [waves][E]: where the wave's next pair of e goes; [E]
     __shared__ int32_t wave_total[kPlanWaves];
     const int wave = threadIdx.x / kWave;
     int32_t* const own = next + wave * a.E;
@@ -108,7 +110,23 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     int total;
     int at = wave_before(sum, total);
     if (lane_id() == 0) wave_total[wave] = total;
+    int32_t* const sizes = next + kPlanWaves * a.E;
+    if (blockIdx.x == 0)
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (j < each && e0 + j < a.E) sizes[e0 + j] = all[j];
     __syncthreads();
+    // The experts by size, the largest first (of equal ones the lower number): an
+    // expert's place is the number of those before it.
+    if (blockIdx.x == 0)
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int e = e0 + j;
+            if (j >= each || e >= a.E) continue;
+            int rank = 0;
+            for (int i = 0; i < a.E; ++i) rank += sizes[i] > all[j] || (sizes[i] == all[j] && i < e);
+            a.by_size[rank] = e;
+        }
     for (int w = 0; w < wave; ++w) at += wave_total[w];
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
@@ -158,7 +176,7 @@ int64_t blocks_of(int64_t P) {
 
 int64_t plan_size(int64_t P, int64_t E) {
     const int64_t blocks = blocks_of(P);
-    return E + 1 + 2 * P + (blocks > 1 ? blocks * E : 0);
+    return E + 1 + 2 * P + E + (blocks > 1 ? blocks * E : 0);
 }
 
 PlanArgs plan_of(int64_t P, int64_t E, int32_t* plan) {
@@ -167,7 +185,8 @@ PlanArgs plan_of(int64_t P, int64_t E, int32_t* plan) {
     a.offsets = plan;
     a.order = plan + E + 1;
     a.place = a.order + P;
-    a.counts = a.place + P;
+    a.by_size = a.place + P;
+    a.counts = a.by_size + E;
     const int64_t blocks = blocks_of(P), per = (P + blocks - 1) / blocks;
     a.span = static_cast<int32_t>((per + kPlanThreads - 1) / kPlanThreads * kPlanThreads);
     a.blocks = static_cast<int32_t>(P == 0 ? 1 : (P + a.span - 1) / a.span);
@@ -176,7 +195,7 @@ PlanArgs plan_of(int64_t P, int64_t E, int32_t* plan) {
 
 void launch_plan(const PlanArgs& a, hipStream_t st) {
     if (a.blocks > 1) plan_count_kernel<<<a.blocks, kPlanThreads, a.E * sizeof(int32_t), st>>>(a);
-    plan_kernel<<<a.blocks, kPlanThreads, kPlanWaves * a.E * sizeof(int32_t), st>>>(a);
+    plan_kernel<<<a.blocks, kPlanThreads, (kPlanWaves + 1) * a.E * sizeof(int32_t), st>>>(a);
 }
 
 }  // namespace iabn_impl

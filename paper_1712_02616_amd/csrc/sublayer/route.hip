@@ -12,7 +12,14 @@
 // (or with groups), scores next to each other decide: they are formed in 32 bits
 // with a bound of their error, and where two that decide are closer than that, those
 // few are formed and compared in 64 bits.  (That is what one wave in a hundred does;
-// all scores in 64 bits for it (16384, 256) bf16, 8 of 256: 29 us instead of PATH.)
+// all scores in 64 bits for it (16384, 256) bf16, 8 of 256: 29 us instead of 20.)
+//
+// Bound by latency: (16384, 256) bf16, 8 of 256 by sigmoids with a bias in 4 of 8
+// groups, 20 us for 9.5 MB (17.6 with no close scores; 12.5 of them without the groups, 12.2 with
+// one choice); four waves a SIMD go through load, scores, groups and choices once.
+// Rows in 16 lanes share the instructions of the maxima (in 64 lanes: 27 us, the
+// (4099, 61) fp32 case 4.4 instead of 3.7; the backward 9.7 instead of 7.6).  One
+// row: 2.6 us, a launch.
 #include <type_traits>
 #include <utility>
 
@@ -467,6 +474,10 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
 }
 
 // ---------------------------------------------------------------- backward
+//
+// (16384, 256) bf16, 8 of 256, not renormalised: 7.6 us for 18 MB, vector arithmetic
+// in 0.64 of the busy cycles (a precise exponential for every logit; 11.7 us where
+// each lane compared each choice with each of its experts, and with a division).
 //
 //   d_j = scale*dw_j;  softmax: dl = s*(d - sum of s_j d_j), d = 0 for what was not
 //   chosen; sigmoid: dl = d*s*(1 - s).  Renormalised, p_j = s_j/sum of the chosen s:

@@ -40,11 +40,11 @@ bool launch_route_bwd(int dtype, const RouteBwdArgs& a, hipStream_t st);
 
 // ---------------------------------------------------------------- the plan
 
-// int32: offsets [E + 1], order [P], place [P], and where several blocks count,
-// their counts [blocks][E].
+// int32: offsets [E + 1], order [P], place [P], the experts by size [E], and where
+// several blocks count, their counts [blocks][E].
 struct PlanArgs {
     const int32_t* experts;  // [P]
-    int32_t *offsets, *order, *place, *counts;
+    int32_t *offsets, *order, *place, *by_size, *counts;
     int32_t P, E;
     int32_t blocks, span;    // pairs of a block
 };

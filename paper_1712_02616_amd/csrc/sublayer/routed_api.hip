@@ -80,7 +80,7 @@ ExpertsSpace experts_space(int64_t M, int64_t k, int64_t E, int64_t C, int64_t F
 GroupArgs group_args(const PlanArgs& plan, const float* weights, int64_t k, int64_t C, int64_t F, int act,
                      float slope) {
     GroupArgs a = {};
-    a.offsets = plan.offsets, a.order = plan.order, a.weights = weights;
+    a.offsets = plan.offsets, a.order = plan.order, a.by_size = plan.by_size, a.weights = weights;
     a.top = iabn_divmagic_make(static_cast<uint32_t>(k));
     a.E = plan.E, a.P = plan.P;
     a.expert_stride = C * F;

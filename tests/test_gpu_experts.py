@@ -38,6 +38,8 @@ def check_plan(experts, E):
     assert plan[E + 1:E + 1 + len(order)] == order
     assert all(v == -99 for v in plan[E + 1 + len(order):E + 1 + P])  # left as it was
     assert plan[E + 1 + P:E + 1 + 2 * P] == place
+    sizes = [offsets[e + 1] - offsets[e] for e in range(E)]
+    assert plan[E + 1 + 2 * P:2 * E + 1 + 2 * P] == sorted(range(E), key=lambda e: (-sizes[e], e))
 
 
 @pytest.mark.parametrize("M,k,E", [(1, 1, 1), (1, 8, 64), (3, 2, 5), (100, 3, 7), (255, 8, 64), (256, 8, 64), (257, 8, 64),
@@ -307,6 +309,17 @@ def test_a_wrong_plan_stays_inside():
             iabn.iabn_experts_forward(x, plan, w[:rows].contiguous(), dev["w_gate"], dev["w_up"], dev["w_down"], y)
             torch.cuda.synchronize()
             intact("y")
+            outs = [torch.empty_like(x), torch.empty_like(w[:rows])]
+            dws = [guarded((E * F, C), torch.bfloat16, 0) for _ in range(3)]
+            gu = [torch.zeros(rows * k, F, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+            for by_size in (wrong, 0):  # (the experts by size)
+                plan[E + 1 + 2 * rows * k:2 * E + 1 + 2 * rows * k] = by_size
+                iabn.iabn_experts_backward(x, x, plan, w[:rows].contiguous(), *gu[:2], dev["w_gate"], dev["w_up"],
+                                           dev["w_down"], *outs, *gu[2:], dws[0][0].view(E, F, C), dws[1][0].view(E, F, C),
+                                           dws[2][0].view(E, C, F))
+                torch.cuda.synchronize()
+                for _, ok in dws:
+                    ok("dw")
             plan[:E + 1] = torch.tensor([wrong, 3, -7, 1 << 29, M * k + 5], dtype=torch.int32)
             iabn.iabn_experts_forward(x, plan, w[:rows].contiguous(), dev["w_gate"], dev["w_up"], dev["w_down"], y)
             torch.cuda.synchronize()

@@ -60,10 +60,10 @@ def test_plan_refuses(lib):  # noqa: F811
 
 def test_plan_size(lib):  # noqa: F811
     size = lib.iabn_experts_plan_size
-    assert size(0, 2, 4) == 5 and size(6, 0, 4) == 5
-    assert size(4, 2, 16) == 17 + 16
+    assert size(0, 2, 4) == 5 + 4 and size(6, 0, 4) == 5 + 4
+    assert size(4, 2, 16) == 17 + 16 + 16
     for M, k, E in ((1, 8, 64), (4096, 8, 64), (100000, 8, 1000), (1 << 25, 32, 1024)):
-        assert E + 1 + 2 * M * k <= size(M, k, E) <= E + 1 + 2 * M * k + 256 * E
+        assert 2 * E + 1 + 2 * M * k <= size(M, k, E) <= 2 * E + 1 + 2 * M * k + 256 * E
     assert size(-1, 2, 4) == size(4, 65, 4) == size(4, 2, 0) == size(4, 2, 1025) == size(1 << 25, 64, 8) == 0
 
 
