@@ -111,22 +111,23 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     int at = wave_before(sum, total);
     if (lane_id() == 0) wave_total[wave] = total;
     int32_t* const sizes = next + kPlanWaves * a.E;
-    if (blockIdx.x == 0)
 #pragma unroll
-        for (int j = 0; j < kEach; ++j)
-            if (j < each && e0 + j < a.E) sizes[e0 + j] = all[j];
+    for (int j = 0; j < kEach; ++j)
+        if (j < each && e0 + j < a.E) sizes[e0 + j] = all[j];
     __syncthreads();
-    // The experts by size, the largest first (of equal ones the lower number): an
-    // expert's place is the number of those before it.
-    if (blockIdx.x == 0)
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-            const int e = e0 + j;
-            if (j >= each || e >= a.E) continue;
-            int rank = 0;
-            for (int i = 0; i < a.E; ++i) rank += sizes[i] > all[j] || (sizes[i] == all[j] && i < e);
-            a.by_size[rank] = e;
-        }
+    // The experts by size, the largest first (of equal ones the lower number), a wave
+    // for each: its place is the number of those before it.  Of few pairs, which one
+    // block counts, they stay in their order.
+    for (int e = blockIdx.x * kPlanWaves + wave; e < a.E; e += a.blocks * kPlanWaves) {
+        const int mine = sizes[e];
+        int rank = a.blocks == 1 ? e : 0;
+        if (a.blocks > 1)
+            for (int base = 0; base < a.E; base += kWave) {
+                const int i = base + static_cast<int>(lane_id()), n = i < a.E ? sizes[i] : -1;
+                rank += __popcll(__ballot(n > mine || (n == mine && i < e)));
+            }
+        if (lane_id() == 0) a.by_size[rank] = e;
+    }
     for (int w = 0; w < wave; ++w) at += wave_total[w];
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
