@@ -19,7 +19,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
-# csrc/: InPlace-ABN; csrc/sublayer/: the feed-forward sublayer.
+# csrc/: InPlace-ABN; csrc/sublayer/: the feed-forward sublayer, routed experts, clipping.
 SOURCES = sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "sublayer", "*.hip")))
 HEADERS = sorted(glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "sublayer", "*.h"))) + [
     os.path.join(ROOT, "include", "iabn.h")]
