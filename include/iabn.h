@@ -557,8 +557,8 @@ int iabn_experts_plan(const int32_t *experts, int32_t *plan, int64_t M, int64_t 
  *                  plan (rows past its last are not written), which the backward
  *                  takes, or both NULL (inference).
  *   act, slope     as in iabn_ffn_forward.
- *   C, F           at most 2^17; no tensor of more than 2^35 elements.  Where C or F
- *                  or k is 0, y (and g, u) are 0.
+ *   C, F           at most 2^17; no tensor of more than 2^35 elements, M*k at most
+ *                  2^29.  Where C or F or k is 0, y (and g, u) are 0.
  * Products are summed in fp32 (matrix cores).  Between the kernels h (and dg, du)
  * are rounded to the storage type, and each pair's term of y and dx to no fewer than
  * 16 digits of fp32's 24, with its range.
@@ -604,7 +604,9 @@ int iabn_experts_backward(const void *dy, const void *x, const int32_t *plan, co
  *
  * iabn_grad_clip: out = g*min(1, max_norm/(norm[0] + 1e-6)).
  *   outs           of the gradients' types and sizes; outs[i] may be grads[i], which
- *                  is then not touched where nothing is clipped.
+ *                  is then not touched where nothing is clipped.  Two outputs
+ *                  that overlap (a tensor that the list has twice) are
+ *                  IABN_ERR_PARAM; nor may outs[i] overlap another's grads[j].
  *   max_norm       >= 0 (inf: no clipping).  A norm that is NaN makes every output
  *                  NaN.
  */

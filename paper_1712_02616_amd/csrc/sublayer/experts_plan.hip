@@ -10,7 +10,7 @@
 // block and one launch; more are counted by a launch of their own, and every block
 // adds up the counts before its own (blocks*E integers from the caches).  65536 pairs
 // of 64 experts: 3 and 7 us (16 with one count on its way at a time and blocks of 256
-// threads); 8 pairs 2.5, a launch.
+// threads); 8 pairs 3.3, a launch.
 #include "routed.h"
 
 namespace iabn_impl {

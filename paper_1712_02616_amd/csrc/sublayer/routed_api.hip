@@ -2,7 +2,10 @@
 // (include/iabn.h): argument validation on the host before any launch, and the
 // entry points themselves.
 
+#include <algorithm>
 #include <cmath>
+#include <memory>
+#include <new>
 
 #include "checks.h"
 #include "groups.h"
@@ -16,6 +19,8 @@ constexpr int64_t kMaxGroups = 64;
 // Widths and elements of the products' matrices (so that their tiles fit a launch).
 constexpr int64_t kMaxExpertWidth = int64_t(1) << 17;
 constexpr int64_t kMaxExpertElems = int64_t(1) << 35;
+// (2^30 pairs in tiles of 64 rows, 256 threads each, would be 2^32 threads.)
+constexpr int64_t kMaxExpertPairs = int64_t(1) << 29;
 
 int check_pairs(int64_t M, int64_t k, int64_t E) {
     if (M < 0 || M > kMaxRouteRows)
@@ -45,6 +50,7 @@ int check_experts(int dtype, int act, float slope, int64_t M, int64_t k, int64_t
     if (rc) return rc;
     if (C < 0 || F < 0 || C > kMaxExpertWidth || F > kMaxExpertWidth)
         return fail(IABN_ERR_SHAPE, "C=%lld or F=%lld is not in [0, 2^17]", (long long)C, (long long)F);
+    if (M * k > kMaxExpertPairs) return fail(IABN_ERR_SHAPE, "M*k exceeds 2^29");
     const int64_t rows = k > 1 ? M * k : M;
     if (rows * C > kMaxExpertElems || rows * F > kMaxExpertElems || E * C * F > kMaxExpertElems)
         return fail(IABN_ERR_SHAPE, "a matrix of M=%lld, k=%lld, E=%lld, C=%lld, F=%lld exceeds 2^35 elements",
@@ -142,6 +148,31 @@ int check_grad_tensors(const void* const* grads, const void* const* outs, bool w
         if (sizes[i] > 0 && (!grads[i] || (with_outs && !outs[i])))
             return fail(IABN_ERR_NULL, "tensor %lld is NULL", (long long)i);
     }
+    return IABN_OK;
+}
+
+// No two outputs may share an element: which of the two wrote it last would be
+// chance, and in place it would be scaled once or twice.
+int check_apart(void* const* outs, const int* dtypes, const int64_t* sizes, int64_t count) {
+    struct Span {
+        uintptr_t begin, end;
+    };
+    Span few[kGradTensors];
+    std::unique_ptr<Span[]> many;
+    if (count > kGradTensors) {
+        many.reset(new (std::nothrow) Span[count]);
+        if (!many) return fail(IABN_ERR_SHAPE, "no memory to look through %lld tensors", (long long)count);
+    }
+    Span* const spans = many ? many.get() : few;
+    int64_t n = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        if (sizes[i] == 0) continue;
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(outs[i]);
+        spans[n++] = {begin, begin + static_cast<uintptr_t>(sizes[i]) * elem_bytes(dtypes[i])};
+    }
+    std::sort(spans, spans + n, [](const Span& a, const Span& b) { return a.begin < b.begin; });
+    for (int64_t i = 1; i < n; ++i)
+        if (spans[i].begin < spans[i - 1].end) return fail(IABN_ERR_PARAM, "two outputs overlap");
     return IABN_OK;
 }
 
@@ -381,6 +412,7 @@ int iabn_grad_clip(const void* const* grads, void* const* outs, const int* dtype
     if (!(max_norm >= 0.0f)) return fail(IABN_ERR_PARAM, "max_norm=%g must be >= 0", max_norm);
     if (list.pieces == 0) return ok();
     if (!norm) return fail(IABN_ERR_NULL, "norm is NULL");
+    if ((rc = check_apart(outs, dtypes, sizes, count))) return rc;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     over_grads(grads, outs, dtypes, sizes, count, list.piece, [&](GradArgs& a) {
         a.norm = norm, a.max_norm = max_norm;

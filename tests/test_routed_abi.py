@@ -104,6 +104,17 @@ def test_experts_refuse(lib):  # noqa: F811
     assert forward(lib, M=0, x=None, y=None, ws=None) == OK
 
 
+@no_gpu
+def test_experts_refuse_more_pairs_than_a_launch_has_tiles_for(lib):  # noqa: F811
+    # 2^30 pairs in tiles of 64 rows, 256 threads each, would be 2^32 threads.
+    for M, k in (((1 << 23) + 1, 64), (1 << 25, 17), (1 << 25, 32)):
+        many = dict(M=M, k=k, E=64, C=1, F=1, ws_bytes=1 << 45)
+        refused(lib, ERR_SHAPE, forward(lib, **many))
+        refused(lib, ERR_SHAPE, backward(lib, **many))
+        assert lib.iabn_experts_workspace_size(M, k, 64, 1, 1, F16) == 0
+    assert lib.iabn_experts_workspace_size(1 << 23, 64, 64, 1, 1, F16) > 0
+
+
 def test_experts_workspace(lib):  # noqa: F811
     size = lib.iabn_experts_workspace_size
     assert size(-1, 2, 8, 16, 24, F16) == size(4, 2, 8, 16, 24, 9) == size(4, 2, 8, 1 << 18, 24, F16) == 0
@@ -146,6 +157,23 @@ def test_grads_refuse(lib):  # noqa: F811
     assert clip(None, None, None, None, 0, None, 1.0, None) == OK
     p0, d0, s0 = grads(sizes=(0, 0), at=None)
     assert clip(p0, p0, d0, s0, 2, None, INF, None) == OK
+
+
+@no_gpu
+def test_clip_refuses_an_output_twice(lib):  # noqa: F811
+    # Elements that two tensors write would be scaled once or twice, by chance.
+    def outs(pairs, dtype=F32):
+        n = len(pairs)
+        at = (ctypes.c_void_p * n)(*[p for p, _ in pairs])
+        return at, at, (ctypes.c_int * n)(*[dtype] * n), (ctypes.c_int64 * n)(*[c for _, c in pairs]), n, P, 1.0
+
+    apart = [(1 << 20, 8), (1 << 12, 8)]
+    for wrong in (apart + [(1 << 20, 8)], apart + [((1 << 20) + 28, 4)], apart + [((1 << 20) - 4, 2)],
+                  [((1 << 20) + 64 * i, 16) for i in range(300)] + [((1 << 20) + 64 * 17, 1)],
+                  [(1 << 20, 16), ((1 << 20) + 8, 1), ((1 << 20) + 32, 1)]):
+        refused(lib, ERR_PARAM, lib.iabn_grad_clip(*outs(wrong), None))
+    # (Empty ones lie nowhere.)
+    assert lib.iabn_grad_clip(*outs([(1 << 20, 0)] * 3), None) == OK
 
 
 def test_grads_workspace(lib):  # noqa: F811
