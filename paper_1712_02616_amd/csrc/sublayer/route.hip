@@ -171,7 +171,9 @@ __device__ __forceinline__ void wave_fence() {
 // The groups that a row keeps, a bit each.  t: the scores in LDS, -inf for what
 // may not be chosen; gs: a place for the groups' scores.  32-bit scores are off by
 // at most `tol` and their own roundings, a group's by twice that: `sure` turns false
-// where it could change which groups are kept.
+// where it could change which groups are kept.  Two scores that cancel in a group's
+// keep their roundings, 2^-24 of each: they are bounded by the sum of their sizes,
+// which stands behind the groups' scores.
 template <int L, typename S>
 __device__ __forceinline__ uint64_t kept_groups(const RouteArgs& a, const S* t, S* gs, int lane, S tol, bool& sure) {
     // A group belongs to `per_group` lanes, which look through it in turn.
@@ -201,33 +203,44 @@ __device__ __forceinline__ uint64_t kept_groups(const RouteArgs& a, const S* t, 
             top1 = larger(top1, o1);
         }
     }
-    if (a.group_top == 2 && top2 > none) top1 += top2;
-    if (g < a.groups && part == 0) gs[g] = top1;
+    S size = top1 < 0 ? -top1 : top1;
+    if (a.group_top == 2 && top2 > none) {
+        size += top2 < 0 ? -top2 : top2;
+        top1 += top2;
+    }
+    constexpr bool kNarrow = sizeof(S) == 4;  // (half of the place is for the sizes)
+    if (g < a.groups && part == 0) {
+        gs[g] = top1;
+        if constexpr (kNarrow) gs[a.groups + g] = size;
+    }
     wave_fence();
     bool keep = false, clear = true;
     if (lane < a.groups) {
-        const S mine = gs[lane];
+        const S mine = gs[lane], my_size = kNarrow ? gs[a.groups + lane] : S(0);
         // How many are above, and how many surely are, and may be.
         int above = 0, surely = 0, maybe = 0;
         for (int i0 = 0; i0 < a.groups; i0 += kReads) {
-            S others[kReads];
+            S others[kReads], sizes[kReads];
 #pragma unroll
-            for (int q = 0; q < kReads; ++q) others[q] = gs[min(i0 + q, a.groups - 1)];
+            for (int q = 0; q < kReads; ++q) {
+                others[q] = gs[min(i0 + q, a.groups - 1)];
+                if constexpr (kNarrow) sizes[q] = gs[a.groups + min(i0 + q, a.groups - 1)];
+            }
 #pragma unroll
             for (int q = 0; q < kReads; ++q) {
                 const int i = i0 + q;
                 const S other = others[q];
                 const bool is = i < a.groups && i != lane;
                 above += is && (other > mine || (other == mine && i < lane));
-                if constexpr (sizeof(S) == 4) {
-                    const S far = 4.0f * tol + 0x1p-22f * (fabsf(mine) + fabsf(other));
+                if constexpr (kNarrow) {
+                    const S far = 4.0f * tol + 0x1p-22f * (my_size + sizes[q]);
                     surely += is && other - mine > far;
                     maybe += is && other - mine > -far;
                 }
             }
         }
         keep = above < a.kept && mine > none;
-        if constexpr (sizeof(S) == 4) clear = mine == none || maybe < a.kept || surely >= a.kept;
+        if constexpr (kNarrow) clear = mine == none || maybe < a.kept || surely >= a.kept;
     }
     sure = sure && __ballot(!clear) == 0;
     const uint64_t all = __ballot(keep);
