@@ -20,6 +20,7 @@
 // Rows in 16 lanes share the instructions of the maxima (in 64 lanes: 27 us, the
 // (4099, 61) fp32 case 4.4 instead of 3.7; the backward 9.7 instead of 7.6).  One
 // row: 2.6 us, a launch.
+#include <limits>
 #include <type_traits>
 #include <utility>
 
@@ -173,7 +174,9 @@ __device__ __forceinline__ void wave_fence() {
 // at most `tol` and their own roundings, a group's by twice that: `sure` turns false
 // where it could change which groups are kept.  Two scores that cancel in a group's
 // keep their roundings, 2^-24 of each: they are bounded by the sum of their sizes,
-// which stands behind the groups' scores.
+// which stands behind the groups' scores.  Where that is past fp32's range no
+// difference is above it and nothing is sure; a group's score is no less than the
+// lowest number, -inf only where the group has nothing.
 template <int L, typename S>
 __device__ __forceinline__ uint64_t kept_groups(const RouteArgs& a, const S* t, S* gs, int lane, S tol, bool& sure) {
     // A group belongs to `per_group` lanes, which look through it in turn.
@@ -203,10 +206,10 @@ __device__ __forceinline__ uint64_t kept_groups(const RouteArgs& a, const S* t, 
             top1 = larger(top1, o1);
         }
     }
-    S size = top1 < 0 ? -top1 : top1;
+    S size = top1 == none ? S(0) : top1 < 0 ? -top1 : top1;
     if (a.group_top == 2 && top2 > none) {
         size += top2 < 0 ? -top2 : top2;
-        top1 += top2;
+        top1 = larger(top1 + top2, std::numeric_limits<S>::lowest());
     }
     constexpr bool kNarrow = sizeof(S) == 4;  // (half of the place is for the sizes)
     if (g < a.groups && part == 0) {
@@ -235,7 +238,7 @@ __device__ __forceinline__ uint64_t kept_groups(const RouteArgs& a, const S* t, 
                 if constexpr (kNarrow) {
                     const S far = 4.0f * tol + 0x1p-22f * (my_size + sizes[q]);
                     surely += is && other - mine > far;
-                    maybe += is && other - mine > -far;
+                    maybe += is && !(mine - other > far);
                 }
             }
         }

@@ -1,5 +1,5 @@
-"""Groups whose score is a sum of two that cancel: the groups that iabn_route_forward
-keeps are those of 64-bit sums.
+"""Groups whose score is a sum of two that cancel, or that leaves fp32's range: the
+groups that iabn_route_forward keeps are those of 64-bit sums.
 
 A score plus a bias of B is off by B*2^-24 in fp32, however small the sum of two such
 values is; sums that differ by less than that have to be told apart all the same."""
@@ -12,6 +12,7 @@ import torch
 import routed_oracle as routed
 from test_gpu_route import run
 
+INF = float("inf")
 pytestmark = [pytest.mark.gpu,
               pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a HIP GPU")]
 
@@ -65,3 +66,18 @@ def test_sums_that_are_equal(M, B):
         b[2 * biased], b[2 * biased + 1] = B, -B
         got, _ = run(torch.zeros(M, 4), 2, bias=b, score="sigmoid", groups=2, kept=1, group_top=2)
         assert (got == torch.tensor([0, 1])).all()
+
+
+@pytest.mark.parametrize("M", [5, 1100])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_sums_past_fp32(M, sign):
+    """Two biases whose sum is past fp32's range: the groups are still in their order,
+    and one below that range is not one with nothing in it."""
+    b = sign * torch.tensor([2.5, 2.5, 3.0, 3.0, 2.0, 2.0]) * 1e38
+    l = torch.zeros(M, 6)
+    for kept in (1, 2):
+        got, _ = run(l, 2 * kept, bias=b, score="sigmoid", groups=3, kept=kept, group_top=2)
+        assert (got >= 0).all()
+    l[:, :2] = -INF
+    got, _ = run(l, 4, bias=b, score="sigmoid", groups=3, kept=2, group_top=2)
+    assert (got >= 2).all()
