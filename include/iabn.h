@@ -597,18 +597,19 @@ int iabn_experts_backward(const void *dy, const void *x, const int32_t *plan, co
  *
  * iabn_grad_norm: norm[0] = sqrt(sum over all tensors of g^2), fp32 on the device.
  * Squares and sums are 64-bit, in a fixed order: no square overflows.  No tensors: 0.
- * An infinity gives inf, a NaN NaN.  Ranks of one training step that hold different
- * tensors add up norm^2 between the two calls.  The workspace holds
- * iabn_grad_norm_workspace_size(sizes, count) bytes (0 for an invalid list), 16-byte
- * aligned.
+ * An infinity gives inf, and so does a norm past fp32's range; a NaN NaN.  Ranks of
+ * one training step that hold different tensors add up norm^2 between the two calls.
+ * The workspace holds iabn_grad_norm_workspace_size(sizes, count) bytes (0 for an
+ * invalid list), 16-byte aligned.
  *
  * iabn_grad_clip: out = g*min(1, max_norm/(norm[0] + 1e-6)).
  *   outs           of the gradients' types and sizes; outs[i] may be grads[i], which
  *                  is then not touched where nothing is clipped.  Two outputs
  *                  that overlap (a tensor that the list has twice) are
  *                  IABN_ERR_PARAM; nor may outs[i] overlap another's grads[j].
- *   max_norm       >= 0 (inf: no clipping).  A norm that is NaN makes every output
- *                  NaN.
+ *   max_norm       >= 0; inf: no clipping, of an infinite norm neither (any other
+ *                  max_norm then makes finite gradients 0).  A norm that is NaN
+ *                  makes every output NaN.
  */
 size_t iabn_grad_norm_workspace_size(const int64_t *sizes, int64_t count);
 

@@ -100,8 +100,10 @@ __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradArgs a) {
     // bf16 values: 277 us, and 132 for the norm; 309 and 118 where the norm's loads
     // are non-temporal.)
     const int t = tensor_of(a, gridDim.x - 1 - blockIdx.x, from, to);
-    const double ratio = static_cast<double>(a.max_norm) / (static_cast<double>(*a.norm) + 1e-6);
-    const float factor = ratio >= 1.0 ? 1.0f : static_cast<float>(ratio);  // (a NaN stays one)
+    const double norm = *a.norm, limit = a.max_norm;
+    // (No limit clips nothing, an infinite norm neither; a NaN stays one.)
+    const double ratio = limit == __builtin_inf() && norm == norm ? 1.0 : limit / (norm + 1e-6);
+    const float factor = ratio >= 1.0 ? 1.0f : static_cast<float>(ratio);
     if (factor == 1.0f && a.in[t] == a.out[t]) return;
     switch (a.dtype[t]) {
         case IABN_F32: scale<IABN_F32>(a.in[t], a.out[t], from, to, factor); break;
