@@ -82,14 +82,15 @@ __global__ __launch_bounds__(kThreads) void grad_join_kernel(const double* part,
     if (threadIdx.x == 0) *norm = static_cast<float>(sqrt(sum));
 }
 
+// By factor*2^power.
 template <int DT>
-__device__ __forceinline__ void scale(const void* in, void* out, int64_t from, int64_t to, float factor) {
+__device__ __forceinline__ void scale(const void* in, void* out, int64_t from, int64_t to, float factor, int power) {
     for (int64_t at = from + int64_t(threadIdx.x) * kChunk; at < to; at += kThreads * kChunk) {
         const int n = static_cast<int>(min(to - at, int64_t(kChunk)));
         float v[kChunk];
         widen<DT>(load_chunk<DT, kStream>(in, at, n), v);
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) v[j] *= factor;
+        for (int j = 0; j < kChunk; ++j) v[j] = ldexpf(v[j] * factor, power);
         store_chunk<DT, kStream>(out, at, n, v);
     }
 }
@@ -103,12 +104,15 @@ __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradArgs a) {
     const double norm = *a.norm, limit = a.max_norm;
     // (No limit clips nothing, an infinite norm neither; a NaN stays one.)
     const double ratio = limit == __builtin_inf() && norm == norm ? 1.0 : limit / (norm + 1e-6);
-    const float factor = ratio >= 1.0 ? 1.0f : static_cast<float>(ratio);
-    if (factor == 1.0f && a.in[t] == a.out[t]) return;
+    // (Below 2^-126 an fp32 factor would have fewer digits: the power of two is apart.)
+    int power = 0;
+    const double digits = ratio > 0.0 && ratio < 0x1p-126 ? frexp(ratio, &power) : ratio;
+    const float factor = ratio >= 1.0 ? 1.0f : static_cast<float>(digits);
+    if (factor == 1.0f && power == 0 && a.in[t] == a.out[t]) return;
     switch (a.dtype[t]) {
-        case IABN_F32: scale<IABN_F32>(a.in[t], a.out[t], from, to, factor); break;
-        case IABN_F16: scale<IABN_F16>(a.in[t], a.out[t], from, to, factor); break;
-        default: scale<IABN_BF16>(a.in[t], a.out[t], from, to, factor); break;
+        case IABN_F32: scale<IABN_F32>(a.in[t], a.out[t], from, to, factor, power); break;
+        case IABN_F16: scale<IABN_F16>(a.in[t], a.out[t], from, to, factor, power); break;
+        default: scale<IABN_BF16>(a.in[t], a.out[t], from, to, factor, power); break;
     }
 }
 
