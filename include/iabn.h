@@ -604,9 +604,10 @@ int iabn_experts_backward(const void *dy, const void *x, const int32_t *plan, co
  *
  * iabn_grad_clip: out = g*min(1, max_norm/(norm[0] + 1e-6)).
  *   outs           of the gradients' types and sizes; outs[i] may be grads[i], which
- *                  is then not touched where nothing is clipped.  Two outputs
- *                  that overlap (a tensor that the list has twice) are
- *                  IABN_ERR_PARAM; nor may outs[i] overlap another's grads[j].
+ *                  is then not touched where nothing is clipped.  IABN_ERR_PARAM:
+ *                  two outputs that overlap (a tensor that the list has twice),
+ *                  an output that overlaps another's gradient or norm, or its own
+ *                  gradient in part.
  *   max_norm       >= 0; inf: no clipping, of an infinite norm neither (any other
  *                  max_norm then makes finite gradients 0).  A norm that is NaN
  *                  makes every output NaN.

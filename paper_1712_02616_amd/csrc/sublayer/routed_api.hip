@@ -152,10 +152,16 @@ int check_grad_tensors(const void* const* grads, const void* const* outs, bool w
 }
 
 // No two outputs may share an element: which of the two wrote it last would be
-// chance, and in place it would be scaled once or twice.
-int check_apart(void* const* outs, const int* dtypes, const int64_t* sizes, int64_t count) {
+// chance, and in place it would be scaled once or twice.  Nor may an output lie over
+// what other blocks read: a gradient, but for its own in the same place, or the norm.
+int check_apart(const void* const* grads, void* const* outs, const int* dtypes, const int64_t* sizes, int64_t count,
+                const float* norm) {
     struct Span {
         uintptr_t begin, end;
+    };
+    const auto span_at = [](const void* p, size_t bytes) {
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(p);
+        return Span{begin, begin + bytes};
     };
     Span few[kGradTensors];
     std::unique_ptr<Span[]> many;
@@ -167,12 +173,22 @@ int check_apart(void* const* outs, const int* dtypes, const int64_t* sizes, int6
     int64_t n = 0;
     for (int64_t i = 0; i < count; ++i) {
         if (sizes[i] == 0) continue;
-        const uintptr_t begin = reinterpret_cast<uintptr_t>(outs[i]);
-        spans[n++] = {begin, begin + static_cast<uintptr_t>(sizes[i]) * elem_bytes(dtypes[i])};
+        spans[n++] = span_at(outs[i], static_cast<size_t>(sizes[i]) * elem_bytes(dtypes[i]));
     }
     std::sort(spans, spans + n, [](const Span& a, const Span& b) { return a.begin < b.begin; });
     for (int64_t i = 1; i < n; ++i)
         if (spans[i].begin < spans[i - 1].end) return fail(IABN_ERR_PARAM, "two outputs overlap");
+    // (Of spans apart, the last one that begins before the end is the one to look at.)
+    const auto meets_an_output = [&](const Span& s) {
+        const Span* const after = std::lower_bound(spans, spans + n, s.end,
+                                                   [](const Span& o, uintptr_t end) { return o.begin < end; });
+        return after != spans && after[-1].end > s.begin;
+    };
+    for (int64_t i = 0; i < count; ++i)
+        if (sizes[i] > 0 && grads[i] != outs[i] &&
+            meets_an_output(span_at(grads[i], static_cast<size_t>(sizes[i]) * elem_bytes(dtypes[i]))))
+            return fail(IABN_ERR_PARAM, "an output overlaps tensor %lld", (long long)i);
+    if (meets_an_output(span_at(norm, sizeof(float)))) return fail(IABN_ERR_PARAM, "an output overlaps norm");
     return IABN_OK;
 }
 
@@ -412,7 +428,7 @@ int iabn_grad_clip(const void* const* grads, void* const* outs, const int* dtype
     if (!(max_norm >= 0.0f)) return fail(IABN_ERR_PARAM, "max_norm=%g must be >= 0", max_norm);
     if (list.pieces == 0) return ok();
     if (!norm) return fail(IABN_ERR_NULL, "norm is NULL");
-    if ((rc = check_apart(outs, dtypes, sizes, count))) return rc;
+    if ((rc = check_apart(grads, outs, dtypes, sizes, count, norm))) return rc;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     over_grads(grads, outs, dtypes, sizes, count, list.piece, [&](GradArgs& a) {
         a.norm = norm, a.max_norm = max_norm;

@@ -247,7 +247,8 @@ def iabn_grad_norm(grads, norm, workspace=None, stream=None):
 
 def iabn_grad_clip(grads, outs, norm, max_norm, stream=None):
     """outs = grads * min(1, max_norm/(norm[0] + 1e-6)), tensor by tensor; ``outs`` may
-    be ``grads``, and no two of them overlap.  Returns ``outs``."""
+    be ``grads``.  No two of them overlap, nor does one overlap another's gradient or
+    ``norm``.  Returns ``outs``."""
     if not isinstance(grads, (list, tuple)):
         grads = list(grads)
     if not isinstance(outs, (list, tuple)):

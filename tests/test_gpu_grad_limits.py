@@ -69,3 +69,16 @@ def test_a_small_factor_is_no_factor_of_one(norm):
     for in_place in (False, True):
         got = clip([g.cuda()], norm, 2.0 ** -140, in_place)[0]
         oracle.check("norm %g" % norm, got, v, 2 * U32 * v.abs() + 2.0 ** -150, torch.float32)
+
+
+def test_refuses_outputs_over_what_it_reads():
+    x = torch.ones(64, device="cuda")
+    a, b, norm = x[:16], x[16:32], torch.full((1,), 3.0, device="cuda")
+    for grads, outs, n in (([a, b], [b, a], norm), ([a], [x[1:17]], norm), ([a], [b], x[31:32]), ([a], [a], x[:1]),
+                           ([a, x[8:24]], [a, x[40:56]], norm)):
+        with pytest.raises(iabn.IabnError) as e:
+            iabn.iabn_grad_clip(grads, outs, n, 1.0)
+        assert e.value.status == 3
+    assert (x == 1).all()
+    outs = iabn.iabn_grad_clip([a, b, a], [a.clone(), b, x[32:48]], norm, 1.0)
+    assert all(torch.equal(o, outs[0]) for o in outs) and (x[:16] == 1).all() and (x[48:] == 1).all()
