@@ -501,11 +501,14 @@ typedef enum { IABN_SCORE_SOFTMAX = 0, IABN_SCORE_SIGMOID = 1 } iabn_score_t;
  *                  the experts are `groups` (at most 64, dividing E) groups of
  *                  consecutive ones, and only the groups_kept of them with the
  *                  highest sums of their group_top (1 or 2) highest c are chosen
- *                  from; groups_kept = groups leaves them all.
+ *                  from; groups_kept = groups leaves them all.  A group with fewer
+ *                  experts that are not switched off has the sum of those, one
+ *                  with none is not kept.
  *   scale          finite.               k  at most E.
  * Of equal ones the lower index comes first.  Without a bias the order of c is
- * that of the logits; otherwise, and for the groups, scores are formed and compared
- * in 64 bits.  A logit or a bias of -inf switches an expert off: it is not chosen,
+ * that of the logits; otherwise, and for the groups, it is that of scores and sums
+ * formed in 64 bits (in 32 where a bound of their error shows that the order is the
+ * same).  A logit or a bias of -inf switches an expert off: it is not chosen,
  * whatever is left, and a slot for which nothing is left has the expert -1 and the
  * weight 0.  A NaN is above every number, so that it shows in the weights.
  * Renormalised weights do not depend on the size of the scores (a row whose
