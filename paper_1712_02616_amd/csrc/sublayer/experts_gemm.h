@@ -13,7 +13,7 @@
 // -> 1024 (fastest and median of 10 passes): dh 400 and 415 us, dW 310 and 710 (down;
 // gate and up), 330 and 760, dx 540 and 580: 0.69, 0.89, 0.77, 1.0 PFLOP/s; the
 // forward of 4096 tokens 315 and 365 us (up), 213 and 250 (down): 0.87, 0.65.  fp32,
-// 333 tokens, 2 of 7 experts, 1000 -> 731: 41 and 21 us, 48 TFLOP/s, one block of four
+// 333 tokens, 2 of 7 experts, 1000 -> 731: 43 and 22 us, 46 TFLOP/s, one block of four
 // waves on a CU.  Few tokens (HBM): one token, 8 of 64 experts, 13.5 and 8.7 us, 5.0
 // and 3.9 TB/s; 24 tokens, 4 of 32, 1200 hidden, fp16 57 and 33 us, 5.2 and 4.7.
 #pragma once
