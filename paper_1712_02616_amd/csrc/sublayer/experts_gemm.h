@@ -92,6 +92,12 @@ void launch_group_few_tiles(GroupArgs a, hipStream_t st) {
     const int64_t blocks = (a.N + 15) / 16 * most_tiles(a.P, a.E, MT * 16), lines = (a.K + kLine - 1) / kLine;
     int waves = MT;
     while (waves < 8 && blocks * a.splits * waves < 2048 && waves * 2 * kFewLines * a.splits <= lines) waves *= 2;
+    // In fp32 no wave adds more than 256 terms of up to 2048 (then their share): y of 16
+    // tokens, 6 of 84 experts (1512 -> 688), is off by 4.5e-7 in root mean square instead
+    // of 1.1e-6, in 164 us instead of 153; of 24 tokens, 8 of 64 (1024 -> 1024), 5.2e-7
+    // instead of 1.0e-6, in 142 instead of 153.
+    if (DT == IABN_F32)
+        while (waves < 8 && waves * 8 * a.splits < lines) waves *= 2;
     const size_t lds = static_cast<size_t>(waves) * NW * MT * kWave * sizeof(f32x4);
     few_kernel<DT, KIND, MT>
         <<<dim3(static_cast<uint32_t>(blocks), a.splits), waves * kWave, lds, st>>>(a);

@@ -16,13 +16,13 @@ M = 100  # (more than the few tokens' kernels take)
 BIG = 4096.0
 
 
-def check(name, got, terms):
+def check(name, got, terms, parts=None):
     """Each of `terms` terms: BIG^2, and ones.  A part of 256 terms rounds 256 times, the
     parts' sum as often as there are parts (two more where a sum is of two products),
     each by half a step of at most the sum."""
     want = BIG * BIG + terms - 1
-    allowed = (256 + -(-terms // 256) + 2) * 2.0 ** -24 * want
-    assert allowed < 0.1 * terms
+    allowed = (256 + (parts or -(-terms // 256)) + 2) * 2.0 ** -24 * want
+    assert allowed < 0.15 * terms
     off = float((got.double() - want).abs().max())
     assert off <= allowed, (name, off, allowed)
 
@@ -81,3 +81,30 @@ def test_projections_and_dh(C, F):
                                new(1, F, C), new(1, F, C), new(1, C, F), act="leaky")
     check("dg", dg, C)
     check("du", du, C)
+
+
+@pytest.mark.parametrize("rows,k,E,N", [(16, 4, 64, 512), (1, 1, 1, 24), (40, 8, 64, 256), (50, 2, 3, 40)])
+def test_few_tokens(rows, k, E, N):
+    """Few tokens' kernels: a wave adds 256 terms, a block has 8 waves for 2048 (many
+    blocks too, whose waves would fill the chip with fewer)."""
+    K = 2048
+    ones = torch.zeros(rows, K, device="cuda")
+    ones[:, 0] = 1.0
+    x = vector(K).cuda().expand(rows, K).contiguous()
+    w = vector(K).cuda().expand(E, N, K).contiguous()
+    chosen = torch.arange(rows * k, dtype=torch.int32, device="cuda").view(rows, k) % E
+    plan = torch.empty(iabn.iabn_experts_plan_size(rows, k, E), dtype=torch.int32, device="cuda")
+    iabn.iabn_experts_plan(chosen, plan, E)
+    weights = torch.zeros(rows, k, device="cuda")
+    weights[:, 0] = 1.0
+    g, u = (torch.empty(rows * k, N, device="cuda") for _ in range(2))
+    iabn.iabn_experts_forward(x, plan, weights, w, w, w.transpose(1, 2).contiguous(), torch.empty_like(x), g, u)
+    check("g", g, K, parts=8)
+    check("u", u, K, parts=8)
+    # y: h = (BIG, 1, ...), the down weights too.
+    x, wide = ones[:, :N].contiguous(), torch.zeros(E, K, N, device="cuda")
+    wide[:, :, 0] = 1.0
+    up = wide.clone()
+    up[:, 0, 0] = BIG
+    y = iabn.iabn_experts_forward(x, plan, weights, wide, up, w, torch.empty_like(x), act="leaky")
+    check("y", y, K, parts=8 + 16)  # (a sum may be split over 16 blocks)
