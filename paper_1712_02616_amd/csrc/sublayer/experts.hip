@@ -96,7 +96,10 @@ void launch_dots(const float* dots, const int32_t* place, float* dweights, int64
 // experts (2048 -> 1024) 143 / 161 / 175 / 181 and 147 / 162 / 164 / 164; 2 of 8 (2048
 // -> 4096) 95 / 97 / 104 / 113 and 128 / 117 / 118 / 132; fp16 4 of 32 (1024 -> 2048) 81
 // / 85 / 91 / 95 and 86 / 90 / 91 / 91; fp32 2 of 7 (1000 -> 731) 30 / 39 / 40 / 69 and
-// 51 each.  One token of the first: 30 and 48.
+// 51 each.  One token of the first: 32 and 48.  What is faster goes by the rows of an
+// expert and its weights' bytes; one limit on tokens lies between: from 40 to 56
+// tokens the tiles would take up to 11 us less of the first, above it the few tokens'
+// kernels up to 19 less of the second (at 64).
 constexpr int64_t kFewTokens = 56;
 bool few_pairs(int64_t M) { return M <= kFewTokens; }
 

@@ -132,7 +132,7 @@ __device__ __forceinline__ bool find_group(const int32_t* offsets, int E, int P,
 // `high` and 8 in `low`: with fp32's range, and so many digits that they do not show
 // beside the result's rounding.  (In the storage type y of (4096, 8 of 64 experts,
 // 2048 -> 1024) bf16 is off by 2.9e-3 in root mean square, with these by 2.3e-3,
-// which h's rounding leaves, at 24 us of 545 more.)
+// which h's rounding leaves, at 26 us of 545 more.)
 template <int DT>
 __device__ __forceinline__ void store_terms(void* high, void* low, int64_t at, int n, const float (&v)[kChunk]) {
     if constexpr (DT == IABN_F32) {

@@ -14,9 +14,11 @@
 // few are formed and compared in 64 bits.  (That is what one wave in a hundred does;
 // all scores in 64 bits for it (16384, 256) bf16, 8 of 256: 29 us instead of 20.)
 //
-// Bound by latency: (16384, 256) bf16, 8 of 256 by sigmoids with a bias in 4 of 8
-// groups, 20 us for 9.5 MB (17.6 with no close scores; 12.5 of them without the groups, 12.2 with
-// one choice); four waves a SIMD go through load, scores, groups and choices once.
+// Bound by instructions: (16384, 256) bf16, 8 of 256 by sigmoids with a bias in 4 of 8
+// groups, 20 us for 9.5 MB, vector units at work in 0.69 of the cycles (17.6 with no
+// close scores; 12.5 of them without the groups, 12.2 with one choice).  A choice goes
+// through a lane's 16 values three times, a group's sum through LDS twice; the rest of
+// the cycles are steps that four waves a SIMD, which go through them once, do not hide.
 // Rows in 16 lanes share the instructions of the maxima (in 64 lanes: 27 us, the
 // (4099, 61) fp32 case 4.4 instead of 3.7; the backward 9.7 instead of 7.6).  One
 // row: 2.6 us, a launch.
@@ -493,7 +495,8 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
 //
 // (16384, 256) bf16, 8 of 256, not renormalised: 7.6 us for 18 MB, vector arithmetic
 // in 0.64 of the busy cycles (a precise exponential for every logit; 11.7 us where
-// each lane compared each choice with each of its experts, and with a division).
+// each lane compared each choice with each of its experts, and with a division); of
+// sigmoids 9.5, two for every logit; renormalised 5.0 and 5.1.
 //
 //   d_j = scale*dw_j;  softmax: dl = s*(d - sum of s_j d_j), d = 0 for what was not
 //   chosen; sigmoid: dl = d*s*(1 - s).  Renormalised, p_j = s_j/sum of the chosen s:
@@ -591,8 +594,14 @@ __global__ __launch_bounds__(kThreads) void route_bwd_kernel(RouteBwdArgs a) {
 
 // ---------------------------------------------------------------- launches
 
-// Rows in 16 lanes where they and the choices fit: four rows share every
-// instruction of the maxima.
+// Rows in 16 lanes where they and the choices fit: four rows share every instruction
+// of the maxima, which counts where there are rows for all SIMDs.  (Rows in 16 and in 64
+// lanes, bf16, us in a graph, forward and backward, for 1024 / 2048 / 4096 / 16384 rows.
+// 2 of 16: 2.1 / 2.1 / 2.1 / 2.6 and 2.3 / 2.4 / 3.0 / 6.2; 2.5 / 2.5 / 2.6 / 3.0 and 2.6 /
+// 2.8 / 3.2 / 6.0.  8 of 64: 3.3 / 3.4 / 3.4 / 5.1 and 3.1 / 3.5 / 4.6 / 11.5; 3.1 / 3.1 / 3.1
+// / 4.1 and 2.8 / 2.9 / 3.4 / 6.8.  8 of 256: 5.8 / 5.9 / 6.0 / 10.2 and 3.9 / 4.4 / 6.0 /
+// 16.2; 4.9 / 5.0 / 5.2 / 7.6 and 3.3 / 3.4 / 4.4 / 9.6.  One limit for all: between it and
+// 4096 rows of 256 the other side would take up to 1.9 us less.)
 bool narrow_rows(int64_t M, int E, int k, int groups) { return E <= 256 && k <= 16 && groups <= 16 && M > 1024; }
 
 template <int DT, int L, int V>
