@@ -601,7 +601,7 @@ __global__ __launch_bounds__(kThreads) void route_bwd_kernel(RouteBwdArgs a) {
 // 2.8 / 3.2 / 6.0.  8 of 64: 3.3 / 3.4 / 3.4 / 5.1 and 3.1 / 3.5 / 4.6 / 11.5; 3.1 / 3.1 / 3.1
 // / 4.1 and 2.8 / 2.9 / 3.4 / 6.8.  8 of 256: 5.8 / 5.9 / 6.0 / 10.2 and 3.9 / 4.4 / 6.0 /
 // 16.2; 4.9 / 5.0 / 5.2 / 7.6 and 3.3 / 3.4 / 4.4 / 9.6.  One limit for all: between it and
-// 4096 rows of 256 the other side would take up to 1.9 us less.)
+// 4096 rows of 256 the other side would take up to 1.9 us less, 2.4 with groups.)
 bool narrow_rows(int64_t M, int E, int k, int groups) { return E <= 256 && k <= 16 && groups <= 16 && M > 1024; }
 
 template <int DT, int L, int V>
